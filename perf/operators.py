@@ -11,7 +11,8 @@ taken from such rows.  A case is one call, or one short sequence of calls, of a 
 
 8-bit rows: blocks of 32 consecutive elements, the last block of a row filled up with zeros; one power of two 2^e per
 block, the smallest with max|x| < 127.5 * 2^e (e >= -126), kept as e + 127; the elements are x * 2^-e rounded to the
-nearest integer, ties to even.  A block that holds an infinity or a NaN has scale 255 and stands for NaNs.
+nearest integer, ties to even.  A block that holds a NaN, an infinity or the last half percent below it (127.5 * 2^121 and
+more) has scale 255 and stands for NaNs.
 """
 from __future__ import annotations
 
@@ -152,7 +153,7 @@ def _to_q8(x: torch.Tensor):
     top = t.abs().view(torch.int32).amax(-1, keepdim=True)         # the bits of a magnitude order like it
     scale = (((top + 0x10000) >> 23) - 6).clamp(min=1)             # one more from 127.5 / 64 on
     q = torch.round(t * ((254 - scale) << 23).view(torch.float32))
-    finite = top < 0x7f800000
+    finite = top < 0x7f7f0000                                      # the bits of 127.5 * 2^121
     q = torch.where(finite, q, torch.zeros_like(q)).to(torch.int8)
     scale = torch.where(finite, scale, torch.full_like(scale, 255)).to(torch.uint8)
     return q.view(rows, blocks * BLOCK), scale.view(rows, blocks)
@@ -233,7 +234,7 @@ def _rounded64(x: torch.Tensor) -> torch.Tensor:
     part, power = torch.frexp(top)                                 # top = part * 2^power, 1/2 <= part < 1
     e = torch.where(part * 128.0 < 127.5, power - 7, power - 6).clamp(min=-126)
     step = ((e.long() + 1023) << 52).view(torch.float64)            # 2^e, exactly
-    out = torch.where(torch.isfinite(top), torch.round(t / step) * step, torch.full_like(t, math.nan))
+    out = torch.where(top < 127.5 * 2.0 ** 121, torch.round(t / step) * step, torch.full_like(t, math.nan))
     return out.reshape(rows, width)[:, :cols]
 
 
