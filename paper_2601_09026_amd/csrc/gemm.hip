@@ -890,17 +890,6 @@ gemm_f32_small_kernel(const GemmArgs a, int tiles_n) {
 // before a product of two reduction-contiguous operands.
 // ---------------------------------------------------------------------------
 
-// Sum that carries its rounding error along (Kahan): 16384 positive terms come out within 7e-8 of their sum, as a
-// plain chain within 8e-7 to 3e-6, depending on their spread.  An infinite sum carries nothing, so it stays infinite.
-struct CarrySum {
-  float sum = 0.f, err = 0.f;
-  __device__ __forceinline__ void add(float x) {
-    const float y = x - err, t = sum + y;
-    err = __builtin_isfinite(t) ? (t - sum) - y : 0.f;
-    sum = t;
-  }
-};
-
 template <int BM, int BN, int STAGES, int WM, int WN, bool TAIL>
 __global__ void __launch_bounds__(64 * WM * WN, WM * WN / 4)
 gemm_tn_mfma_kernel(const GemmTnArgs a, int tiles_m, int tiles_n, int splits, int total_tiles, int per_xcd) {

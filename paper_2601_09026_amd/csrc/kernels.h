@@ -139,6 +139,47 @@ hipError_t launch_sum_slots(const float* in, int n, long elems, float* out, floa
 size_t ln_param_partial_floats(int n_groups, int T, int d, int n_items);
 hipError_t launch_ln_param_grad(const LnParamArgs& a, float* partial, bool is_bf16, hipStream_t st);
 
+// ---- q8.hip, norm.hip, q8_grad.hip: rows kept in 8 bits, LayerNorm on its own, gradients from kept rows ------------
+struct Q8Rows {                                           // q8.h has the format
+  unsigned char* q;                                       // [rows, 32 * blocks] (int8)
+  unsigned char* scale;                                   // [rows, blocks]
+  long rows; int cols;
+};
+hipError_t launch_q8_pack(const Q8Rows& r, const void* x, long ldx, bool is_bf16, hipStream_t st);
+// `groups` runs of r.rows rows, src_rows kept rows apart (also backwards), to runs dst_rows rows of x apart
+hipError_t launch_q8_unpack(const Q8Rows& r, void* x, long ldx, bool is_bf16, int groups, long src_rows, long dst_rows,
+                            hipStream_t st);
+struct NormFwdArgs {
+  long rows; int cols, blocks;                            // blocks: q8_blocks(cols)
+  const void* x; long ldx;
+  const float *gamma, *beta;                              // null: 1, 0
+  void* y; long ldy; bool y_bf16;
+  float *mean, *rstd;                                     // optional
+  unsigned char *xq, *xs, *yq, *ys;                       // optional copies in 8 bits
+  float eps;
+};
+hipError_t launch_norm_forward(const NormFwdArgs& a, bool x_bf16, hipStream_t st);
+struct NormBwdArgs {
+  long rows; int cols, blocks;
+  const void* dy; long ldy;
+  const void* x; long ldx; bool x_bf16;                   // x_bf16: of x and of dx
+  const unsigned char *xq, *xs;                           // x in 8 bits instead, or null
+  const float *gamma, *mean, *rstd;                       // gamma null: 1
+  void* dx; long lddx;                                    // optional, as dgamma and dbeta
+  float *dgamma, *dbeta;
+};
+size_t norm_backward_partial_floats(long rows, int cols);
+hipError_t launch_norm_backward(const NormBwdArgs& a, bool dy_bf16, float* partial, hipStream_t st);
+struct Q8GradArgs {
+  long rows; int M, N;                                    // tokens, out features, in features
+  const void* dy; long ldy;                               // [rows, M]
+  const unsigned char *xq, *xs; int blocks;               // [rows, N] in 8 bits
+  float *dW, *db;                                         // [M, N]; [M] or null
+  float scale;
+};
+size_t q8_grad_partial_floats(long rows, int M, int N, bool dy_bf16);
+hipError_t launch_q8_grad(const Q8GradArgs& a, bool dy_bf16, float* partial, hipStream_t st);
+
 // ---- attention.hip -----------------------------------------------------------
 struct AttnArgs {
   int n_groups, B, H, dh, Sq, Sk, causal;

@@ -25,8 +25,10 @@
 #include <vector>
 
 #include "../../include/mgrit.h"
+#include "api.h"
 #include "common.h"
 #include "kernels.h"
+#include "q8.h"
 
 using namespace mg;
 
@@ -231,6 +233,12 @@ struct Engine {
   // adjoint without the N-layer linearisation cache: the cache arrays hold one launch chunk (Gc slots,
   // one set per lane) and every chunk of transposed steps first recomputes the internals of its layers
   bool recompute = false;
+  // adjoint from states that were kept in 8 bits (q8.h): [N, T, d] rows of 32 * blocks.  Without the N-layer cache a lane
+  // brings back the states of its chunk, in lin through tabLin; with it all of them are brought back before the cache is filled.
+  const unsigned char *z8 = nullptr, *z8_scale = nullptr;
+  bool from_q8 = false;
+  float* lin = nullptr;
+  void** tabLin = nullptr;
   // sign of the step inside OUT = RHS + sign * (step): -1 while the driver forms a coarse right-hand side
   float rhs_sign = 1.f;
   long Td() const { return (long)T * d; }
@@ -330,6 +338,10 @@ struct Engine {
     dxin = b.take<float>(G * T * d);
     Dbuf = b.take<float>(G * md.batch * H * md.seq);
     qkv = o = act = nullptr; xin = nullptr;
+    if (from_q8 && recompute) {
+      lin = b.take<float>(G * T * d);
+      tabLin = b.take<void*>(G);
+    }
     if (per_group_mem) {
       membG = b.take_bytes(G * Tm * d * esz);
       dkvc = b.take_bytes(G * Tm * 2 * d * esz);
@@ -884,6 +896,17 @@ int forward_groups(Engine& E, Engine* E2, int G, Rows IN, Rows OUT, Rows RHS, Pa
   });
 }
 
+// The linearisation states of a chunk, brought back from 8 bits where that is how they are kept (no N-layer cache: E.recompute)
+int bring_back(Engine& E, int n, Rows& LIN) {
+  if (!E.from_q8) return MGRIT_OK;
+  const long blocks = q8_blocks(E.d);
+  const Q8Rows r = {const_cast<unsigned char*>(E.z8) + (long)LIN.i0 * E.T * blocks * Q8_BLOCK,
+                    const_cast<unsigned char*>(E.z8_scale) + (long)LIN.i0 * E.T * blocks, E.T, E.d};
+  HIPCHK(launch_q8_unpack(r, E.lin, E.d, false, n, (long)LIN.is * E.T, E.T, E.st));
+  LIN = Rows{(const void* const*)E.tabLin, 0, 1};
+  return MGRIT_OK;
+}
+
 // emit: the steps also write the parameter gradients of their layers (DT, may be null) and the
 // memory-gradient terms (dE_all, may be null); the caller guarantees that IN holds final values
 int adjoint_groups(Engine& E, Engine* E2, int G, Rows IN, Rows OUT, Rows RHS, Params TH, Params THT, Rows LIN,
@@ -903,16 +926,17 @@ int adjoint_groups(Engine& E, Engine* E2, int G, Rows IN, Rows OUT, Rows RHS, Pa
     }
     Slots slots = shift(cs, c0);
     gp.dE_slots = slots;
+    Rows at = shift(LIN, c0);
     if (L.recompute) {                    // the internals of this chunk's layers, into the lane's chunk-sized cache
       slots = Slots{0, 1};
-      STCHK(forward_chunk(L, n, shift(LIN, c0), NO_ROWS, NO_ROWS, shift(TH, c0), 0.f, 1, slots,
-                          sd ? s.MEM : NO_ROWS));
+      STCHK(bring_back(L, n, at));
+      STCHK(forward_chunk(L, n, at, NO_ROWS, NO_ROWS, shift(TH, c0), 0.f, 1, slots, sd ? s.MEM : NO_ROWS));
     }
     STCHK(adjoint_chunk(L, n, shift(IN, c0), shift(OUT, c0), shift(RHS, c0), shift(TH, c0), shift(THT, c0),
-                        shift(LIN, c0), slots, hstep, emit ? &gp : nullptr, sd ? &s : nullptr, sh ? &shc : nullptr));
+                        at, slots, hstep, emit ? &gp : nullptr, sd ? &s : nullptr, sh ? &shc : nullptr));
     if (!emit) return (int)MGRIT_OK;
     const bool shadow = sh && shc.have_inputs(n);
-    return param_grads_chunk(L, n, shift(THT, c0), shift(LIN, c0), slots, hstep, gp, shadow ? shc.in : L.cb,
+    return param_grads_chunk(L, n, shift(THT, c0), at, slots, hstep, gp, shadow ? shc.in : L.cb,
                              shadow ? shc.in_slots : Slots{0, 1}, sd ? &s : nullptr);
   });
 }
@@ -929,14 +953,15 @@ int gradient_groups(Engine& E, Engine* E2, int G, Rows IN, Params TH, Params THT
     if (sd) s = shift(*sd, c0);
     Slots slots = shift(cs, c0);
     gp.dE_slots = slots;
+    Rows at = shift(LIN, c0);
     if (L.recompute) {
       slots = Slots{0, 1};
-      STCHK(forward_chunk(L, n, shift(LIN, c0), NO_ROWS, NO_ROWS, shift(TH, c0), 0.f, 1, slots,
-                          sd ? s.MEM : NO_ROWS));
+      STCHK(bring_back(L, n, at));
+      STCHK(forward_chunk(L, n, at, NO_ROWS, NO_ROWS, shift(TH, c0), 0.f, 1, slots, sd ? s.MEM : NO_ROWS));
     }
-    STCHK(adjoint_chunk(L, n, shift(IN, c0), NO_ROWS, NO_ROWS, shift(TH, c0), shift(THT, c0), shift(LIN, c0),
+    STCHK(adjoint_chunk(L, n, shift(IN, c0), NO_ROWS, NO_ROWS, shift(TH, c0), shift(THT, c0), at,
                         slots, hstep, &gp, sd ? &s : nullptr));
-    return param_grads_chunk(L, n, shift(THT, c0), shift(LIN, c0), slots, hstep, gp, L.cb, Slots{0, 1},
+    return param_grads_chunk(L, n, shift(THT, c0), at, slots, hstep, gp, L.cb, Slots{0, 1},
                              sd ? &s : nullptr);
   });
 }
@@ -1357,6 +1382,7 @@ bool keeps_kv(const mgrit_model_desc* md, const mgrit_opts* op) {
 struct Extras {
   bool kv = true;                   // forward: the memory's K | V of every layer where that can pay (see keeps_kv)
   bool few = true;                  // launch chunks for layers of few tokens (see default_groups)
+  bool q8 = false;                  // adjoint: the states are kept in 8 bits (the call's form, not a choice)
 };
 
 struct Plan {                       // workspace of mgrit_forward / mgrit_adjoint
@@ -1365,6 +1391,7 @@ struct Plan {                       // workspace of mgrit_forward / mgrit_adjoin
   Driver D;
   void* thT_blocks = nullptr;
   void** tabDT = nullptr;           // layer n -> gradient block (adjoint with parameter gradients)
+  float* z_all = nullptr;           // states brought back from 8 bits, [N, T, d]
   float* dE_all = nullptr;          // cross-attention decoder: per-layer terms of the memory gradient
   size_t bytes = 0;
 };
@@ -1385,6 +1412,7 @@ int make_plan(Plan& P, const mgrit_model_desc* md, const mgrit_opts* op, int mod
   const int M0 = serial ? 1 : N / op->cf;
   E.keep_inputs = mode == 2;
   E.recompute = adjoint && !g_adjoint_cache;
+  E.from_q8 = adjoint && extras.q8;
   int gc = solve_groups(md, M0, E.recompute, extras.few);
   const int widest = adjoint ? (N > M0 ? N : M0) : M0;      // the cache pass batches over all N layers
   if (gc > widest) gc = widest;
@@ -1403,6 +1431,7 @@ int make_plan(Plan& P, const mgrit_model_desc* md, const mgrit_opts* op, int mod
   D.h = op->h;
   D.tabW = b.take<void*>(N + 1);
   D.tabTh = b.take<void*>(N);
+  if (E.from_q8 && !E.recompute) P.z_all = b.take<float>((size_t)N * E.T * E.d);
   if (adjoint) {
     D.tabZ = b.take<void*>(N + 1);
     D.tabThT = b.take<void*>(N);
@@ -1536,6 +1565,12 @@ int layer_step_on(const mgrit_model_desc* desc, int adjoint, int n_groups, const
 
 }  // namespace
 
+std::recursive_mutex& mg::call_mutex() { return g_call_mutex; }
+int mg::hip_failed(hipError_t e) {
+  g_last_hip_error = (int)e;
+  return MGRIT_HIP_ERROR;
+}
+
 // Scratch memory of layer_step_batched_static: one array per GPU, part of the loaded code object (the
 // runtime places it when the library is loaded on a device; nothing is allocated at call time).
 // On the host this name is only a handle for hipGetSymbolAddress: the device address is looked up once
@@ -1622,10 +1657,11 @@ size_t least_bytes(const mgrit_model_desc* desc, const mgrit_opts* opts, int mod
 }
 // The first of the plans, fastest first, that a workspace of that size has room for; false: none.
 bool fit_plan(const mgrit_model_desc* desc, const mgrit_opts* opts, int mode, int share_mode, size_t bytes, Extras& x) {
+  const bool q8 = x.q8;
   for (bool kv : {true, false}) {
     if (!kv && (mode || share_mode || !keeps_kv(desc, opts))) break;
     for (bool few : {true, false}) {
-      x = {kv, few};
+      x = {kv, few, q8};
       if (plan_bytes(desc, opts, mode, share_mode, x) <= bytes) return true;
     }
   }
@@ -1674,10 +1710,11 @@ int forward_impl(const mgrit_model_desc* desc, const mgrit_opts* opts, const voi
 }
 
 // prefilled: the cache already holds the entries that a forward solve with share_ws = workspace leaves
+// z8_scale: the states are kept in 8 bits, Z_all their elements
 int adjoint_impl(const mgrit_model_desc* desc, const mgrit_opts* opts, const void* Z_all,
                  const void* const* theta, const void* memory, const void* lambda_N, void* lambda_all,
                  void* dmemory, void* const* dtheta, float* resnorm, void* workspace, size_t workspace_bytes,
-                 bool prefilled, void* stream) {
+                 bool prefilled, void* stream, const void* z8_scale = nullptr) {
   std::lock_guard<std::recursive_mutex> call_lock(g_call_mutex);
   if (prefilled && !g_adjoint_cache) return MGRIT_INVALID_ARG;
   STCHK(validate_desc(desc));
@@ -1689,6 +1726,7 @@ int adjoint_impl(const mgrit_model_desc* desc, const mgrit_opts* opts, const voi
   if (dtheta) STCHK(check_ptr_array((const void* const*)dtheta, opts->N));
   const int mode = (dtheta || dmemory) ? 2 : 1;
   Extras extras;
+  extras.q8 = z8_scale != nullptr;
   if (!fit_plan(desc, opts, mode, 0, workspace_bytes, extras)) return MGRIT_WORKSPACE_TOO_SMALL;
   hipStream_t st = static_cast<hipStream_t>(stream);
 
@@ -1698,6 +1736,19 @@ int adjoint_impl(const mgrit_model_desc* desc, const mgrit_opts* opts, const voi
   Driver& D = P.D;
   const int N = opts->N;
   const size_t state = (size_t)E.T * E.d * sizeof(float);
+  if (z8_scale) {
+    for (Engine* L : {&E, D.E2}) {
+      if (!L) continue;
+      L->z8 = static_cast<const unsigned char*>(Z_all);
+      L->z8_scale = static_cast<const unsigned char*>(z8_scale);
+      if (L->recompute) HIPCHK(launch_fill_table(L->tabLin, reinterpret_cast<char*>(L->lin), (long)state, L->Gc, st));
+    }
+    if (!E.recompute) {
+      const Q8Rows r = {const_cast<unsigned char*>(E.z8), const_cast<unsigned char*>(E.z8_scale), (long)N * E.T, E.d};
+      HIPCHK(launch_q8_unpack(r, P.z_all, E.d, false, 1, 0, 0, st));
+    }
+    Z_all = P.z_all;                      // (null without the cache: no state is reached through the table then)
+  }
   // reversed index: point m lives in row N-m
   HIPCHK(launch_fill_table(D.tabW, static_cast<char*>(lambda_all) + (size_t)N * state, -(long)state, N + 1, st));
   HIPCHK(launch_fill_table(D.tabZ, static_cast<char*>(const_cast<void*>(Z_all)), (long)state, N + 1, st));
@@ -1819,6 +1870,22 @@ int mgrit_adjoint(const mgrit_model_desc* desc, const mgrit_opts* opts, const vo
                   void* stream) {
   return adjoint_impl(desc, opts, Z_all, theta, memory, lambda_N, lambda_all, dmemory, dtheta, resnorm, workspace,
                       workspace_bytes, false, stream);
+}
+
+size_t mgrit_adjoint_q8_workspace_bytes(const mgrit_model_desc* desc, const mgrit_opts* opts, int adjoint) {
+  if (validate_desc(desc) != MGRIT_OK || validate_opts(opts) != MGRIT_OK || adjoint < 1 || adjoint > 2) return 0;
+  Extras x;
+  x.q8 = true;
+  return plan_bytes(desc, opts, adjoint, 0, x);
+}
+
+int mgrit_adjoint_q8(const mgrit_model_desc* desc, const mgrit_opts* opts, const void* Z_q8, const void* Z_q8_scale,
+                     const void* const* theta, const void* memory, const void* lambda_N, void* lambda_all,
+                     void* dmemory, void* const* dtheta, float* resnorm, void* workspace, size_t workspace_bytes,
+                     void* stream) {
+  if (!Z_q8_scale || (reinterpret_cast<uintptr_t>(Z_q8) & 15)) return MGRIT_INVALID_ARG;
+  return adjoint_impl(desc, opts, Z_q8, theta, memory, lambda_N, lambda_all, dmemory, dtheta, resnorm, workspace,
+                      workspace_bytes, false, stream, Z_q8_scale);
 }
 
 int mgrit_adjoint_linearised(const mgrit_model_desc* desc, const mgrit_opts* opts, const void* Z_all,

@@ -11,7 +11,8 @@ enum ProfClass : int {
   PC_GEMM_MFMA = 8,          // + epilogue id (0..6): launches over several groups (relaxation sweeps)
   PC_GEMM_MFMA_SINGLE = 16,  // + epilogue id: one group per launch (the serial coarse chain)
   PC_CHAIN = 24,             // row-local chains of a narrow layer
-  PC_COUNT = 25
+  PC_Q8 = 25, PC_NORM_FWD = 26, PC_NORM_BWD = 27, PC_Q8_GRAD = 28,   // rows in 8 bits, LayerNorm on its own, gradients
+  PC_COUNT = 29
 };
 
 bool prof_enabled();
