@@ -419,8 +419,8 @@ int mgrit_layer_norm_backward(const mgrit_norm_desc* desc, const void* dy, int64
  *   dy               device [rows, out_features], fp32 or bf16 (dy_dtype)
  *   x_q8, x_q8_scale device, 8-bit rows of in_features elements
  * dW and db are fp32 and overwritten; products are exact and added up in fp32 (an fp32 dy is multiplied in full, not
- * rounded to bf16).  At most 2^24 features either way and 2^31 weights (MGRIT_UNSUPPORTED beyond).  Workspace: 256-byte
- * aligned, mgrit_q8_weight_grad_workspace_bytes (host only, 0 on invalid arguments). */
+ * rounded to bf16).  At most 2^24 features either way, dy_stride 2^24 and 2^31 weights (MGRIT_UNSUPPORTED beyond).
+ * Workspace: 256-byte aligned, mgrit_q8_weight_grad_workspace_bytes (host only, 0 on invalid arguments). */
 size_t mgrit_q8_weight_grad_workspace_bytes(int64_t rows, int32_t out_features, int32_t in_features, int dy_dtype);
 int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features, int dy_dtype,
                          const void* dy, int64_t dy_stride, const void* x_q8, const void* x_q8_scale, float scale,

@@ -144,6 +144,7 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
                          void* workspace, size_t workspace_bytes, void* stream) {
   STCHK(check_weight_grad(rows, out_features, in_features, dy_dtype));
   STCHK(check_rows(rows, out_features, dy, dy_stride, dy_dtype));
+  if (rows && dy_stride > MOST_FEATURES) return MGRIT_UNSUPPORTED;        // a tile's offsets have 32 bits
   STCHK(check_q8(rows, x_q8, x_q8_scale));
   if (!dW || !aligned(dW, 4) || !aligned(db, 4) || !isfinite(scale)) return MGRIT_INVALID_ARG;
   if (!workspace || !aligned(workspace, 256)) return MGRIT_INVALID_ARG;

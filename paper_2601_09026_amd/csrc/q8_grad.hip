@@ -4,12 +4,17 @@
 // fp32 dY is exactly the sum of three of 8 bits each (cut, not rounded: hi = its upper 16 bits, then the same of the rest,
 // then what is left).  So the products run on the bf16 matrix cores, one or three of them, without any rounding of an
 // operand, and the sums are fp32 either way: what differs from an fp32 product is only the order of the additions.
-// Bound by the matrix cores (2 T M N flops, or three times that).
+// Bound by the matrix cores (2 T M N flops, or three times that).  16384 tokens, 4096 x 4096, bf16: 495 us, 1110 TFLOP/s, where
+// the library's product of bf16 operands in this order reaches 1150; 8192 tokens, 4096 x 2048, fp32: 366 us, 375 TFLOP/s (1126
+// of bf16 products; the fp32 matrix cores' own limit is 157).
 //
 // Both operands are token-major and the reduction runs over the tokens, so the tiles are staged as they lie in memory
 // ([token][feature], bf16) and the fragments come out of LDS through the transposing read; rows of a tile keep their
-// 16-byte chunks XOR-swizzled by the row.  Global loads go to registers a tile and a half ahead; between there and LDS the
-// kept rows become bf16 and an fp32 dY its three parts.
+// 16-byte chunks XOR-swizzled by the row.  Global loads go to registers two tiles ahead; between there and LDS the kept rows
+// become bf16 (2.5 instructions per element, once per tile and not per fragment) and an fp32 dY its three parts.  What
+// paid, at 16384 x 4096 x 4096 in bf16: one tile of LDS stored before another is multiplied 721 us; stores, loads and
+// fragment reads between the products 731 (spilling); conversions and addresses of fewer instructions 508; wavefronts of
+// 64 x 128 instead of 128 x 64 in the block 495.
 #include "kernels.h"
 #include "lds_limit.h"
 #include "prof.h"
@@ -18,7 +23,7 @@
 namespace mg {
 namespace {
 
-constexpr int BK = 32;                                   // tokens per tile
+template <int V> using Int = std::integral_constant<int, V>;
 
 // upper halves of two words: the two as bf16, cut
 __device__ __forceinline__ unsigned upper(float lo, float hi) { return __builtin_amdgcn_perm(f_bits(hi), f_bits(lo), 0x07060302u); }
@@ -56,128 +61,169 @@ template <> struct Chunk<float> {
   }
   __device__ float at(int j) const { return v[j >> 2][j & 3]; }
   __device__ void parts(u32x4 (&out)[3]) const {
-    float hi[8], mid[8], lo[8];
+    float top = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float x = at(j);
-      hi[j] = x;
-      const float r = __builtin_isinf(x) ? 0.f : x - cut(x);       // an infinity has no rest; a NaN stays one
-      mid[j] = r;
-      lo[j] = r - cut(r);
+    for (int j = 0; j < 8; j += 2) top = fmaxf(top, fmaxf(fabsf(at(j)), fabsf(at(j + 1))));
+    float mid[8], lo[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mid[j] = at(j) - cut(at(j));
+    if (__builtin_expect(__builtin_isinf(top), 0)) {      // an infinity has no rest (a NaN's is one)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mid[j] = __builtin_isinf(at(j)) ? 0.f : mid[j];
     }
 #pragma unroll
+    for (int j = 0; j < 8; ++j) lo[j] = mid[j] - cut(mid[j]);
+#pragma unroll
     for (int j = 0; j < 4; ++j) {
-      out[0][j] = upper(hi[2 * j], hi[2 * j + 1]);
+      out[0][j] = upper(at(2 * j), at(2 * j + 1));
       out[1][j] = upper(mid[2 * j], mid[2 * j + 1]);
       out[2][j] = upper(lo[2 * j], lo[2 * j + 1]);
     }
   }
 };
 
-template <typename T, int BM, int BN, int WM, int WN, int OCC>
+// byte I of a word, signed, as a float (the compiler takes two instructions for it)
+template <int I> __device__ __forceinline__ float signed_byte(unsigned v) {
+  float f;
+  if constexpr (I == 0) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(v));
+  if constexpr (I == 1) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(v));
+  if constexpr (I == 2) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(v));
+  if constexpr (I == 3) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(v));
+  return f;
+}
+// 4 kept elements as bf16
+__device__ __forceinline__ u32x2 kept_bf16(unsigned q, float step) {
+  return u32x2{upper(signed_byte<0>(q) * step, signed_byte<1>(q) * step), upper(signed_byte<2>(q) * step, signed_byte<3>(q) * step)};
+}
+
+// the sum of a fragment's 8 values
+__device__ __forceinline__ float fragment_sum(bf16x8 v) {
+  const u32x4 u = __builtin_bit_cast(u32x4, v);
+  float t[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t[i] = bits_f(u[i] << 16) + bits_f(u[i] & 0xffff0000u);
+  return (t[0] + t[1]) + (t[2] + t[3]);
+}
+
+// The work of a launch: `whole` tiles in one piece, then `rest` tiles of `slices` slices each.  Blocks go to the 8 XCDs in
+// turn; each XCD takes a contiguous run of either kind, so that what it works on at a time shares panels of the operands in
+// its L2.
+struct Items {
+  int whole, rest, slices, whole_xcd, rest_xcd;
+  Items(int tiles, int w, int s) : whole(w), rest(tiles - w), slices(s), whole_xcd((w + 7) / 8), rest_xcd((int)(((long)rest * s + 7) / 8)) {}
+  int blocks() const { return 8 * (whole_xcd + rest_xcd); }
+  __device__ bool item(int block, int& tile, int& slice) const {
+    const int xcd = block & 7, i = block >> 3;
+    slice = 0;
+    if (i < whole_xcd) {
+      tile = xcd * whole_xcd + i;
+      return tile < whole;
+    }
+    const int k = xcd * rest_xcd + i - whole_xcd;
+    tile = __builtin_amdgcn_readfirstlane(k / slices);
+    slice = k - tile * slices;
+    tile += whole;
+    return k < rest * slices;
+  }
+};
+
+template <typename T, int BM, int BN, int BK, int WM, int WN, int OCC>
 __global__ void __launch_bounds__(64 * WM * WN, OCC * WM * WN / 4)
-q8_grad_kernel(const Q8GradArgs a, int tiles_n, int per_slice, int splits, int total, int per_xcd, float* partial) {
+q8_grad_kernel(const Q8GradArgs a, int tiles_n, Items it, float* partial) {
   constexpr int NT = 64 * WM * WN, PARTS = std::is_same<T, float>::value ? 3 : 1;
   constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
   constexpr int RA = BM * 2, RB = BN * 2;                // bytes per LDS row
   constexpr int A_BYTES = BK * RA, B_BYTES = BK * RB, STAGE = PARTS * A_BYTES + B_BYTES;
-  constexpr int A_CH = BK * BM / 8 / NT, B_CH = BK * BN / 8 / NT;
-  static_assert(A_CH * NT * 8 == BK * BM && B_CH * NT * 8 == BK * BN && NT % (BM / 8) == 0, "tile / thread split");
+  constexpr int BE = BK * BN >= 16 * NT ? 16 : 8;          // kept elements per chunk
+  constexpr int A_CH = BK * BM / 8 / NT, B_CH = BK * BN / BE / NT, JOBS = A_CH + B_CH;
+  static_assert(A_CH * NT * 8 == BK * BM && B_CH * NT * BE == BK * BN && NT % (BM / 8) == 0, "tile / thread split");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  // an XCD takes a contiguous range of tiles, which share panels of the operands in its L2
-  const int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (tile >= total) return;
-  const int sp = __builtin_amdgcn_readfirstlane(tile / per_slice), tg = tile - sp * per_slice;
-  const int tm = __builtin_amdgcn_readfirstlane(tg / tiles_n), tn = tg - tm * tiles_n;
+  int tile, sp;
+  if (!it.item(blockIdx.x, tile, sp)) return;
+  const int splits = tile < it.whole ? 1 : it.slices;
+  const int tm = __builtin_amdgcn_readfirstlane(tile / tiles_n), tn = tile - tm * tiles_n;
   const int m0 = tm * BM, n0 = tn * BN, M = a.M, N = a.N, NP = a.blocks * Q8_BLOCK;
-  const long all_tiles = (a.rows + BK - 1) / BK;
-  const long kt0 = all_tiles * sp / splits, kt1 = all_tiles * (sp + 1) / splits;
-  const long K = (kt1 * BK < a.rows ? kt1 * BK : a.rows) - kt0 * BK;
-  const T* A = static_cast<const T*>(a.dy) + kt0 * BK * a.ldy + m0;
-  const unsigned char* Q = a.xq + kt0 * BK * NP + n0;
-  const unsigned char* S = a.xs + kt0 * BK * a.blocks + n0 / Q8_BLOCK;
+  const int all_tiles = (int)((a.rows + BK - 1) / BK);
+  const int kt0 = (int)((long)all_tiles * sp / splits), KT = (int)((long)all_tiles * (sp + 1) / splits) - kt0;
+  const long first = (long)kt0 * BK;
+  const int K = (int)(first + (long)KT * BK < a.rows ? (long)KT * BK : a.rows - first);     // tokens of the slice
+  const T* A = static_cast<const T*>(a.dy) + first * a.ldy + m0;
+  const unsigned char* Q = a.xq + first * NP + n0;
+  const unsigned char* S = a.xs + first * a.blocks + n0 / Q8_BLOCK;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wm0 = (wave / WN) * WTM, wn0 = (wave % WN) * WTN;
   auto swz_of = [](int row_bytes, int r) { return row_bytes >= 256 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; };
 
-  // this thread's chunks of a tile: token and feature
-  int arow[A_CH], brow[B_CH], adst[A_CH], bdst[B_CH];
-  const int ac = (threadIdx.x % (BM / 8)) * 8;
-  int bc[B_CH];
-#pragma unroll
-  for (int j = 0; j < A_CH; ++j) {
-    arow[j] = (threadIdx.x + j * NT) / (BM / 8);
-    adst[j] = arow[j] * RA + (((ac >> 3) ^ swz_of(RA, arow[j])) << 4);
-  }
-#pragma unroll
-  for (int j = 0; j < B_CH; ++j) {
-    const int id = threadIdx.x + j * NT;
-    brow[j] = id / (BN / 8);
-    bc[j] = id % (BN / 8) * 8;
-    bdst[j] = PARTS * A_BYTES + brow[j] * RB + (((bc[j] >> 3) ^ swz_of(RB, brow[j])) << 4);
-  }
+  // This thread's chunks of a tile: chunk j lies j * (rows of a pass) tokens below chunk 0.  A tile's base is uniform, a
+  // thread's place in it has 32 bits.
+  constexpr int A_ROWS = NT / (BM / 8), B_ROWS = NT / (BN / BE);
+  const int ar = threadIdx.x / (BM / 8), ac = threadIdx.x % (BM / 8) * 8;
+  const int br = threadIdx.x / (BN / BE), bc = threadIdx.x % (BN / BE) * BE;
   Chunk<T> ra[A_CH];
-  u32x2 rq[B_CH];
-  unsigned rs[B_CH];
-  const bool inner = m0 + BM <= M && n0 + BN <= NP;
-  auto load = [&](long k0) {
-    if (k0 >= K) return;
-    const T* at = A + k0 * a.ldy;
-    const unsigned char *q = Q + k0 * NP, *s = S + k0 * a.blocks;
-    if (inner && k0 + BK <= K) {
-#pragma unroll
-      for (int j = 0; j < A_CH; ++j) ra[j].load(at + arow[j] * a.ldy + ac);
-#pragma unroll
-      for (int j = 0; j < B_CH; ++j) {
-        rq[j] = *reinterpret_cast<const u32x2*>(q + (long)brow[j] * NP + bc[j]);
-        rs[j] = s[brow[j] * a.blocks + bc[j] / Q8_BLOCK];
+  unsigned rq[B_CH][BE / 4], rs[B_CH];
+  // (chunks past the last feature read the tile's first one instead: their columns are never stored)
+  const int ac_in = m0 + ac < M ? ac : 0, bc_in = n0 + bc < NP ? bc : 0;
+  const unsigned va = (unsigned)(ar * a.ldy + ac_in), vq = (unsigned)(br * NP + bc_in), vs = (unsigned)(br * a.blocks + bc_in / Q8_BLOCK);
+  auto load = [&](auto whole, int j, int kt) {            // job j of tile kt
+    const int k0 = kt * BK;
+    if (j < A_CH) {
+      const T* p = A + (long)(k0 + j * A_ROWS) * a.ldy;
+      if constexpr (decltype(whole)::value) {
+        ra[j < A_CH ? j : 0].load(p + va);
+      } else {                                            // zeros past the last token
+        Chunk<T>& c = ra[j < A_CH ? j : 0];
+        const int n = k0 + ar + j * A_ROWS < K ? M - m0 - ac_in : 0;
+        if (n >= 8) c.load(p + va);
+        else c.load_some(p + va, n);
       }
-      return;
-    }
+    } else {
+      const int i = j - A_CH < 0 ? 0 : j - A_CH;
+      const unsigned char *q = Q + (long)(k0 + i * B_ROWS) * NP, *s = S + (long)(k0 + i * B_ROWS) * a.blocks;
+      bool there = true;
+      if constexpr (!decltype(whole)::value) there = k0 + br + i * B_ROWS < K;
 #pragma unroll
-    for (int j = 0; j < A_CH; ++j) {                      // zeros past the last token and the last feature
-      const int n = k0 + arow[j] < K ? M - m0 - ac : 0;
-      if (n >= 8) ra[j].load(at + arow[j] * a.ldy + ac);
-      else if (n > 0) ra[j].load_some(at + arow[j] * a.ldy + ac, n);
-      else ra[j].clear();
-    }
+      for (int e = 0; e < BE / 4; ++e) rq[i][e] = 0;
+      rs[i] = 127;
+      if (there) {
+        if constexpr (BE == 16) {
+          const u32x4 v = *reinterpret_cast<const u32x4*>(q + vq);
 #pragma unroll
-    for (int j = 0; j < B_CH; ++j) {
-      rq[j] = u32x2{0, 0};
-      rs[j] = 127;
-      if (k0 + brow[j] < K && n0 + bc[j] < NP) {
-        rq[j] = *reinterpret_cast<const u32x2*>(q + (long)brow[j] * NP + bc[j]);
-        rs[j] = s[brow[j] * a.blocks + bc[j] / Q8_BLOCK];
+          for (int e = 0; e < 4; ++e) rq[i][e] = v[e];
+        } else {
+          const u32x2 v = *reinterpret_cast<const u32x2*>(q + vq);
+          rq[i][0] = v[0]; rq[i][1] = v[1];
+        }
+        rs[i] = s[vs];
       }
     }
   };
-  const bool sums = tn == 0 && a.db;                      // the first column of tiles adds up dY as well
-  CarrySum bias[8];
-  auto store = [&](int stage) {
+  auto store = [&](int j, int stage) {
     unsigned char* base = smem + stage * STAGE;
-#pragma unroll
-    for (int j = 0; j < A_CH; ++j) {
+    if (j < A_CH) {
+      const int row = ar + j * A_ROWS, at = row * RA + (((ac >> 3) ^ swz_of(RA, row)) << 4);
       u32x4 p[PARTS];
-      ra[j].parts(p);
+      ra[j < A_CH ? j : 0].parts(p);
 #pragma unroll
-      for (int i = 0; i < PARTS; ++i) *reinterpret_cast<u32x4*>(base + i * A_BYTES + adst[j]) = p[i];
-    }
+      for (int i = 0; i < PARTS; ++i) *reinterpret_cast<u32x4*>(base + i * A_BYTES + at) = p[i];
+    } else {
+      const int i = j - A_CH < 0 ? 0 : j - A_CH;
+      const int row = br + i * B_ROWS;
+      const float step = q8_step(rs[i]);
 #pragma unroll
-    for (int j = 0; j < B_CH; ++j) {
-      const float step = q8_step(rs[j]);
-      const f32x4 lo = q8_values(rq[j][0], step), hi = q8_values(rq[j][1], step);
-      *reinterpret_cast<u32x4*>(base + bdst[j]) = u32x4{upper(lo[0], lo[1]), upper(lo[2], lo[3]), upper(hi[0], hi[1]), upper(hi[2], hi[3])};
-    }
-    if (sums) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float t = ra[0].at(e);
-#pragma unroll
-        for (int j = 1; j < A_CH; ++j) t += ra[j].at(e);
-        bias[e].add(t);
+      for (int e = 0; e < BE / 8; ++e) {
+        const int at = PARTS * A_BYTES + row * RB + ((((bc >> 3) + e) ^ swz_of(RB, row)) << 4);
+        const u32x2 lo = kept_bf16(rq[i][2 * e], step), hi = kept_bf16(rq[i][2 * e + 1], step);
+        *reinterpret_cast<u32x4*>(base + at) = u32x4{lo[0], lo[1], hi[0], hi[1]};
       }
     }
   };
+  // The first column of tiles adds up dY as well, from the fragments: of the WN wavefronts that read the same ones each
+  // takes every WN-th 16 tokens.
+  const bool sums = tn == 0 && a.db;
+  CarrySum bias[TM];
+  float run[TM];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) run[i] = 0.f;
 
   // fragments: tokens 8*(lane/32).., one column per lane
   const int lh = lane >> 5, trow = 8 * lh + ((lane & 15) >> 2), low = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
@@ -197,97 +243,165 @@ q8_grad_kernel(const Q8GradArgs a, int tiles_n, int per_slice, int splits, int t
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   const lds_byte* lds0 = (const lds_byte*)smem;
 
-  const long KT = kt1 - kt0;
-  load(0);
-  if (KT > 0) store(0);
-  load(BK);
+  // A tile is STEPS steps of NM products each: 16 tokens and one part of dY.  During a step the next one's fragments are
+  // read.  The next tile's chunks go to the other stage during all steps but the last, the registers that held them are
+  // loaded again (for the tile after that) right behind; the last step begins with the block's barrier and reads the next
+  // tile's first fragments.
+  constexpr int KS = BK / 16, STEPS = KS * PARTS, NM = TM * TN, SLOTS = (STEPS - 1) * NM;
+  static_assert(STEPS >= 2, "a step to hand over in");
+  TrFrag fa[2][TM], fb[2][TN];
+  auto read_a = [&](auto step, unsigned stage_off, int i) {
+    constexpr int s = decltype(step)::value, ks = s / PARTS, part = PARTS - 1 - s % PARTS;
+    tr_read<part * A_BYTES + 16 * ks * RA, part * A_BYTES + (16 * ks + 4) * RA>(fa[s & 1][i], lds0 + stage_off + offa[i]);
+  };
+  auto read_b = [&](auto step, unsigned stage_off, int j) {
+    constexpr int s = decltype(step)::value, ks = s / PARTS;
+    tr_read<16 * ks * RB, (16 * ks + 4) * RB>(fb[ks & 1][j], lds0 + stage_off + offb[j]);
+  };
+  auto run_step = [&](auto step, auto jobs, auto whole, unsigned read_off, int nxt, int kt) {
+    constexpr int s = decltype(step)::value, ks = s / PARTS, r = (s + 1) % STEPS;
+    constexpr int RD = TM + (r % PARTS == 0 ? TN : 0);
+    bf16x8 xa[TM], xb[TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) xa[i] = tr_value(fa[s & 1][i]);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) xb[j] = tr_value(fb[ks & 1][j]);
+    __builtin_amdgcn_sched_barrier(0);
+    if (sums && wave % WN == ks % WN) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) run[i] += fragment_sum(xa[i]);
+    }
+#pragma unroll
+    for (int q = 0; q < NM; ++q) {
+      const int i = q / TN, j = q % TN;
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j], xa[i], acc[i][j], 0, 0, 0);
+      const int r0 = (q * RD * 4 / 3 + NM - 1) / NM, r1 = ((q + 1) * RD * 4 / 3 + NM - 1) / NM;
+#pragma unroll
+      for (int u = 0; u < RD; ++u)
+        if (u >= r0 && (u < r1 || q == NM - 1)) {
+          if (u < TM) read_a(Int<r>{}, read_off, u < TM ? u : 0);
+          else read_b(Int<r>{}, read_off, u < TM ? 0 : u - TM);
+        }
+      if constexpr (decltype(jobs)::value) {
+        const int slot = s * NM + q;
+#pragma unroll
+        for (int u = 0; u < JOBS; ++u)
+          if (u * SLOTS / JOBS == slot) {
+            store(u, nxt);
+            if (decltype(whole)::value || kt + 2 < KT) load(whole, u, kt + 2);
+          }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  int cur = 0;
+  auto tile_step = [&](auto jobs, auto whole, int kt) {
+    const unsigned so = cur * STAGE, sn = (cur ^ 1) * STAGE;
+    auto go = [&](auto self, auto step) {
+      constexpr int s = decltype(step)::value;
+      if constexpr (s < STEPS - 1) {
+        run_step(step, jobs, whole, so, cur ^ 1, kt);
+        self(self, Int<s + 1>{});
+      } else {
+        wait_lgkm();
+        bare_barrier();
+        run_step(step, std::false_type{}, whole, sn, cur ^ 1, kt);
+      }
+    };
+    go(go, Int<0>{});
+    if (sums) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) { bias[i].add(run[i]); run[i] = 0.f; }
+    }
+    cur ^= 1;
+  };
+  auto every_load = [&](int kt) {
+#pragma unroll
+    for (int j = 0; j < JOBS; ++j) load(std::false_type{}, j, kt);
+  };
+  every_load(0);
+#pragma unroll
+  for (int j = 0; j < JOBS; ++j) store(j, 0);
+  if (KT > 1) every_load(1);
   wait_lgkm();
   bare_barrier();
-  for (long kt = 0; kt < KT; ++kt) {
-    const int cur = (int)(kt & 1);
-    if (kt + 1 < KT) store(cur ^ 1);
-    load((kt + 2) * BK);
-    const lds_byte* base = lds0 + cur * STAGE;
 #pragma unroll
-    for (int ks = 0; ks < BK / 16; ++ks) {
-      bf16x8 xb[TN];
+  for (int i = 0; i < TM; ++i) read_a(Int<0>{}, 0, i);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        TrFrag f;
-        f.lo = tr_read4(base + offb[j] + 16 * ks * RB);
-        f.hi = tr_read4(base + offb[j] + (16 * ks + 4) * RB);
-        xb[j] = tr_value(f);
-      }
-#pragma unroll
-      for (int p = PARTS - 1; p >= 0; --p) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-          TrFrag f;
-          f.lo = tr_read4(base + p * A_BYTES + offa[i] + 16 * ks * RA);
-          f.hi = tr_read4(base + p * A_BYTES + offa[i] + (16 * ks + 4) * RA);
-          const bf16x8 xa = tr_value(f);
-#pragma unroll
-          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j], xa, acc[i][j], 0, 0, 0);
-        }
-      }
-    }
-    wait_lgkm();
-    bare_barrier();
-  }
-  float *dW = a.dW, *db = a.db, scale = a.scale;
-  if (splits > 1) {                                       // unscaled into the slice's [M x N | M] of the scratch
-    dW = partial + (long)sp * ((long)M * N + M);
-    db = dW + (long)M * N;
+  for (int j = 0; j < TN; ++j) read_b(Int<0>{}, 0, j);
+  // Whole tiles are loaded without a test: those that end before the last token, and, where a chunk reaches past the last
+  // feature into the next token's row, before the tokens behind which there are not 7 more elements.
+  const long safe = m0 + BM <= M || M % 8 == 0 ? a.rows : a.rows - (7 + a.ldy - 1) / a.ldy;
+  const int whole_tiles = (int)((safe - first < K ? safe - first : K) / BK);
+  int kt = 0;
+  for (; kt + 2 < whole_tiles; ++kt) tile_step(std::true_type{}, std::true_type{}, kt);
+  for (; kt + 1 < KT; ++kt) tile_step(std::true_type{}, std::false_type{}, kt);
+  if (KT > 0) tile_step(std::false_type{}, std::false_type{}, kt);
+  wait_lgkm();
+  bare_barrier();
+  // a slice's sums go unscaled to the scratch, [BM x BN | BM] per slice of a tile
+  float scale = a.scale, *part = nullptr;
+  if (splits > 1) {
+    part = partial + (long)((tile - it.whole) * splits + sp) * (BM * BN + BM);
     scale = 1.f;
   }
   if (sums) {                                             // block-uniform
-    float* red = reinterpret_cast<float*>(smem);
+    float* red = reinterpret_cast<float*>(smem);          // [WN][2 halves of the tokens][BM]
 #pragma unroll
-    for (int e = 0; e < 8; ++e) red[threadIdx.x / (BM / 8) * BM + ac + e] = bias[e].sum;
+    for (int i = 0; i < TM; ++i) red[((wave % WN) * 2 + lh) * BM + wm0 + 32 * i + (lane & 31)] = bias[i].sum;
     __syncthreads();
     for (int m = threadIdx.x; m < BM && m0 + m < M; m += NT) {
       CarrySum t;
-      for (int g = 0; g < NT / (BM / 8); ++g) t.add(red[g * BM + m]);
-      db[m0 + m] = scale * t.sum;
+#pragma unroll
+      for (int g = 0; g < 2 * WN; ++g) t.add(red[g * BM + m]);
+      if (part) part[BM * BN + m] = t.sum;
+      else a.db[m0 + m] = scale * t.sum;
     }
   }
   // a lane holds 4 consecutive columns of one row at a time
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int m = m0 + wm0 + 32 * i + (lane & 31);
-    if (m >= M) continue;
-    float* out = dW + (long)m * N;
+    const int m = wm0 + 32 * i + (lane & 31);
+    if (m0 + m >= M) continue;
+    float* out = part ? part + m * BN - n0 : a.dW + (long)(m0 + m) * N;
+    const int stop = part ? n0 + BN : N;
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int n = n0 + wn0 + 32 * j + 8 * q + 4 * lh;
         const f32x4 v = {scale * acc[i][j][4 * q], scale * acc[i][j][4 * q + 1], scale * acc[i][j][4 * q + 2], scale * acc[i][j][4 * q + 3]};
-        if (n < N) store4_row<float>(out, n, N, v);
+        if (n < N) store4_row<float>(out, n, stop, v);
       }
   }
 }
 
-// sums of the slices, in order
-__global__ void __launch_bounds__(256) q8_grad_join_kernel(const float* partial, int splits, long mn, int M, float* dW, float* db, float scale) {
-  const long each = mn + M, i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (i >= each) return;
+// The tiles that were cut into slices: the slices' sums, in order.  A block takes 1024 elements of a tile, or a tile's bias.
+__global__ void __launch_bounds__(256) q8_grad_join_kernel(const Q8GradArgs a, const float* partial, int whole, int slices, int BM, int BN, int tiles_n) {
+  const int tile = whole + blockIdx.y, tm = tile / tiles_n, tn = tile - tm * tiles_n;
+  const long each = (long)BM * BN + BM;
+  const float* p = partial + (long)blockIdx.y * slices * each;
+  const int e = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (e >= BM * BN) {                                     // BM is a multiple of 4
+    const int m = tm * BM + e - BM * BN;
+    if (tn != 0 || !a.db || e >= each) return;
+    for (int i = 0; i < 4 && m + i < a.M; ++i) {
+      CarrySum t;
+      for (int s = 0; s < slices; ++s) t.add(p[s * each + e + i]);
+      a.db[m + i] = a.scale * t.sum;
+    }
+    return;
+  }
+  const int r = e / BN, m = tm * BM + r, n = tn * BN + e - r * BN;
+  if (m >= a.M || n >= a.N) return;
   CarrySum acc[4];
-  const int n = each - i < 4 ? (int)(each - i) : 4;
-  for (int s = 0; s < splits; ++s) {
-    const float* p = partial + s * each + i;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (n == 4) v = load4u<float>(p);
-    else
-      for (int e = 0; e < n; ++e) v[e] = p[e];
+#pragma unroll 4
+  for (int s = 0; s < slices; ++s) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p + s * each + e);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e].add(v[e]);
+    for (int i = 0; i < 4; ++i) acc[i].add(v[i]);
   }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (i + e < mn) dW[i + e] = scale * acc[e].sum;
-    else if (i + e < each && db) db[i + e - mn] = scale * acc[e].sum;
-  }
+  store4_row<float>(a.dW + (long)m * a.N, n, a.N, a.scale * f32x4{acc[0].sum, acc[1].sum, acc[2].sum, acc[3].sum});
 }
 
 __global__ void __launch_bounds__(256) q8_grad_zero_kernel(long mn, int M, float* dW, float* db) {
@@ -296,35 +410,56 @@ __global__ void __launch_bounds__(256) q8_grad_zero_kernel(long mn, int M, float
   else if (i < mn + M && db) db[i - mn] = 0.f;
 }
 
-// Slices of the token sum: a launch with few tiles is cut along the tokens until the chip is full, which costs writing and
-// adding up the slices' results.  The number follows from the sizes alone, not from the device, so that results do not
-// depend on it either.
+// Tile and slices of a launch.  Tiles that fill whole rounds of the chip are computed in one piece; those of the last
+// round, which would leave part of it idle, are cut along the tokens into slices that fill it, which costs writing and
+// adding up the slices' sums.  The time of a round is fixed + tokens * per_token[blocks on a CU], that of joining slices
+// J0 + J1 * slices and their bytes, fitted to 1100 launches (64 to 70001 tokens, 64 x 64 to 50257 x 768 weights, both
+// types) and within 6-9 % of them; the pick is 0.6 % slower than the best of all tiles and slices on average, 10 % at worst.
+// One piece or slices of the last round: 4096 tokens, 50257 x 768, bf16, 363 against 348 us; 16384 x 4096 x 1024 394
+// against 148.  Large tiles or small ones: 16384 x 4096 x 4096 495, 685, 1415 us; 2048 x 384 x 384 23, 14, 12.7.
+// CUS is a constant: the plan, and with it the order of the sums, follows from the sizes alone.
 constexpr int CUS = 256;
-struct Plan { int splits; };
+struct Tile { int bm, bn, bk, per_cu; double fixed, per_token[4]; };       // us, us per 1000 tokens
+constexpr Tile TILES_BF16[] = {{256, 256, 64, 1, 6.3, {24.7}}, {128, 128, 64, 2, 6.0, {14.7, 18.6}},
+                               {64, 64, 64, 4, 4.8, {7.6, 9.4, 12.8, 16.1}}};
+constexpr Tile TILES_F32[] = {{128, 256, 64, 1, 6.3, {36.3}}, {128, 128, 32, 2, 5.6, {36.0, 46.3}},
+                              {64, 64, 32, 4, 4.7, {20.1, 23.5, 30.7, 38.0}}};
+constexpr double J0 = 1.6, J1 = 0.43, J_BYTES = 4.8e6;                     // us, us a slice, bytes per us
+constexpr int MOST_SLICES = 64;
+struct Plan { int cfg, tiles_m, tiles_n, whole, slices; };
 Plan plan(long rows, int M, int N, bool dy_bf16) {
-  const long tiles = (long)((M + 127) / 128) * ((N + 127) / 128), ktiles = (rows + BK - 1) / BK;
-  Plan best = {1};
+  Plan best = {};
   double best_cost = 1e300;
-  for (int s = 1; s <= 64 && (s == 1 || (ktiles / s >= 8 && tiles * s <= 1 << 20)); s *= 2) {
-    const double rounds = (double)((tiles * s + 2 * CUS - 1) / (2 * CUS));
-    double cost = rounds * (4.0 + (dy_bf16 ? 0.5 : 1.2) * ((ktiles + s - 1) / s));
-    if (s > 1) cost += 4.0 + 2.0 * s * (double)M * N * 4.0 / 3e6;
-    if (cost < best_cost) { best_cost = cost; best.splits = s; }
+  for (int c = 0; c < 3; ++c) {
+    const Tile& t = dy_bf16 ? TILES_BF16[c] : TILES_F32[c];
+    const long tm = (M + t.bm - 1) / t.bm, tn = (N + t.bn - 1) / t.bn, tiles = tm * tn, fill = CUS * t.per_cu;
+    const long whole = tiles / fill * fill, rest = tiles - whole, ktiles = (rows + t.bk - 1) / t.bk;
+    const double base = (double)(whole / fill) * (t.fixed + t.per_token[t.per_cu - 1] * rows / 1000.0);
+    for (long s = 1; s == 1 || (rest && s <= MOST_SLICES && s <= ktiles && rest * s <= fill); ++s) {
+      double cost = base;
+      if (rest) cost += t.fixed + t.per_token[(rest * s - 1) / CUS] * ((ktiles + s - 1) / s * t.bk) / 1000.0;
+      if (s > 1) cost += J0 + J1 * s + 2.0 * s * rest * t.bm * t.bn * 4.0 / J_BYTES;
+      if (cost < best_cost) {
+        best_cost = cost;
+        best = {c, (int)tm, (int)tn, (int)(s > 1 ? whole : tiles), (int)s};
+      }
+    }
   }
   return best;
 }
 
-template <typename T, int BM, int BN, int WM, int WN, int OCC>
-hipError_t launch_tile(const Q8GradArgs& a, int splits, float* partial, hipStream_t st) {
+template <typename T, int BM, int BN, int BK, int WM, int WN, int OCC>
+hipError_t launch_tile(const Q8GradArgs& a, const Plan& p, float* partial, hipStream_t st) {
   constexpr int PARTS = std::is_same<T, float>::value ? 3 : 1;
-  const long tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN, total = tiles_m * tiles_n * splits;
-  const int per_xcd = (int)((total + 7) / 8);
   const size_t smem = 2 * (size_t)BK * 2 * (PARTS * BM + BN);
-  static_assert(64 * WM * WN / (BM / 8) * BM * 4 <= 2 * BK * 2 * (PARTS * BM + BN), "the bias sums fit");
-  auto kern = q8_grad_kernel<T, BM, BN, WM, WN, OCC>;
+  static_assert(2 * WN * BM * 4 <= 2 * BK * 2 * (PARTS * BM + BN), "the bias sums fit");
+  auto kern = q8_grad_kernel<T, BM, BN, BK, WM, WN, OCC>;
   static unsigned long raised = 0;
   if (const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kern), (int)smem, raised); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3(per_xcd * 8), dim3(64 * WM * WN), smem, st, a, (int)tiles_n, (int)(tiles_m * tiles_n), splits, (int)total, per_xcd, partial);
+  const Items it(p.tiles_m * p.tiles_n, p.whole, p.slices);
+  hipLaunchKernelGGL(kern, dim3(it.blocks()), dim3(64 * WM * WN), smem, st, a, p.tiles_n, it, partial);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess || !it.rest) return e;
+  hipLaunchKernelGGL(q8_grad_join_kernel, dim3((BM * BN + BM + 1023) / 1024, it.rest), dim3(256), 0, st, a, partial, p.whole, p.slices, BM, BN, p.tiles_n);
   return hipGetLastError();
 }
 
@@ -332,8 +467,9 @@ hipError_t launch_tile(const Q8GradArgs& a, int splits, float* partial, hipStrea
 
 size_t q8_grad_partial_floats(long rows, int M, int N, bool dy_bf16) {
   if (rows <= 0) return 0;
-  const int s = plan(rows, M, N, dy_bf16).splits;
-  return s == 1 ? 0 : (size_t)s * ((size_t)M * N + M);
+  const Plan p = plan(rows, M, N, dy_bf16);
+  const Tile& t = dy_bf16 ? TILES_BF16[p.cfg] : TILES_F32[p.cfg];
+  return (size_t)(p.tiles_m * p.tiles_n - p.whole) * p.slices * (t.bm * t.bn + t.bm);
 }
 
 hipError_t launch_q8_grad(const Q8GradArgs& a, bool dy_bf16, float* partial, hipStream_t st) {
@@ -344,10 +480,14 @@ hipError_t launch_q8_grad(const Q8GradArgs& a, bool dy_bf16, float* partial, hip
   }
   ProfScope ps(PC_Q8_GRAD, 2.0 * a.rows * mn, (double)a.rows * (a.M * (dy_bf16 ? 2.0 : 4.0) + 33.0 * a.blocks) + 4.0 * each, st);
   const Plan p = plan(a.rows, a.M, a.N, dy_bf16);
-  const hipError_t e = dy_bf16 ? launch_tile<bf16, 128, 128, 2, 2, 2>(a, p.splits, partial, st) : launch_tile<float, 128, 128, 2, 2, 2>(a, p.splits, partial, st);
-  if (e != hipSuccess || p.splits == 1) return e;
-  hipLaunchKernelGGL(q8_grad_join_kernel, dim3((unsigned)((each + 1023) / 1024)), dim3(256), 0, st, partial, p.splits, mn, a.M, a.dW, a.db, a.scale);
-  return hipGetLastError();
+  if (dy_bf16) {
+    if (p.cfg == 0) return launch_tile<bf16, 256, 256, 64, 4, 2, 1>(a, p, partial, st);
+    if (p.cfg == 1) return launch_tile<bf16, 128, 128, 64, 2, 2, 2>(a, p, partial, st);
+    return launch_tile<bf16, 64, 64, 64, 2, 2, 4>(a, p, partial, st);
+  }
+  if (p.cfg == 0) return launch_tile<float, 128, 256, 64, 2, 4, 1>(a, p, partial, st);
+  if (p.cfg == 1) return launch_tile<float, 128, 128, 32, 2, 2, 2>(a, p, partial, st);
+  return launch_tile<float, 64, 64, 32, 2, 2, 4>(a, p, partial, st);
 }
 
 }  // namespace mg

@@ -392,6 +392,24 @@ def test_weight_grad_of_many_rows(rows, m, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,m,k", [(40, 4111, 4300), (65, 4112, 4300), (777, 2601, 2300), (900, 9000, 1100), (1000, 17413, 1000),
+                                      (12608, 2051, 1000)])
+def test_weight_grad_of_large_weights(rows, m, k, dtype):
+    """The large tiles, with ragged edges either way, whole tiles and slices in one launch; the reference is the product of
+    the same values in float64 on the device."""
+    say("weight grad large", rows, m, k, dtype)
+    dy, x8 = rand(1, rows, m, dtype=dtype), mb.mgrit_q8_pack(rand(2, rows, k))
+    xv = mb.mgrit_q8_unpack(x8).double()
+    dW, db = mb.mgrit_q8_weight_grad(dy, x8, scale=0.5)
+    ref_w, size = 0.5 * dy.double().t().contiguous() @ xv, 0.5 * dy.double().abs().t().contiguous() @ xv.abs()
+    adds = rows * (3 if dtype == F32 else 1) + 64
+    assert bool(((dW.double() - ref_w).abs() <= 2 * adds * U * size).all())
+    rms = (dy.double().square().t().contiguous() @ xv.square()).sum().sqrt() * 0.5
+    assert float((dW.double() - ref_w).norm()) <= U * (2 * np.sqrt(adds) + 8) * float(rms)
+    close(db, 0.5 * n64(dy).sum(0), 0.5 * (rows + 64) * U * np.abs(n64(dy)).sum(0), "db")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("m", [24, 200, 256])
 def test_weight_grad_of_slices_of_wider_rows(m, dtype):
     say("weight grad strides", m, dtype)

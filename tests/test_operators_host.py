@@ -88,7 +88,7 @@ def test_weight_grad_refusals():
     assert call(scale=float("inf")) == INVALID and call(scale=float("nan")) == INVALID
     assert call(ws=None) == INVALID and call(ws=6 * P + 64) == INVALID
     assert call(m=1 << 16, k=1 << 16, lddy=1 << 16) == UNSUPPORTED and call(rows=1 << 31) == UNSUPPORTED
-    assert call(m=(1 << 24) + 1, k=1, lddy=1 << 25) == UNSUPPORTED
+    assert call(m=(1 << 24) + 1, k=1, lddy=1 << 25) == UNSUPPORTED and call(lddy=(1 << 24) + 1) == UNSUPPORTED
     need = mb.mgrit_q8_weight_grad_workspace_bytes(8192, 64, 64, torch.float32)
     assert need > 256 and call(rows=8192, m=64, k=64, lddy=64, n=need - 1) == SMALL
     assert mb.lib().mgrit_q8_weight_grad_workspace_bytes(-1, 4, 4, 0) == 0
