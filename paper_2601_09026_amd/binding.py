@@ -468,9 +468,9 @@ def mgrit_adjoint(desc: ModelDesc, opts: Opts, Z_all, theta: List[torch.Tensor],
     if q8:
         if linearised:
             raise ValueError("linearised: the adjoint of that pair takes Z_all as the forward call left it")
-        if tuple(Z_all.shape) != (opts.N + 1, T, d):
+        if Z_all.shape != (opts.N + 1, T, d):
             raise ValueError(f"Z_all: expected 8-bit rows of shape {(opts.N + 1, T, d)}, got {tuple(Z_all.shape)}")
-        _check_q8(Z_all, "Z_all", _current_device())
+        _check_q8(Z_all, "Z_all", _device_of(Z_all.q, "Z_all"))
     else:
         _check_state(Z_all, (opts.N + 1, T, d), "Z_all")
     _check_state(lambda_N, (T, d), "lambda_N")
@@ -698,8 +698,8 @@ def mgrit_adjoint_stacked(desc: ModelDesc, opts: Opts, n_enc: int, Z_all: torch.
 
 
 # ---- operators around the solves: 8-bit rows, LayerNorm of rows, gradients from 8-bit rows ------------
+# (Small calls take as long as the host needs for them: what is asked of tensors below is what costs least.)
 Q8_BLOCK = 32                        # MGRIT_Q8_BLOCK of the header
-NORM_MOST_COLS = 16384
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -710,8 +710,9 @@ class Q8Rows:
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor, cols: int):
         blocks = (int(cols) + Q8_BLOCK - 1) // Q8_BLOCK
-        if (cols < 1 or q.dtype != torch.int8 or scale.dtype != torch.uint8 or q.dim() < 1
-                or q.shape != (*scale.shape[:-1], blocks * Q8_BLOCK) or scale.shape[-1:] != (blocks,)):
+        lead = scale.shape[:-1]
+        if (cols < 1 or q.dtype != torch.int8 or scale.dtype != torch.uint8 or scale.dim() < 1
+                or q.shape != (*lead, blocks * Q8_BLOCK) or scale.shape != (*lead, blocks)):
             raise ValueError(f"8-bit rows of {cols} elements: expected int8 [..., {blocks * Q8_BLOCK}] and uint8 [..., "
                              f"{blocks}], got {q.dtype} {tuple(q.shape)} and {scale.dtype} {tuple(scale.shape)}")
         self.q, self.scale, self.cols = q, scale, int(cols)
@@ -736,95 +737,94 @@ class Q8Rows:
 
 def q8_empty(shape, device="cuda") -> Q8Rows:
     """Uninitialised 8-bit rows for a tensor of that shape."""
-    *lead, cols = (int(n) for n in shape)
+    *lead, cols = shape
     blocks = (cols + Q8_BLOCK - 1) // Q8_BLOCK
     return Q8Rows(torch.empty((*lead, blocks * Q8_BLOCK), dtype=torch.int8, device=device),
                   torch.empty((*lead, blocks), dtype=torch.uint8, device=device), cols)
 
 
-def _current_device() -> Optional[int]:
-    return torch.cuda.current_device() if torch.cuda.is_available() else None
+def _device_of(t: torch.Tensor, name: str) -> int:
+    """Index of a call's device: that of its first operand, which has to be the current one."""
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
+        raise ValueError(f"{name}: expected a tensor on the current device, got one on {t.device}")
+    return device
 
 
-def _check_device(t: torch.Tensor, name: str, device: Optional[int]):
-    if not t.is_cuda or t.device.index != device:
+def _check_device(t: torch.Tensor, name: str, device: int):
+    if t.get_device() != device:
         raise ValueError(f"{name}: expected a tensor on the current device, got one on {t.device}")
 
 
-def _check_q8(r: Q8Rows, name: str, device: Optional[int]):
+def _check_q8(r: Q8Rows, name: str, device: int, shape=None):
     _check_device(r.q, name, device)
     _check_device(r.scale, name, device)
     if not (r.q.is_contiguous() and r.scale.is_contiguous()):
         raise ValueError(f"{name}: expected contiguous 8-bit rows")
+    if shape is not None and (r.cols != shape[-1] or r.q.shape[:-1] != shape[:-1]):
+        raise ValueError(f"{name}: expected 8-bit rows of shape {tuple(shape)}, got {tuple(r.shape)}")
 
 
-def _check_rows(t: torch.Tensor, name: str, device: Optional[int], shape=None):
+def _check_rows(t: torch.Tensor, name: str, device: int, shape=None):
     """(rows, cols, stride) of a matrix argument: leading dimensions that lie one behind the other are rows."""
     _check_device(t, name, device)
-    if t.dtype not in _DTYPES or t.dim() < 1 or t.shape[-1] < 1 or (shape is not None and tuple(t.shape) != tuple(shape)):
+    own = t.shape
+    if t.dtype not in _DTYPES or len(own) < 1 or own[-1] < 1 or (shape is not None and own != shape):
         raise ValueError(f"{name}: expected fp32 or bf16 rows" + (f" of shape {tuple(shape)}" if shape is not None else "") +
-                         f", got {t.dtype} {tuple(t.shape)}")
-    cols = t.shape[-1]
+                         f", got {t.dtype} {tuple(own)}")
+    cols = own[-1]
     if t.is_contiguous():
         return t.numel() // cols, cols, cols
-    if t.dim() == 2 and t.stride(1) == 1 and (t.shape[0] == 1 or t.stride(0) >= cols):
-        return t.shape[0], cols, max(t.stride(0), cols)
+    if len(own) == 2 and t.stride(1) == 1 and (own[0] == 1 or t.stride(0) >= cols):
+        return own[0], cols, max(t.stride(0), cols)
     raise ValueError(f"{name}: expected contiguous rows, or a matrix of rows at one distance, got strides {t.stride()}")
 
 
-def _check_vector(t: Optional[torch.Tensor], n: int, name: str, device: Optional[int]):
+def _check_vector(t: Optional[torch.Tensor], n: int, name: str, device: int) -> Optional[int]:
+    """Address of a vector argument, None without."""
     if t is None:
-        return
+        return None
     _check_device(t, name, device)
-    if t.dtype != torch.float32 or tuple(t.shape) != (n,) or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous fp32 vector of {n}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
 
 
-class _On:
-    """Where a call runs: new tensors belong to the stream it is enqueued on, and the memory of tensors that were made on
-    another one is not handed out again before the call has run."""
-
-    def __init__(self, stream: Optional[torch.cuda.Stream]):
-        now = torch.cuda.current_stream()
-        self.stream = now if stream is None else stream
-        self.other = self.stream != now
-        self.context = torch.cuda.stream(self.stream) if self.other else None
-
-    def __enter__(self):
-        if self.other:
-            self.context.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self.other:
-            self.context.__exit__(*exc)
-        return False
-
-    def uses(self, *tensors):
-        if self.other:
-            for t in tensors:
-                for u in ((t.q, t.scale) if isinstance(t, Q8Rows) else (t,)):
-                    if u is not None:
-                        u.record_stream(self.stream)
-
-    @property
-    def handle(self):
-        return self.stream.cuda_stream
+def _on(stream: Optional[torch.cuda.Stream], device: int):
+    """(handle, stream if it is not the current one): where a call is enqueued."""
+    current = torch._C._cuda_getCurrentRawStream(device)
+    if stream is None or stream.cuda_stream == current:
+        return current, None
+    return stream.cuda_stream, stream
 
 
-def _call(name: str, *args):
-    st = getattr(lib(), name)(*args)
-    if st != MGRIT_OK:
-        raise MgritError(st, name)
+def _new(shape, dtype: torch.dtype, device: torch.device, other: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A new tensor that belongs to the stream its call is enqueued on."""
+    if other is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(other):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _at(t) -> Optional[int]:
-    return None if t is None else t.data_ptr()
+def _new_q8(shape, device: torch.device, other: Optional[torch.cuda.Stream]) -> Q8Rows:
+    if other is None:
+        return q8_empty(shape, device)
+    with torch.cuda.stream(other):
+        return q8_empty(shape, device)
 
 
-def _workspace(given: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+def _in_use(other: Optional[torch.cuda.Stream], *operands):
+    """After a call on another stream than the current one: the operands' memory is not handed out again before it ran."""
+    if other is not None:
+        for t in operands:
+            for u in ((t.q, t.scale) if isinstance(t, Q8Rows) else (t,)):
+                if u is not None:
+                    u.record_stream(other)
+
+
+def _workspace(given: Optional[torch.Tensor], need: int, device: torch.device, other) -> torch.Tensor:
     if given is None:
-        return torch.empty(need, dtype=torch.uint8, device=device)
+        return _new(need, torch.uint8, device, other)
     if given.dtype != torch.uint8 or not given.is_contiguous() or given.device != device:
         raise ValueError("workspace: expected a contiguous uint8 tensor on the operands' device")
     return given
@@ -836,32 +836,38 @@ def mgrit_q8_blocks(cols: int) -> int:
 
 def mgrit_q8_pack(x: torch.Tensor, out: Optional[Q8Rows] = None, stream: Optional[torch.cuda.Stream] = None) -> Q8Rows:
     """The 8-bit rows of x (fp32 or bf16, [..., cols])."""
-    device = _current_device()
+    device = _device_of(x, "x")
     rows, cols, stride = _check_rows(x, "x", device)
-    with _On(stream) as on:
-        if out is None:
-            out = q8_empty(x.shape, x.device)
-        _check_q8(out, "out", device)
-        if out.shape != x.shape:
-            raise ValueError(f"out: expected 8-bit rows of shape {tuple(x.shape)}, got {tuple(out.shape)}")
-        _call("mgrit_q8_pack", rows, cols, _DTYPES[x.dtype], x.data_ptr(), stride, _at(out.q), _at(out.scale), on.handle)
-        on.uses(x, out)
+    handle, other = _on(stream, device)
+    if out is None:
+        out = _new_q8(x.shape, x.device, other)
+    else:
+        _check_q8(out, "out", device, x.shape)
+    st = lib().mgrit_q8_pack(rows, cols, _DTYPES[x.dtype], x.data_ptr(), stride, out.q.data_ptr(), out.scale.data_ptr(), handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_q8_pack")
+    _in_use(other, x, out)
     return out
 
 
 def mgrit_q8_unpack(x: Q8Rows, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """What 8-bit rows stand for, as fp32 or bf16 (exactly, in either)."""
-    device = _current_device()
+    device = _device_of(x.q, "x")
     _check_q8(x, "x", device)
-    with _On(stream) as on:
-        if out is None:
-            if dtype not in _DTYPES:
-                raise ValueError(f"dtype: expected float32 or bfloat16, got {dtype}")
-            out = torch.empty(x.shape, dtype=dtype, device=x.device)
+    handle, other = _on(stream, device)
+    if out is None:
+        if dtype not in _DTYPES:
+            raise ValueError(f"dtype: expected float32 or bfloat16, got {dtype}")
+        out = _new(x.shape, dtype, x.device, other)
+        rows, cols = x.rows, x.cols
+        stride = cols
+    else:
         rows, cols, stride = _check_rows(out, "out", device, x.shape)
-        _call("mgrit_q8_unpack", rows, cols, _DTYPES[out.dtype], _at(x.q), _at(x.scale), out.data_ptr(), stride, on.handle)
-        on.uses(x, out)
+    st = lib().mgrit_q8_unpack(rows, cols, _DTYPES[out.dtype], x.q.data_ptr(), x.scale.data_ptr(), out.data_ptr(), stride, handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_q8_unpack")
+    _in_use(other, x, out)
     return out
 
 
@@ -872,35 +878,40 @@ def mgrit_layer_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = No
                              stream: Optional[torch.cuda.Stream] = None):
     """Returns (y, mean, rstd): LayerNorm of the rows of x (fp32 or bf16, [..., cols]) with y of y_dtype (x's own by
     default) and the rows' statistics, fp32 [rows].  x_q8, y_q8: 8-bit rows (q8_empty) filled from the same pass."""
-    device = _current_device()
+    device = _device_of(x, "x")
     rows, cols, ldx = _check_rows(x, "x", device)
-    _check_vector(gamma, cols, "gamma", device)
-    _check_vector(beta, cols, "beta", device)
-    for t, name in ((x_q8, "x_q8"), (y_q8, "y_q8")):
-        if t is not None:
-            _check_q8(t, name, device)
-            if t.shape != x.shape:
-                raise ValueError(f"{name}: expected 8-bit rows of shape {tuple(x.shape)}, got {tuple(t.shape)}")
-    with _On(stream) as on:
-        if y is None:
-            y = torch.empty(x.shape, dtype=x.dtype if y_dtype is None else y_dtype, device=x.device)
+    handle, other = _on(stream, device)
+    if y is None:
+        y_dtype = x.dtype if y_dtype is None else y_dtype
+        if y_dtype not in _DTYPES:
+            raise ValueError(f"y_dtype: expected float32 or bfloat16, got {y_dtype}")
+        y, ldy = _new(x.shape, y_dtype, x.device, other), cols
+    else:
         _, _, ldy = _check_rows(y, "y", device, x.shape)
-        if mean is None:
-            mean = torch.empty(rows, dtype=torch.float32, device=x.device)
-        if rstd is None:
-            rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-        _check_vector(mean, rows, "mean", device)
-        _check_vector(rstd, rows, "rstd", device)
-        desc = NormDesc(rows, cols, _DTYPES[x.dtype], _DTYPES[y.dtype], eps)
-        _call("mgrit_layer_norm_forward", C.byref(desc), x.data_ptr(), ldx, _at(gamma), _at(beta), y.data_ptr(), ldy,
-              mean.data_ptr(), rstd.data_ptr(), *(_at(p) for t in (x_q8, y_q8) for p in ((t.q, t.scale) if t else (None, None))),
-              on.handle)
-        on.uses(x, gamma, beta, y, mean, rstd, x_q8, y_q8)
+        if y_dtype is not None and y_dtype != y.dtype:
+            raise ValueError(f"y: expected {y_dtype}, got {y.dtype}")
+    if mean is None:
+        mean = _new(rows, torch.float32, x.device, other)
+    if rstd is None:
+        rstd = _new(rows, torch.float32, x.device, other)
+    copies = [None] * 4
+    for k, (t, name) in enumerate(((x_q8, "x_q8"), (y_q8, "y_q8"))):
+        if t is not None:
+            _check_q8(t, name, device, x.shape)
+            copies[2 * k:2 * k + 2] = t.q.data_ptr(), t.scale.data_ptr()
+    desc = NormDesc(rows, cols, _DTYPES[x.dtype], _DTYPES[y.dtype], eps)
+    st = lib().mgrit_layer_norm_forward(desc, x.data_ptr(), ldx, _check_vector(gamma, cols, "gamma", device),
+                                        _check_vector(beta, cols, "beta", device), y.data_ptr(), ldy,
+                                        _check_vector(mean, rows, "mean", device), _check_vector(rstd, rows, "rstd", device),
+                                        *copies, handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_layer_norm_forward")
+    _in_use(other, x, gamma, beta, y, mean, rstd, x_q8, y_q8)
     return y, mean, rstd
 
 
 def mgrit_layer_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
-    return int(lib().mgrit_layer_norm_backward_workspace_bytes(C.byref(NormDesc(rows, cols, 0, 0, 1e-5))))
+    return int(lib().mgrit_layer_norm_backward_workspace_bytes(NormDesc(rows, cols, 0, 0, 1e-5)))
 
 
 def mgrit_layer_norm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
@@ -909,38 +920,37 @@ def mgrit_layer_norm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor]
                               workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Returns (dx, dgamma, dbeta) of mgrit_layer_norm_forward for the cotangent dy.  x: its input, or the Q8Rows kept of
     it; mean, rstd: as it returned them.  dx has x's type (8-bit rows: dx_dtype, fp32 by default)."""
-    device = _current_device()
-    rows, cols, lddy = _check_rows(dy, "dy", device, x.shape)
-    q8 = x if isinstance(x, Q8Rows) else None
-    if q8 is not None:
-        _check_q8(q8, "x", device)
-        x_at, ldx, x_dtype = None, 0, torch.float32 if dx_dtype is None else dx_dtype
+    device = _device_of(dy, "dy")
+    rows, cols, lddy = _check_rows(dy, "dy", device)
+    if isinstance(x, Q8Rows):
+        _check_q8(x, "x", device, dy.shape)
+        x_at, ldx, xq, xs = None, 0, x.q.data_ptr(), x.scale.data_ptr()
+        x_dtype = torch.float32 if dx_dtype is None else dx_dtype
     else:
-        _, _, ldx = _check_rows(x, "x", device)
-        x_at, x_dtype = x.data_ptr(), x.dtype
+        _, _, ldx = _check_rows(x, "x", device, dy.shape)
+        x_at, xq, xs, x_dtype = x.data_ptr(), None, None, x.dtype
     if x_dtype not in _DTYPES or (dx_dtype is not None and dx_dtype != x_dtype):
         raise ValueError(f"dx_dtype: dx has the type of x, float32 or bfloat16, got {dx_dtype}")
-    _check_vector(gamma, cols, "gamma", device)
-    _check_vector(mean, rows, "mean", device)
-    _check_vector(rstd, rows, "rstd", device)
-    with _On(stream) as on:
-        if dx is None:
-            dx = torch.empty(dy.shape, dtype=x_dtype, device=dy.device)
+    handle, other = _on(stream, device)
+    if dx is None:
+        dx, lddx = _new(dy.shape, x_dtype, dy.device, other), cols
+    else:
         _, _, lddx = _check_rows(dx, "dx", device, dy.shape)
         if dx.dtype != x_dtype:
             raise ValueError(f"dx: expected {x_dtype}, got {dx.dtype}")
-        if dgamma is None:
-            dgamma = torch.empty(cols, dtype=torch.float32, device=dy.device)
-        if dbeta is None:
-            dbeta = torch.empty(cols, dtype=torch.float32, device=dy.device)
-        _check_vector(dgamma, cols, "dgamma", device)
-        _check_vector(dbeta, cols, "dbeta", device)
-        desc = NormDesc(rows, cols, _DTYPES[x_dtype], _DTYPES[dy.dtype], 1e-5)
-        ws = _workspace(workspace, int(lib().mgrit_layer_norm_backward_workspace_bytes(C.byref(desc))), dy.device)
-        _call("mgrit_layer_norm_backward", C.byref(desc), dy.data_ptr(), lddy, x_at, ldx, _at(q8.q if q8 else None),
-              _at(q8.scale if q8 else None), _at(gamma), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), lddx,
-              dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), ws.numel(), on.handle)
-        on.uses(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws)
+    if dgamma is None:
+        dgamma = _new(cols, torch.float32, dy.device, other)
+    if dbeta is None:
+        dbeta = _new(cols, torch.float32, dy.device, other)
+    desc, L = NormDesc(rows, cols, _DTYPES[x_dtype], _DTYPES[dy.dtype], 1e-5), lib()
+    ws = _workspace(workspace, L.mgrit_layer_norm_backward_workspace_bytes(desc), dy.device, other)
+    st = L.mgrit_layer_norm_backward(desc, dy.data_ptr(), lddy, x_at, ldx, xq, xs, _check_vector(gamma, cols, "gamma", device),
+                                     _check_vector(mean, rows, "mean", device), _check_vector(rstd, rows, "rstd", device),
+                                     dx.data_ptr(), lddx, _check_vector(dgamma, cols, "dgamma", device),
+                                     _check_vector(dbeta, cols, "dbeta", device), ws.data_ptr(), ws.numel(), handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_layer_norm_backward")
+    _in_use(other, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws)
     return dx, dgamma, dbeta
 
 
@@ -953,22 +963,23 @@ def mgrit_q8_weight_grad(dy: torch.Tensor, x: Q8Rows, scale: float = 1.0, dW: Op
                          stream: Optional[torch.cuda.Stream] = None):
     """Returns (dW [out_features, in_features], db [out_features]), fp32, of a linear map whose input rows were kept as x:
     dW = scale * dy^T x, db = scale * the sum of dy's rows.  dy: fp32 or bf16, [..., out_features]."""
-    device = _current_device()
-    _check_q8(x, "x", device)
+    device = _device_of(dy, "dy")
     rows, m, ldy = _check_rows(dy, "dy", device)
-    if dy.shape[:-1] != x.shape[:-1]:
-        raise ValueError(f"dy: expected {tuple(x.shape[:-1])} rows as x, got {tuple(dy.shape[:-1])}")
-    with _On(stream) as on:
-        if dW is None:
-            dW = torch.empty((m, x.cols), dtype=torch.float32, device=dy.device)
+    _check_q8(x, "x", device, (*dy.shape[:-1], x.cols))
+    handle, other = _on(stream, device)
+    if dW is None:
+        dW = _new((m, x.cols), torch.float32, dy.device, other)
+    else:
         _check_device(dW, "dW", device)
-        if dW.dtype != torch.float32 or tuple(dW.shape) != (m, x.cols) or not dW.is_contiguous():
+        if dW.dtype != torch.float32 or dW.shape != (m, x.cols) or not dW.is_contiguous():
             raise ValueError(f"dW: expected a contiguous fp32 matrix of shape {(m, x.cols)}, got {dW.dtype} {tuple(dW.shape)}")
-        if db is None:
-            db = torch.empty(m, dtype=torch.float32, device=dy.device)
-        _check_vector(db, m, "db", device)
-        ws = _workspace(workspace, mgrit_q8_weight_grad_workspace_bytes(rows, m, x.cols, dy.dtype), dy.device)
-        _call("mgrit_q8_weight_grad", rows, m, x.cols, _DTYPES[dy.dtype], dy.data_ptr(), ldy, _at(x.q), _at(x.scale),
-              float(scale), dW.data_ptr(), db.data_ptr(), ws.data_ptr(), ws.numel(), on.handle)
-        on.uses(dy, x, dW, db, ws)
+    if db is None:
+        db = _new(m, torch.float32, dy.device, other)
+    L, dtype = lib(), _DTYPES[dy.dtype]
+    ws = _workspace(workspace, L.mgrit_q8_weight_grad_workspace_bytes(rows, m, x.cols, dtype), dy.device, other)
+    st = L.mgrit_q8_weight_grad(rows, m, x.cols, dtype, dy.data_ptr(), ldy, x.q.data_ptr(), x.scale.data_ptr(), scale,
+                                dW.data_ptr(), _check_vector(db, m, "db", device), ws.data_ptr(), ws.numel(), handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_q8_weight_grad")
+    _in_use(other, dy, x, dW, db, ws)
     return dW, db
