@@ -405,8 +405,8 @@ int mgrit_layer_norm_forward(const mgrit_norm_desc* desc, const void* x, int64_t
  *   x or x_q8, x_q8_scale   one of the two forms of x (the other NULL); with 8-bit rows xhat is formed from what they
  *                           stand for and the forward pass's own mean and rstd
  *   dx, dgamma, dbeta       out, each may be NULL, not all; overwritten.  dx must be neither dy nor x and not overlap them.
- *   workspace               device, 256-byte aligned, mgrit_layer_norm_backward_workspace_bytes (host only, 0 on invalid
- *                           arguments); may be NULL if dgamma and dbeta are */
+ *   workspace               device, 256-byte aligned, mgrit_layer_norm_backward_workspace_bytes (host only; 0, also on
+ *                           invalid arguments: none is needed and it may be NULL, as without dgamma and dbeta) */
 size_t mgrit_layer_norm_backward_workspace_bytes(const mgrit_norm_desc* desc);
 int mgrit_layer_norm_backward(const mgrit_norm_desc* desc, const void* dy, int64_t dy_stride,
                               const void* x, int64_t x_stride, const void* x_q8, const void* x_q8_scale,
@@ -420,7 +420,8 @@ int mgrit_layer_norm_backward(const mgrit_norm_desc* desc, const void* dy, int64
  *   x_q8, x_q8_scale device, 8-bit rows of in_features elements
  * dW and db are fp32 and overwritten; products are exact and added up in fp32 (an fp32 dy is multiplied in full, not
  * rounded to bf16).  At most 2^24 features either way, dy_stride 2^24 and 2^31 weights (MGRIT_UNSUPPORTED beyond).
- * Workspace: 256-byte aligned, mgrit_q8_weight_grad_workspace_bytes (host only, 0 on invalid arguments). */
+ * Workspace: 256-byte aligned, mgrit_q8_weight_grad_workspace_bytes (host only; 0, also on invalid arguments: none is
+ * needed and it may be NULL). */
 size_t mgrit_q8_weight_grad_workspace_bytes(int64_t rows, int32_t out_features, int32_t in_features, int dy_dtype);
 int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features, int dy_dtype,
                          const void* dy, int64_t dy_stride, const void* x_q8, const void* x_q8_scale, float scale,

@@ -709,13 +709,20 @@ class Q8Rows:
     __slots__ = ("q", "scale", "cols")
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor, cols: int):
-        blocks = (int(cols) + Q8_BLOCK - 1) // Q8_BLOCK
-        lead = scale.shape[:-1]
-        if (cols < 1 or q.dtype != torch.int8 or scale.dtype != torch.uint8 or scale.dim() < 1
-                or q.shape != (*lead, blocks * Q8_BLOCK) or scale.shape != (*lead, blocks)):
+        blocks = (cols + Q8_BLOCK - 1) // Q8_BLOCK
+        at, kept = scale.shape, q.shape
+        if (cols < 1 or q.dtype is not torch.int8 or scale.dtype is not torch.uint8 or len(at) < 1 or len(kept) != len(at)
+                or at[-1] != blocks or kept[-1] != blocks * Q8_BLOCK or kept[:-1] != at[:-1]):
             raise ValueError(f"8-bit rows of {cols} elements: expected int8 [..., {blocks * Q8_BLOCK}] and uint8 [..., "
                              f"{blocks}], got {q.dtype} {tuple(q.shape)} and {scale.dtype} {tuple(scale.shape)}")
         self.q, self.scale, self.cols = q, scale, int(cols)
+
+    @classmethod
+    def _of(cls, q: torch.Tensor, scale: torch.Tensor, cols: int) -> "Q8Rows":
+        """Without the checks, for tensors made here."""
+        rows = object.__new__(cls)
+        rows.q, rows.scale, rows.cols = q, scale, cols
+        return rows
 
     @property
     def shape(self) -> torch.Size:
@@ -738,9 +745,11 @@ class Q8Rows:
 def q8_empty(shape, device="cuda") -> Q8Rows:
     """Uninitialised 8-bit rows for a tensor of that shape."""
     *lead, cols = shape
+    if cols < 1:
+        raise ValueError(f"8-bit rows: expected rows of at least one element, got {tuple(shape)}")
     blocks = (cols + Q8_BLOCK - 1) // Q8_BLOCK
-    return Q8Rows(torch.empty((*lead, blocks * Q8_BLOCK), dtype=torch.int8, device=device),
-                  torch.empty((*lead, blocks), dtype=torch.uint8, device=device), cols)
+    return Q8Rows._of(torch.empty((*lead, blocks * Q8_BLOCK), dtype=torch.int8, device=device),
+                      torch.empty((*lead, blocks), dtype=torch.uint8, device=device), cols)
 
 
 def _device_of(t: torch.Tensor, name: str) -> int:
@@ -757,11 +766,12 @@ def _check_device(t: torch.Tensor, name: str, device: int):
 
 
 def _check_q8(r: Q8Rows, name: str, device: int, shape=None):
-    _check_device(r.q, name, device)
-    _check_device(r.scale, name, device)
-    if not (r.q.is_contiguous() and r.scale.is_contiguous()):
+    q, scale = r.q, r.scale
+    if q.get_device() != device or scale.get_device() != device:
+        raise ValueError(f"{name}: expected tensors on the current device, got some on {q.device} and {scale.device}")
+    if not (q.is_contiguous() and scale.is_contiguous()):
         raise ValueError(f"{name}: expected contiguous 8-bit rows")
-    if shape is not None and (r.cols != shape[-1] or r.q.shape[:-1] != shape[:-1]):
+    if shape is not None and (r.cols != shape[-1] or q.shape[:-1] != shape[:-1]):
         raise ValueError(f"{name}: expected 8-bit rows of shape {tuple(shape)}, got {tuple(r.shape)}")
 
 
@@ -813,21 +823,30 @@ def _new_q8(shape, device: torch.device, other: Optional[torch.cuda.Stream]) -> 
         return q8_empty(shape, device)
 
 
-def _in_use(other: Optional[torch.cuda.Stream], *operands):
+def _in_use(other: torch.cuda.Stream, *operands):
     """After a call on another stream than the current one: the operands' memory is not handed out again before it ran."""
-    if other is not None:
-        for t in operands:
-            for u in ((t.q, t.scale) if isinstance(t, Q8Rows) else (t,)):
-                if u is not None:
-                    u.record_stream(other)
+    for t in operands:
+        for u in ((t.q, t.scale) if isinstance(t, Q8Rows) else (t,)):
+            if u is not None:
+                u.record_stream(other)
 
 
-def _workspace(given: Optional[torch.Tensor], need: int, device: torch.device, other) -> torch.Tensor:
+def _workspace(given: Optional[torch.Tensor], need: int, device: torch.device, other):
+    """(tensor, address, bytes): the caller's, or a new one if the call needs any."""
     if given is None:
-        return _new(need, torch.uint8, device, other)
+        given = _new(need, torch.uint8, device, other) if need else None
+        return given, given.data_ptr() if need else None, need
     if given.dtype != torch.uint8 or not given.is_contiguous() or given.device != device:
         raise ValueError("workspace: expected a contiguous uint8 tensor on the operands' device")
-    return given
+    return given, given.data_ptr(), given.numel()
+
+
+def _vector(given: Optional[torch.Tensor], n: int, name: str, device: int, like: torch.Tensor, other):
+    """(tensor, address): the caller's output vector, or a new one."""
+    if given is None:
+        given = _new(n, torch.float32, like.device, other)
+        return given, given.data_ptr()
+    return given, _check_vector(given, n, name, device)
 
 
 def mgrit_q8_blocks(cols: int) -> int:
@@ -846,7 +865,8 @@ def mgrit_q8_pack(x: torch.Tensor, out: Optional[Q8Rows] = None, stream: Optiona
     st = lib().mgrit_q8_pack(rows, cols, _DTYPES[x.dtype], x.data_ptr(), stride, out.q.data_ptr(), out.scale.data_ptr(), handle)
     if st != MGRIT_OK:
         raise MgritError(st, "mgrit_q8_pack")
-    _in_use(other, x, out)
+    if other is not None:
+        _in_use(other, x, out)
     return out
 
 
@@ -867,7 +887,8 @@ def mgrit_q8_unpack(x: Q8Rows, dtype: torch.dtype = torch.float32, out: Optional
     st = lib().mgrit_q8_unpack(rows, cols, _DTYPES[out.dtype], x.q.data_ptr(), x.scale.data_ptr(), out.data_ptr(), stride, handle)
     if st != MGRIT_OK:
         raise MgritError(st, "mgrit_q8_unpack")
-    _in_use(other, x, out)
+    if other is not None:
+        _in_use(other, x, out)
     return out
 
 
@@ -890,23 +911,23 @@ def mgrit_layer_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = No
         _, _, ldy = _check_rows(y, "y", device, x.shape)
         if y_dtype is not None and y_dtype != y.dtype:
             raise ValueError(f"y: expected {y_dtype}, got {y.dtype}")
-    if mean is None:
-        mean = _new(rows, torch.float32, x.device, other)
-    if rstd is None:
-        rstd = _new(rows, torch.float32, x.device, other)
-    copies = [None] * 4
-    for k, (t, name) in enumerate(((x_q8, "x_q8"), (y_q8, "y_q8"))):
-        if t is not None:
-            _check_q8(t, name, device, x.shape)
-            copies[2 * k:2 * k + 2] = t.q.data_ptr(), t.scale.data_ptr()
+    mean, mean_at = _vector(mean, rows, "mean", device, x, other)
+    rstd, rstd_at = _vector(rstd, rows, "rstd", device, x, other)
+    xq = xs = yq = ys = None
+    if x_q8 is not None:
+        _check_q8(x_q8, "x_q8", device, x.shape)
+        xq, xs = x_q8.q.data_ptr(), x_q8.scale.data_ptr()
+    if y_q8 is not None:
+        _check_q8(y_q8, "y_q8", device, x.shape)
+        yq, ys = y_q8.q.data_ptr(), y_q8.scale.data_ptr()
     desc = NormDesc(rows, cols, _DTYPES[x.dtype], _DTYPES[y.dtype], eps)
     st = lib().mgrit_layer_norm_forward(desc, x.data_ptr(), ldx, _check_vector(gamma, cols, "gamma", device),
                                         _check_vector(beta, cols, "beta", device), y.data_ptr(), ldy,
-                                        _check_vector(mean, rows, "mean", device), _check_vector(rstd, rows, "rstd", device),
-                                        *copies, handle)
+                                        mean_at, rstd_at, xq, xs, yq, ys, handle)
     if st != MGRIT_OK:
         raise MgritError(st, "mgrit_layer_norm_forward")
-    _in_use(other, x, gamma, beta, y, mean, rstd, x_q8, y_q8)
+    if other is not None:
+        _in_use(other, x, gamma, beta, y, mean, rstd, x_q8, y_q8)
     return y, mean, rstd
 
 
@@ -938,19 +959,17 @@ def mgrit_layer_norm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor]
         _, _, lddx = _check_rows(dx, "dx", device, dy.shape)
         if dx.dtype != x_dtype:
             raise ValueError(f"dx: expected {x_dtype}, got {dx.dtype}")
-    if dgamma is None:
-        dgamma = _new(cols, torch.float32, dy.device, other)
-    if dbeta is None:
-        dbeta = _new(cols, torch.float32, dy.device, other)
+    dgamma, dgamma_at = _vector(dgamma, cols, "dgamma", device, dy, other)
+    dbeta, dbeta_at = _vector(dbeta, cols, "dbeta", device, dy, other)
     desc, L = NormDesc(rows, cols, _DTYPES[x_dtype], _DTYPES[dy.dtype], 1e-5), lib()
-    ws = _workspace(workspace, L.mgrit_layer_norm_backward_workspace_bytes(desc), dy.device, other)
+    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_layer_norm_backward_workspace_bytes(desc), dy.device, other)
     st = L.mgrit_layer_norm_backward(desc, dy.data_ptr(), lddy, x_at, ldx, xq, xs, _check_vector(gamma, cols, "gamma", device),
                                      _check_vector(mean, rows, "mean", device), _check_vector(rstd, rows, "rstd", device),
-                                     dx.data_ptr(), lddx, _check_vector(dgamma, cols, "dgamma", device),
-                                     _check_vector(dbeta, cols, "dbeta", device), ws.data_ptr(), ws.numel(), handle)
+                                     dx.data_ptr(), lddx, dgamma_at, dbeta_at, ws_at, ws_bytes, handle)
     if st != MGRIT_OK:
         raise MgritError(st, "mgrit_layer_norm_backward")
-    _in_use(other, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws)
+    if other is not None:
+        _in_use(other, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws)
     return dx, dgamma, dbeta
 
 
@@ -973,13 +992,14 @@ def mgrit_q8_weight_grad(dy: torch.Tensor, x: Q8Rows, scale: float = 1.0, dW: Op
         _check_device(dW, "dW", device)
         if dW.dtype != torch.float32 or dW.shape != (m, x.cols) or not dW.is_contiguous():
             raise ValueError(f"dW: expected a contiguous fp32 matrix of shape {(m, x.cols)}, got {dW.dtype} {tuple(dW.shape)}")
-    if db is None:
-        db = _new(m, torch.float32, dy.device, other)
+    db, db_at = _vector(db, m, "db", device, dy, other)
     L, dtype = lib(), _DTYPES[dy.dtype]
-    ws = _workspace(workspace, L.mgrit_q8_weight_grad_workspace_bytes(rows, m, x.cols, dtype), dy.device, other)
+    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_q8_weight_grad_workspace_bytes(rows, m, x.cols, dtype), dy.device,
+                                     other)
     st = L.mgrit_q8_weight_grad(rows, m, x.cols, dtype, dy.data_ptr(), ldy, x.q.data_ptr(), x.scale.data_ptr(), scale,
-                                dW.data_ptr(), _check_vector(db, m, "db", device), ws.data_ptr(), ws.numel(), handle)
+                                dW.data_ptr(), db_at, ws_at, ws_bytes, handle)
     if st != MGRIT_OK:
         raise MgritError(st, "mgrit_q8_weight_grad")
-    _in_use(other, dy, x, dW, db, ws)
+    if other is not None:
+        _in_use(other, dy, x, dW, db, ws)
     return dW, db

@@ -53,6 +53,11 @@ int check_weight_grad(int64_t rows, int32_t out_features, int32_t in_features, i
   if (out_features > MOST_FEATURES || in_features > MOST_FEATURES) return MGRIT_UNSUPPORTED;
   return rows > MOST_ROWS || (int64_t)out_features * in_features > MOST_WEIGHTS ? MGRIT_UNSUPPORTED : MGRIT_OK;
 }
+int check_workspace(size_t need, const void* workspace, size_t bytes) {
+  if (!need) return MGRIT_OK;
+  if (!workspace || !aligned(workspace, 256)) return MGRIT_INVALID_ARG;
+  return bytes < need ? MGRIT_WORKSPACE_TOO_SMALL : MGRIT_OK;
+}
 int enqueued(hipError_t e) { return e == hipSuccess ? MGRIT_OK : hip_failed(e); }
 Q8Rows kept(int64_t rows, int32_t cols, const void* q, const void* scale) {
   return Q8Rows{static_cast<unsigned char*>(const_cast<void*>(q)), static_cast<unsigned char*>(const_cast<void*>(scale)), rows, cols};
@@ -104,7 +109,7 @@ int mgrit_layer_norm_forward(const mgrit_norm_desc* desc, const void* x, int64_t
 }
 
 size_t mgrit_layer_norm_backward_workspace_bytes(const mgrit_norm_desc* desc) {
-  return check_norm(desc) == MGRIT_OK ? 4 * norm_backward_partial_floats(desc->rows, desc->cols) + 256 : 0;
+  return check_norm(desc) == MGRIT_OK ? 4 * norm_backward_partial_floats(desc->rows, desc->cols) : 0;
 }
 
 int mgrit_layer_norm_backward(const mgrit_norm_desc* desc, const void* dy, int64_t dy_stride, const void* x,
@@ -121,10 +126,7 @@ int mgrit_layer_norm_backward(const mgrit_norm_desc* desc, const void* dy, int64
   if (desc->rows && (!mean || !rstd)) return MGRIT_INVALID_ARG;
   if (!aligned(gamma, 4) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4)) return MGRIT_INVALID_ARG;
   if (dx && (dx == dy || dx == x)) return MGRIT_INVALID_ARG;
-  if (dgamma || dbeta) {
-    if (!workspace || !aligned(workspace, 256)) return MGRIT_INVALID_ARG;
-    if (workspace_bytes < mgrit_layer_norm_backward_workspace_bytes(desc)) return MGRIT_WORKSPACE_TOO_SMALL;
-  }
+  if (dgamma || dbeta) STCHK(check_workspace(mgrit_layer_norm_backward_workspace_bytes(desc), workspace, workspace_bytes));
   std::lock_guard<std::recursive_mutex> call_lock(call_mutex());
   NormBwdArgs a = {};
   a.rows = desc->rows; a.cols = desc->cols; a.blocks = (int)q8_blocks(desc->cols);
@@ -136,7 +138,7 @@ int mgrit_layer_norm_backward(const mgrit_norm_desc* desc, const void* dy, int64
 
 size_t mgrit_q8_weight_grad_workspace_bytes(int64_t rows, int32_t out_features, int32_t in_features, int dy_dtype) {
   if (check_weight_grad(rows, out_features, in_features, dy_dtype) != MGRIT_OK) return 0;
-  return 4 * q8_grad_partial_floats(rows, out_features, in_features, dy_dtype == MGRIT_DTYPE_BF16) + 256;
+  return 4 * q8_grad_partial_floats(rows, out_features, in_features, dy_dtype == MGRIT_DTYPE_BF16);
 }
 
 int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features, int dy_dtype, const void* dy,
@@ -147,8 +149,7 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
   if (rows && dy_stride > MOST_FEATURES) return MGRIT_UNSUPPORTED;        // a tile's offsets have 32 bits
   STCHK(check_q8(rows, x_q8, x_q8_scale));
   if (!dW || !aligned(dW, 4) || !aligned(db, 4) || !isfinite(scale)) return MGRIT_INVALID_ARG;
-  if (!workspace || !aligned(workspace, 256)) return MGRIT_INVALID_ARG;
-  if (workspace_bytes < mgrit_q8_weight_grad_workspace_bytes(rows, out_features, in_features, dy_dtype)) return MGRIT_WORKSPACE_TOO_SMALL;
+  STCHK(check_workspace(mgrit_q8_weight_grad_workspace_bytes(rows, out_features, in_features, dy_dtype), workspace, workspace_bytes));
   std::lock_guard<std::recursive_mutex> call_lock(call_mutex());
   Q8GradArgs a = {};
   a.rows = rows; a.M = out_features; a.N = in_features; a.dy = dy; a.ldy = dy_stride;

@@ -563,7 +563,7 @@ def test_binding_refusals_on_the_device():
     with pytest.raises(mb.MgritError, match="invalid argument"):
         mb.mgrit_layer_norm_backward(y, x, None, mean, rstd, dx=y)
     with pytest.raises(mb.MgritError, match="workspace too small"):
-        mb.mgrit_q8_weight_grad(y, r, workspace=torch.empty(128, dtype=torch.uint8, device="cuda"))
+        mb.mgrit_q8_weight_grad(rand(1, 4000, 64), mb.mgrit_q8_pack(rand(2, 4000, 64)), workspace=torch.empty(128, dtype=torch.uint8, device="cuda"))
     with pytest.raises(mb.MgritError, match="unsupported"):
         mb.mgrit_layer_norm_forward(torch.zeros(2, 16385, device="cuda"))
 

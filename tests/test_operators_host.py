@@ -71,9 +71,11 @@ def test_norm_backward_refusals():
     assert call(lddy=39) == INVALID and call(ldx=39) == INVALID and call(lddx=39) == INVALID
     assert call(dx=None, dg=None, db=None) == INVALID
     assert call(dx=P) == INVALID and call(dx=2 * P) == INVALID                            # dx over dy, over x
-    assert call(ws=None) == INVALID and call(ws=9 * P + 128) == INVALID and call(dg=7 * P + 2) == INVALID
-    need = mb.lib().mgrit_layer_norm_backward_workspace_bytes(C.byref(norm(rows=5000)))
-    assert need > 256 and call(norm(rows=5000), n=need - 1) == SMALL
+    assert call(dg=7 * P + 2) == INVALID and call(db=8 * P + 1) == INVALID
+    many = norm(rows=5000)
+    need = mb.lib().mgrit_layer_norm_backward_workspace_bytes(C.byref(many))
+    assert need > 0 and call(many, n=need - 1) == SMALL
+    assert call(many, ws=None) == INVALID and call(many, ws=9 * P + 128) == INVALID
     assert call(norm(rows=0), dy=None, x=None, mean=None, rstd=None, dx=None, dg=None, db=None) == INVALID
 
 
@@ -86,17 +88,17 @@ def test_weight_grad_refusals():
     assert call(lddy=23) == INVALID and call(dy=P + 2) == INVALID and call(xq=2 * P + 8) == INVALID
     assert call(dW=4 * P + 2) == INVALID and call(db=5 * P + 1) == INVALID
     assert call(scale=float("inf")) == INVALID and call(scale=float("nan")) == INVALID
-    assert call(ws=None) == INVALID and call(ws=6 * P + 64) == INVALID
     assert call(m=1 << 16, k=1 << 16, lddy=1 << 16) == UNSUPPORTED and call(rows=1 << 31) == UNSUPPORTED
     assert call(m=(1 << 24) + 1, k=1, lddy=1 << 25) == UNSUPPORTED and call(lddy=(1 << 24) + 1) == UNSUPPORTED
     need = mb.mgrit_q8_weight_grad_workspace_bytes(8192, 64, 64, torch.float32)
-    assert need > 256 and call(rows=8192, m=64, k=64, lddy=64, n=need - 1) == SMALL
+    assert need > 0 and call(rows=8192, m=64, k=64, lddy=64, n=need - 1) == SMALL
+    assert call(rows=8192, m=64, k=64, lddy=64, ws=None) == INVALID and call(rows=8192, m=64, k=64, lddy=64, ws=6 * P + 64) == INVALID
     assert mb.lib().mgrit_q8_weight_grad_workspace_bytes(-1, 4, 4, 0) == 0
 
 
 def test_workspace_sizes_do_not_fall_with_the_rows():
     sizes = [mb.mgrit_layer_norm_backward_workspace_bytes(r, 768) for r in (0, 1, 64, 4096, 1 << 20)]
-    assert sizes == sorted(sizes) and sizes[0] > 0
+    assert sizes == sorted(sizes) and sizes[0] == 0 < sizes[-1]
 
 
 def test_adjoint_q8_host_side():
