@@ -389,7 +389,8 @@ int mgrit_q8_unpack(int64_t rows, int32_t cols, int dtype, const void* q, const 
  *   x_q8, x_q8_scale   optional out: the 8-bit rows of x, as mgrit_q8_pack writes them, from the same pass
  *   y_q8, y_q8_scale   optional out: the 8-bit rows of y (of the values stored in y)
  * y may be x itself (same type and stride).  A row with a NaN or an infinity has NaN in y, and in rstd; others are not
- * touched by it. */
+ * touched by it.  Sums are fp32: a row whose sum of squared differences passes its range (differences beyond 1e19) has an
+ * rstd of 0. */
 typedef struct mgrit_norm_desc {
   int64_t rows;
   int32_t cols;
@@ -419,7 +420,8 @@ int mgrit_layer_norm_backward(const mgrit_norm_desc* desc, const void* dy, int64
  *   dy               device [rows, out_features], fp32 or bf16 (dy_dtype)
  *   x_q8, x_q8_scale device, 8-bit rows of in_features elements
  * dW and db are fp32 and overwritten; products are exact and added up in fp32 (an fp32 dy is multiplied in full, not
- * rounded to bf16).  At most 2^24 features either way, dy_stride 2^24 and 2^31 weights (MGRIT_UNSUPPORTED beyond).
+ * rounded to bf16; of its bits only those below 2^-133 are lost).  At most 2^24 features either way, dy_stride 2^24, 2^31 weights and 2^31 - 256 rows
+ * (MGRIT_UNSUPPORTED beyond).
  * Workspace: 256-byte aligned, mgrit_q8_weight_grad_workspace_bytes (host only; 0, also on invalid arguments: none is
  * needed and it may be NULL). */
 size_t mgrit_q8_weight_grad_workspace_bytes(int64_t rows, int32_t out_features, int32_t in_features, int dy_dtype);

@@ -408,6 +408,8 @@ def _stream_handle(stream: Optional[torch.cuda.Stream]) -> C.c_void_p:
 
 
 def _check_state(t: torch.Tensor, shape, name: str):
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: expected a tensor, got {type(t).__name__}")
     if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == tuple(shape)):
         raise ValueError(f"{name}: expected contiguous fp32 device tensor of shape {tuple(shape)}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -700,6 +702,7 @@ def mgrit_adjoint_stacked(desc: ModelDesc, opts: Opts, n_enc: int, Z_all: torch.
 # ---- operators around the solves: 8-bit rows, LayerNorm of rows, gradients from 8-bit rows ------------
 # (Small calls take as long as the host needs for them: what is asked of tensors below is what costs least.)
 Q8_BLOCK = 32                        # MGRIT_Q8_BLOCK of the header
+MOST_COLS = 2 ** 31 - 1              # a row's length has 32 bits in the header, and ctypes cuts what has more
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -711,7 +714,7 @@ class Q8Rows:
     def __init__(self, q: torch.Tensor, scale: torch.Tensor, cols: int):
         blocks = (cols + Q8_BLOCK - 1) // Q8_BLOCK
         at, kept = scale.shape, q.shape
-        if (cols < 1 or q.dtype is not torch.int8 or scale.dtype is not torch.uint8 or len(at) < 1 or len(kept) != len(at)
+        if (not 0 < cols <= MOST_COLS or q.dtype is not torch.int8 or scale.dtype is not torch.uint8 or len(at) < 1 or len(kept) != len(at)
                 or at[-1] != blocks or kept[-1] != blocks * Q8_BLOCK or kept[:-1] != at[:-1]):
             raise ValueError(f"8-bit rows of {cols} elements: expected int8 [..., {blocks * Q8_BLOCK}] and uint8 [..., "
                              f"{blocks}], got {q.dtype} {tuple(q.shape)} and {scale.dtype} {tuple(scale.shape)}")
@@ -745,8 +748,8 @@ class Q8Rows:
 def q8_empty(shape, device="cuda") -> Q8Rows:
     """Uninitialised 8-bit rows for a tensor of that shape."""
     *lead, cols = shape
-    if cols < 1:
-        raise ValueError(f"8-bit rows: expected rows of at least one element, got {tuple(shape)}")
+    if not 0 < cols <= MOST_COLS:
+        raise ValueError(f"8-bit rows: expected rows of 1 to 2^31 - 1 elements, got {tuple(shape)}")
     blocks = (cols + Q8_BLOCK - 1) // Q8_BLOCK
     return Q8Rows._of(torch.empty((*lead, blocks * Q8_BLOCK), dtype=torch.int8, device=device),
                       torch.empty((*lead, blocks), dtype=torch.uint8, device=device), cols)
@@ -779,8 +782,8 @@ def _check_rows(t: torch.Tensor, name: str, device: int, shape=None):
     """(rows, cols, stride) of a matrix argument: leading dimensions that lie one behind the other are rows."""
     _check_device(t, name, device)
     own = t.shape
-    if t.dtype not in _DTYPES or len(own) < 1 or own[-1] < 1 or (shape is not None and own != shape):
-        raise ValueError(f"{name}: expected fp32 or bf16 rows" + (f" of shape {tuple(shape)}" if shape is not None else "") +
+    if t.dtype not in _DTYPES or len(own) < 1 or not 0 < own[-1] <= MOST_COLS or (shape is not None and own != shape):
+        raise ValueError(f"{name}: expected fp32 or bf16 rows of at most 2^31 - 1 elements" + (f" of shape {tuple(shape)}" if shape is not None else "") +
                          f", got {t.dtype} {tuple(own)}")
     cols = own[-1]
     if t.is_contiguous():
@@ -849,8 +852,14 @@ def _vector(given: Optional[torch.Tensor], n: int, name: str, device: int, like:
     return given, _check_vector(given, n, name, device)
 
 
+def _c_int32(n: int) -> int:
+    if n > MOST_COLS:
+        raise ValueError(f"expected a length of at most 2^31 - 1, got {n}")
+    return n
+
+
 def mgrit_q8_blocks(cols: int) -> int:
-    return int(lib().mgrit_q8_blocks(int(cols)))
+    return int(lib().mgrit_q8_blocks(_c_int32(int(cols))))
 
 
 def mgrit_q8_pack(x: torch.Tensor, out: Optional[Q8Rows] = None, stream: Optional[torch.cuda.Stream] = None) -> Q8Rows:
@@ -872,7 +881,7 @@ def mgrit_q8_pack(x: torch.Tensor, out: Optional[Q8Rows] = None, stream: Optiona
 
 def mgrit_q8_unpack(x: Q8Rows, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """What 8-bit rows stand for, as fp32 or bf16 (exactly, in either)."""
+    """What 8-bit rows stand for, as fp32 or bf16 (exactly, in either); with out, in its type."""
     device = _device_of(x.q, "x")
     _check_q8(x, "x", device)
     handle, other = _on(stream, device)
@@ -932,7 +941,7 @@ def mgrit_layer_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = No
 
 
 def mgrit_layer_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
-    return int(lib().mgrit_layer_norm_backward_workspace_bytes(NormDesc(rows, cols, 0, 0, 1e-5)))
+    return int(lib().mgrit_layer_norm_backward_workspace_bytes(NormDesc(rows, _c_int32(cols), 0, 0, 1e-5)))
 
 
 def mgrit_layer_norm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
@@ -974,7 +983,7 @@ def mgrit_layer_norm_backward(dy: torch.Tensor, x, gamma: Optional[torch.Tensor]
 
 
 def mgrit_q8_weight_grad_workspace_bytes(rows: int, out_features: int, in_features: int, dtype: torch.dtype) -> int:
-    return int(lib().mgrit_q8_weight_grad_workspace_bytes(rows, out_features, in_features, _DTYPES[dtype]))
+    return int(lib().mgrit_q8_weight_grad_workspace_bytes(rows, _c_int32(out_features), _c_int32(in_features), _DTYPES[dtype]))
 
 
 def mgrit_q8_weight_grad(dy: torch.Tensor, x: Q8Rows, scale: float = 1.0, dW: Optional[torch.Tensor] = None,

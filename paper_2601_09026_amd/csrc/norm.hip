@@ -222,11 +222,12 @@ __global__ void __launch_bounds__(block_threads<LPR>()) norm_forward_kernel(cons
     }
     wave_sums<LPR>(d, d2);
     float rest = rounded_product(d, n_share), mu = mu0 + rest;
-    float m2 = fmaxf(d2 - d * rest, 0.f);                // sum of (x - mu)^2; fmaxf drops a NaN, d2 keeps it
+    // sum of (x - mu)^2; fmaxf drops a NaN, d2 keeps it (an infinite d2 has nothing to be corrected)
+    float m2 = d2 < __builtin_inff() ? fmaxf(d2 - d * rest, 0.f) : d2;
     if constexpr (LPR > 64) {
       // the wavefronts' shares: mean of the means, and sum (x - mu)^2 = sum over shares of theirs + their number * (difference
       // of the means)^2
-      const f32x4* all = exchange(f32x4{mu, d2 == d2 ? m2 : d2, (float)share, 0.f});
+      const f32x4* all = exchange(f32x4{mu, m2, (float)share, 0.f});
       const float own = mu, base = all[0][0];
       float mean = 0.f, sq = 0.f;
 #pragma unroll 4
@@ -238,10 +239,10 @@ __global__ void __launch_bounds__(block_threads<LPR>()) norm_forward_kernel(cons
 #pragma unroll 4
       for (int w = 0; w < LPR / 64; ++w) sq += all[w][2] * ((all[w][0] - mu) * (all[w][0] - mu));
       rest += mu - own;
-      d2 = m2 = sq;
+      m2 = sq;
     }
     // (a row with a NaN, or with an infinity, has NaN throughout)
-    const float rstd = d2 == d2 ? 1.0f / sqrtf(m2 * n + a.eps) : d2;
+    const float rstd = 1.0f / sqrtf(m2 * n + a.eps);
     if (live && lane == 0) {
       if (a.mean) a.mean[row] = mu;
       if (a.rstd) a.rstd[row] = rstd;

@@ -21,6 +21,7 @@ constexpr int64_t MOST_ROWS = 0x7fffffff;
 constexpr int32_t MOST_NORM_COLS = 16384;              // a row lies in the registers of 1024 lanes
 constexpr int64_t MOST_ELEMENTS = (int64_t)1 << 40, MOST_WEIGHTS = (int64_t)1 << 31;
 constexpr int32_t MOST_FEATURES = 1 << 24;
+constexpr int64_t MOST_TOKENS = MOST_ROWS - 255;       // the index of a token behind the last one, in its tile, has 32 bits
 
 bool known(int dtype) { return dtype == MGRIT_DTYPE_F32 || dtype == MGRIT_DTYPE_BF16; }
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -51,7 +52,7 @@ int check_copy(const void* q, const void* scale) {
 int check_weight_grad(int64_t rows, int32_t out_features, int32_t in_features, int dy_dtype) {
   if (rows < 0 || out_features < 1 || in_features < 1 || !known(dy_dtype)) return MGRIT_INVALID_ARG;
   if (out_features > MOST_FEATURES || in_features > MOST_FEATURES) return MGRIT_UNSUPPORTED;
-  return rows > MOST_ROWS || (int64_t)out_features * in_features > MOST_WEIGHTS ? MGRIT_UNSUPPORTED : MGRIT_OK;
+  return rows > MOST_TOKENS || (int64_t)out_features * in_features > MOST_WEIGHTS ? MGRIT_UNSUPPORTED : MGRIT_OK;
 }
 int check_workspace(size_t need, const void* workspace, size_t bytes) {
   if (!need) return MGRIT_OK;
@@ -96,6 +97,7 @@ int mgrit_layer_norm_forward(const mgrit_norm_desc* desc, const void* x, int64_t
   if (!aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return MGRIT_INVALID_ARG;
   STCHK(check_copy(x_q8, x_q8_scale));
   STCHK(check_copy(y_q8, y_q8_scale));
+  if ((y_q8 && (y_q8 == x_q8 || y_q8_scale == x_q8_scale)) || (mean && mean == rstd)) return MGRIT_INVALID_ARG;
   // in place: every row is read before it is written, if it keeps its place
   if (desc->rows && x == y && (x_stride != y_stride || desc->x_dtype != desc->y_dtype)) return MGRIT_INVALID_ARG;
   std::lock_guard<std::recursive_mutex> call_lock(call_mutex());
@@ -125,7 +127,7 @@ int mgrit_layer_norm_backward(const mgrit_norm_desc* desc, const void* dy, int64
   if (dx) STCHK(check_rows(desc->rows, desc->cols, dx, dx_stride, desc->x_dtype));
   if (desc->rows && (!mean || !rstd)) return MGRIT_INVALID_ARG;
   if (!aligned(gamma, 4) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4)) return MGRIT_INVALID_ARG;
-  if (dx && (dx == dy || dx == x)) return MGRIT_INVALID_ARG;
+  if ((dx && (dx == dy || dx == x)) || (dgamma && dgamma == dbeta)) return MGRIT_INVALID_ARG;
   if (dgamma || dbeta) STCHK(check_workspace(mgrit_layer_norm_backward_workspace_bytes(desc), workspace, workspace_bytes));
   std::lock_guard<std::recursive_mutex> call_lock(call_mutex());
   NormBwdArgs a = {};

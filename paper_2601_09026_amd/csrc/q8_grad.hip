@@ -2,7 +2,7 @@
 //   dW[m,n] = scale * sum_t dY[t,m] x~[t,n],   db[m] = scale * sum_t dY[t,m]
 // A kept value is 7 bits and a sign times a power of two, so it is a bf16 number as it is; a bf16 dY is one as well, and an
 // fp32 dY is exactly the sum of three of 8 bits each (cut, not rounded: hi = its upper 16 bits, then the same of the rest,
-// then what is left).  So the products run on the bf16 matrix cores, one or three of them, without any rounding of an
+// then what is left; bits below 2^-133, bf16's last, are lost).  So the products run on the bf16 matrix cores, one or three of them, without any rounding of an
 // operand, and the sums are fp32 either way: what differs from an fp32 product is only the order of the additions.
 // Bound by the matrix cores (2 T M N flops, or three times that).  16384 tokens, 4096 x 4096, bf16: 495 us, 1110 TFLOP/s, where
 // the library's product of bf16 operands in this order reaches 1150; 8192 tokens, 4096 x 2048, fp32: 366 us, 375 TFLOP/s (1126

@@ -103,3 +103,34 @@ def test_a_training_step_with_kept_rows():
     near(dbeta, rbeta)
     ref, _ = mb.mgrit_adjoint(dm.desc, opts, mb.mgrit_q8_unpack(kept_z), dm.blocks, lamN)
     assert torch.equal(lam, ref)
+
+
+@pytest.mark.parametrize("cache", [True, False])
+def test_captured_calls_replay_bit_identically(cache):
+    print(f"[case] captured adjoint q8 cache={cache}", flush=True)
+    wl = model(wls.ARCH_CAUSAL, wls.DTYPE_BF16, 128, 8, 2)
+    dm = DeviceModel(wl, weight_std=0.05, keep_host=False)
+    opts = mb.mgrit_opts(wl.N, wl.h, wl.cf, wl.levels, wl.iters)
+    Z, _ = mb.mgrit_forward(dm.desc, opts, dev(wls.initial_state(wl)), dm.blocks)
+    lamN, z8 = dev(wls.terminal_adjoint(wl)), mb.q8_empty(Z.shape)
+    mb.mgrit_set_adjoint_cache(cache)
+    try:
+        ws = torch.empty(mb.mgrit_adjoint_q8_workspace_bytes(dm.desc, opts, 1), dtype=torch.uint8, device="cuda")
+        def run():
+            return mb.mgrit_adjoint(dm.desc, opts, mb.mgrit_q8_pack(Z, out=z8), dm.blocks, lamN, workspace=ws)
+        want = [t.clone() for t in run()]
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got = run()
+        for rep in range(3):
+            for t in (*got, z8.q, z8.scale):
+                t.fill_(rep + 1)
+            ws.fill_(255)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            for p, q in zip(got, want):
+                assert torch.equal(p, q), f"replay {rep}"
+    finally:
+        mb.mgrit_set_adjoint_cache(True)

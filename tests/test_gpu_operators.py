@@ -3,6 +3,8 @@ bit, LayerNorm of rows and the gradients from kept rows within bounds that follo
 
 u = 2^-24 is half a step of fp32, relative; sums that are taken in fp32 err by at most (additions in sequence) * u * (sum
 of magnitudes); an output of fewer bits adds half of its step."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -583,3 +585,120 @@ def test_calls_are_profiled():
         mb.mgrit_profile_enable(0)
     assert {k: v["launches"] for k, v in got.items()} == {"q8": 1, "norm_fwd": 1, "norm_bwd": 1, "q8_weight_grad": 1}
     assert got["q8_weight_grad"]["flops"] == 2 * 64 * 96 * 96 and got["q8"]["bytes"] == 64 * 96 * 4 + 64 * 3 * 33
+
+
+# ------------------------------------------------------------------ ranges
+@pytest.mark.parametrize("cols", [3, 40, 768, 5000])
+def test_norm_forward_of_rows_past_the_range(cols):
+    """Squares past fp32: an rstd of 0, y = beta; the rows beside it stay as they are."""
+    say("norm past the range", cols)
+    x = rand(1, 6, cols)
+    want = mb.mgrit_layer_norm_forward(x, beta=torch.full((cols,), 0.25, device="cuda"))
+    big = x.clone()
+    big[2] *= 1e30
+    y, mean, rstd = mb.mgrit_layer_norm_forward(big, beta=torch.full((cols,), 0.25, device="cuda"))
+    assert rstd[2] == 0 and (y[2] == 0.25).all() and torch.isfinite(mean).all()
+    others = [0, 1, 3, 4, 5]
+    for got, ref in zip((y, mean, rstd), want):
+        assert torch.equal(got[others], ref[others])
+
+
+@pytest.mark.parametrize("dtype,size", [(F32, 2.0 ** -112), (F32, 2.0 ** -126), (BF16, 2.0 ** -126)])
+def test_weight_grad_of_tiny_cotangents(dtype, size):
+    """Cotangents whose parts (fp32) or values (bf16) are below the smallest normal number still count.  One token per sum, so
+    that a product is the result.  A bf16 number holds bits down to 2^-133: what of an fp32 cotangent lies below is cut off."""
+    say("weight grad, tiny cotangents", dtype, size)
+    dy = (rand(1, 1, 130).clamp(-3, 3) * size).to(dtype)
+    x = torch.where(rand(2, 1, 70) > 0, 64.0, -64.0)
+    dW, db = mb.mgrit_q8_weight_grad(dy, mb.mgrit_q8_pack(x))
+    ref = np.outer(n64(dy)[0], n64(x)[0])
+    # three parts' products, each exact or rounded to fp32's last step, 2^-149, and two additions of u each
+    lost = 2.0 ** -133 if dtype == F32 else 0.0
+    close(dW, ref, 2 * U * np.abs(ref) + 3 * 2.0 ** -149 + lost * 64, "dW")
+    close(db, n64(dy)[0], 2 * U * np.abs(n64(dy)[0]) + 3 * 2.0 ** -149 + lost, "db")
+
+
+def far_rows(rows, cols, stride, dtype):
+    """Rows `stride` elements apart, NaN-free; only they are initialised."""
+    return torch.empty((rows - 1) * stride + cols, dtype=dtype, device="cuda").as_strided((rows, cols), (stride, 1))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_offsets_past_32_bits(dtype):
+    """Rows that lie further than 2^32 bytes, and elements, from the first one."""
+    say("far rows", dtype)
+    x, dy, gamma = rand(1, 6, 200, dtype=dtype), rand(2, 6, 200, dtype=dtype), rand(3, 200)
+    stride = (1 << 30) + 3
+    fx, fdy, fy = (far_rows(6, 200, stride, dtype) for _ in range(3))
+    fx.copy_(x)
+    fdy.copy_(dy)
+    same_rows(mb.mgrit_q8_pack(fx), mb.mgrit_q8_pack(x))
+    want = mb.mgrit_layer_norm_forward(x, gamma)
+    got = mb.mgrit_layer_norm_forward(fx, gamma, y=fy)
+    for p, q in zip(got, want):
+        assert torch.equal(p, q)
+    mean, rstd = want[1:]
+    for p, q in zip(mb.mgrit_layer_norm_backward(fdy, fx, gamma, mean, rstd, dx=fy), mb.mgrit_layer_norm_backward(dy, x, gamma, mean, rstd)):
+        assert torch.equal(p, q)
+    r = mb.mgrit_q8_pack(x)
+    assert torch.equal(mb.mgrit_q8_unpack(r, out=fy), mb.mgrit_q8_unpack(r, dtype=dtype))
+    del fx, fdy, fy, got
+    tokens = 300                                           # the stride is the most that is allowed
+    far, near, x8 = far_rows(tokens, 100, 1 << 24, dtype), rand(4, tokens, 100, dtype=dtype), mb.mgrit_q8_pack(rand(5, tokens, 60))
+    far.copy_(near)
+    for p, q in zip(mb.mgrit_q8_weight_grad(far, x8), mb.mgrit_q8_weight_grad(near, x8)):
+        assert torch.equal(p, q)
+    with pytest.raises(mb.MgritError, match="unsupported"):
+        mb.mgrit_q8_weight_grad(far_rows(2, 100, (1 << 24) + 1, dtype), mb.mgrit_q8_pack(rand(5, 2, 60)))
+    del far
+    torch.cuda.empty_cache()
+
+
+def test_more_blocks_than_one_launch_takes():
+    """2^30 rows and a few more, of one element (2 GB, 34 GB kept): the second launch's rows."""
+    say("2^30 + 77 rows")
+    rows = (1 << 30) + 77
+    x = torch.zeros((rows, 1), dtype=BF16, device="cuda")
+    at = torch.tensor([0, 1, 12345, (1 << 30) - 1, 1 << 30, (1 << 30) + 1, rows - 1], device="cuda")
+    x[at, 0] = torch.arange(1.0, 8.0, device="cuda").to(BF16)
+    r = mb.mgrit_q8_pack(x)
+    same_rows(mb.Q8Rows(r.q[at], r.scale[at], 1), kept(x[at]))
+    assert torch.equal(mb.mgrit_q8_unpack(r, out=torch.ones_like(x)), x)
+    del r, x
+    torch.cuda.empty_cache()
+
+
+def test_binding_refuses_rows_of_more_than_32_bits():
+    say("a row of 2^31 elements")
+    x = torch.empty((1, 1 << 31), dtype=BF16, device="cuda")
+    for f in (lambda: mb.mgrit_q8_pack(x), lambda: mb.mgrit_layer_norm_forward(x), lambda: mb.mgrit_q8_weight_grad(x, mb.mgrit_q8_pack(rand(1, 1, 4)))):
+        with pytest.raises(ValueError, match="2\\^31 - 1"):
+            f()
+    del x
+    torch.cuda.empty_cache()
+
+
+def test_calls_of_two_threads():
+    """Two host threads, a stream each."""
+    say("two threads")
+    data = [(rand(10 + i, 900, 200), rand(20 + i, 900, 200)) for i in range(2)]
+    def run(x, dy):
+        r = mb.q8_empty(x.shape)
+        _, mean, rstd = mb.mgrit_layer_norm_forward(x, x_q8=r)
+        return [mean, rstd, r.q, *mb.mgrit_layer_norm_backward(dy, r, None, mean, rstd), *mb.mgrit_q8_weight_grad(dy, r)]
+    want = [run(*d) for d in data]
+    torch.cuda.synchronize()
+    bad = []
+    def work(i):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            for _ in range(20):
+                got = run(*data[i])
+                s.synchronize()
+                bad.extend(1 for p, q in zip(got, want[i]) if not torch.equal(p, q))
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad

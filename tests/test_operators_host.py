@@ -53,6 +53,9 @@ def test_norm_forward_refusals():
     assert call(xq=7 * P + 8, xs=8 * P) == INVALID
     assert call(y=P, ldy=48) == INVALID and call(norm(y_dtype=1), y=P) == INVALID          # in place at another place
     assert call(norm(rows=0), x=None, y=None, gamma=None, beta=None, mean=None, rstd=None) == mb.MGRIT_OK
+    # one array for two results
+    assert call(rstd=5 * P) == INVALID
+    assert call(xq=7 * P, xs=8 * P, yq=7 * P, ys=9 * P) == INVALID and call(xq=7 * P, xs=8 * P, yq=9 * P, ys=8 * P) == INVALID
 
 
 def test_norm_backward_refusals():
@@ -71,7 +74,7 @@ def test_norm_backward_refusals():
     assert call(lddy=39) == INVALID and call(ldx=39) == INVALID and call(lddx=39) == INVALID
     assert call(dx=None, dg=None, db=None) == INVALID
     assert call(dx=P) == INVALID and call(dx=2 * P) == INVALID                            # dx over dy, over x
-    assert call(dg=7 * P + 2) == INVALID and call(db=8 * P + 1) == INVALID
+    assert call(dg=7 * P + 2) == INVALID and call(db=8 * P + 1) == INVALID and call(db=7 * P) == INVALID
     many = norm(rows=5000)
     need = mb.lib().mgrit_layer_norm_backward_workspace_bytes(C.byref(many))
     assert need > 0 and call(many, n=need - 1) == SMALL
@@ -94,6 +97,9 @@ def test_weight_grad_refusals():
     assert need > 0 and call(rows=8192, m=64, k=64, lddy=64, n=need - 1) == SMALL
     assert call(rows=8192, m=64, k=64, lddy=64, ws=None) == INVALID and call(rows=8192, m=64, k=64, lddy=64, ws=6 * P + 64) == INVALID
     assert mb.lib().mgrit_q8_weight_grad_workspace_bytes(-1, 4, 4, 0) == 0
+    most = (1 << 31) - 256
+    assert call(rows=most + 1, m=1, k=1) == UNSUPPORTED and mb.mgrit_q8_weight_grad_workspace_bytes(most + 1, 1, 1, torch.float32) == 0
+    assert mb.mgrit_q8_weight_grad_workspace_bytes(most, 1, 1, torch.float32) > 0
 
 
 def test_workspace_sizes_do_not_fall_with_the_rows():
@@ -139,3 +145,27 @@ def test_binding_refuses_what_the_library_cannot_see():
             mb.Q8Rows(*bad)
     with pytest.raises(IndexError):
         mb.Q8Rows(q, s, 40)[0, 1]
+
+
+def test_binding_refuses_lengths_of_more_than_32_bits():
+    """The header's row lengths have 32 bits; a longer one is refused and not cut."""
+    n = (1 << 32) + 40
+    for f in (lambda: mb.mgrit_q8_blocks(n), lambda: mb.q8_empty((2, n), "meta"),
+              lambda: mb.mgrit_layer_norm_backward_workspace_bytes(5000, n),
+              lambda: mb.mgrit_q8_weight_grad_workspace_bytes(8, n, 4, torch.float32),
+              lambda: mb.mgrit_q8_weight_grad_workspace_bytes(8, 4, n, torch.float32),
+              lambda: mb.Q8Rows(torch.empty((1, n + 24), dtype=torch.int8, device="meta"),
+                                torch.empty((1, n // 32 + 1), dtype=torch.uint8, device="meta"), n)):
+        with pytest.raises(ValueError, match="2\\^31 - 1|expected int8"):
+            f()
+
+
+def test_other_adjoints_refuse_kept_states():
+    wl = wls.named_workloads()["tiny_encoder"]
+    desc, opts = mb.model_desc(wl), mb.mgrit_opts(wl.N, wl.h, wl.cf, wl.levels, wl.iters)
+    z8 = mb.q8_empty((wl.N + 1, wl.tokens, wl.d_model), "cpu")
+    lam = torch.zeros(wl.tokens, wl.d_model)
+    with pytest.raises(ValueError, match="expected a tensor, got Q8Rows"):
+        mb.mgrit_adjoint_buffered(desc, opts, mb.BufferOpts(0, 0, 0.0), z8, [lam] * wl.N, lam)
+    with pytest.raises(ValueError, match="expected a tensor, got Q8Rows"):
+        mb.mgrit_forward(desc, opts, z8, [lam] * wl.N)
