@@ -14,7 +14,10 @@
 // become bf16 (2.5 instructions per element, once per tile and not per fragment) and an fp32 dY its three parts.  What
 // paid, at 16384 x 4096 x 4096 in bf16: one tile of LDS stored before another is multiplied 721 us; stores, loads and
 // fragment reads between the products 731 (spilling); conversions and addresses of fewer instructions 508; wavefronts of
-// 64 x 128 instead of 128 x 64 in the block 495.
+// 64 x 128 instead of 128 x 64 in the block 495.  What is left: the matrix cores are busy for 52 % of the cycles (with counters
+// running), LDS for 38 %, wavefronts wait for a free slot to issue in for 37 % and for data or the barrier in 25 %.  A
+// swizzle that spreads the kept rows' stores over all banks, a sixth of the LDS cycles less, gained nothing.  Rows of dY at
+// odd addresses cost 3 to 12 % (16384 x 4095 x 4096; 4096 x 50257 x 768, aligned to 2, 4, 8 and 16 bytes: 398, 385, 362, 355 us).
 #include "kernels.h"
 #include "lds_limit.h"
 #include "prof.h"
