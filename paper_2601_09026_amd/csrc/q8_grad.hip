@@ -16,7 +16,9 @@
 // fragment reads between the products 731 (spilling); conversions and addresses of fewer instructions 508; wavefronts of
 // 64 x 128 instead of 128 x 64 in the block 495.  What is left: the matrix cores are busy for 52 % of the cycles (with counters
 // running), LDS for 38 %, wavefronts wait for a free slot to issue in for 37 % and for data or the barrier in 25 %.  A
-// swizzle that spreads the kept rows' stores over all banks, a sixth of the LDS cycles less, gained nothing.  Rows of dY at
+// swizzle that spreads the kept rows' stores over all banks, a sixth of the LDS cycles less, gained nothing.  All that the
+// conversions cost: 511 -> 491 us without that of the kept rows (values wrong), fp32, 8192 x 4096 x 2048, 370 -> 346, and 313
+// without the parts of dY; a pass that did them beforehand would take 36 us for its bytes in the one case, 58 in the other.  Rows of dY at
 // odd addresses cost 3 to 12 % (16384 x 4095 x 4096; 4096 x 50257 x 768, aligned to 2, 4, 8 and 16 bytes: 398, 385, 362, 355 us).
 #include "kernels.h"
 #include "lds_limit.h"
