@@ -757,6 +757,8 @@ def q8_empty(shape, device="cuda") -> Q8Rows:
 
 def _device_of(t: torch.Tensor, name: str) -> int:
     """Index of a call's device: that of its first operand, which has to be the current one."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: expected a tensor, got {type(t).__name__}")
     device = t.get_device()
     if device < 0 or device != torch._C._cuda_getDevice():
         raise ValueError(f"{name}: expected a tensor on the current device, got one on {t.device}")
@@ -764,12 +766,20 @@ def _device_of(t: torch.Tensor, name: str) -> int:
 
 
 def _check_device(t: torch.Tensor, name: str, device: int):
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: expected a tensor, got {type(t).__name__}")
     if t.get_device() != device:
         raise ValueError(f"{name}: expected a tensor on the current device, got one on {t.device}")
 
 
+def _is_q8(r: Q8Rows, name: str) -> Q8Rows:
+    if not isinstance(r, Q8Rows):
+        raise ValueError(f"{name}: expected Q8Rows, got {type(r).__name__}")
+    return r
+
+
 def _check_q8(r: Q8Rows, name: str, device: int, shape=None):
-    q, scale = r.q, r.scale
+    q, scale = _is_q8(r, name).q, r.scale
     if q.get_device() != device or scale.get_device() != device:
         raise ValueError(f"{name}: expected tensors on the current device, got some on {q.device} and {scale.device}")
     if not (q.is_contiguous() and scale.is_contiguous()):
@@ -882,7 +892,7 @@ def mgrit_q8_pack(x: torch.Tensor, out: Optional[Q8Rows] = None, stream: Optiona
 def mgrit_q8_unpack(x: Q8Rows, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """What 8-bit rows stand for, as fp32 or bf16 (exactly, in either); with out, in its type."""
-    device = _device_of(x.q, "x")
+    device = _device_of(_is_q8(x, "x").q, "x")
     _check_q8(x, "x", device)
     handle, other = _on(stream, device)
     if out is None:
@@ -993,7 +1003,7 @@ def mgrit_q8_weight_grad(dy: torch.Tensor, x: Q8Rows, scale: float = 1.0, dW: Op
     dW = scale * dy^T x, db = scale * the sum of dy's rows.  dy: fp32 or bf16, [..., out_features]."""
     device = _device_of(dy, "dy")
     rows, m, ldy = _check_rows(dy, "dy", device)
-    _check_q8(x, "x", device, (*dy.shape[:-1], x.cols))
+    _check_q8(x, "x", device, (*dy.shape[:-1], _is_q8(x, "x").cols))
     handle, other = _on(stream, device)
     if dW is None:
         dW = _new((m, x.cols), torch.float32, dy.device, other)

@@ -702,3 +702,48 @@ def test_calls_of_two_threads():
     for t in threads:
         t.join()
     assert not bad
+
+
+def test_binding_names_what_is_of_the_wrong_kind():
+    say("wrong kinds")
+    x = rand(1, 4, 64)
+    x8 = mb.mgrit_q8_pack(x)
+    for f in (lambda: mb.mgrit_q8_weight_grad(x, x), lambda: mb.mgrit_q8_pack(x, out=x), lambda: mb.mgrit_layer_norm_forward(x, y_q8=x)):
+        with pytest.raises(ValueError, match="expected Q8Rows, got Tensor"):
+            f()
+    for f in (lambda: mb.mgrit_q8_unpack(x8, out=x8), lambda: mb.mgrit_layer_norm_forward(x, gamma=x8),
+              lambda: mb.mgrit_q8_weight_grad(x, x8, dW=x8), lambda: mb.mgrit_layer_norm_backward(x, x, None, 0.0, 1.0)):
+        with pytest.raises(ValueError, match="expected a tensor, got"):
+            f()
+
+
+def test_the_most_rows():
+    """2^31 - 1 rows of one element: x = 1 has the mean 1, y = beta, and dbeta counts the rows (a slot's part of them is exact,
+    and so are the sums of slots: multiples of the slot's size up to the last)."""
+    say("2^31 - 1 rows of LayerNorm")
+    rows, one = (1 << 31) - 1, torch.ones(1, device="cuda")
+    x = torch.ones((rows, 1), dtype=BF16, device="cuda")
+    y, mean, rstd = mb.mgrit_layer_norm_forward(x, one, 0.5 * one)
+    assert (y == 0.5).all() and (mean == 1).all()
+    ref = mb.mgrit_layer_norm_forward(x[:1], one, 0.5 * one)[2]
+    assert (rstd == ref).all()
+    dx, dgamma, dbeta = mb.mgrit_layer_norm_backward(x, x, one, mean, rstd, dx=y)
+    assert dx is y and (dx == 0).all() and dgamma[0] == 0
+    assert abs(float(dbeta[0]) - rows) <= rows * 64 * U
+    del x, y, mean, rstd, dx
+    torch.cuda.empty_cache()
+
+
+def test_the_most_tokens():
+    """2^31 - 256 tokens of one feature (69 GB kept): sums of ones are exact at that number, a multiple of 256 below 2^32."""
+    say("2^31 - 256 tokens of a weight gradient")
+    tokens = (1 << 31) - 256
+    x8 = mb.q8_empty((tokens, 1))
+    x8.q.zero_()
+    x8.q[:, 0] = 64
+    x8.scale.fill_(121)                                    # 64 * 2^-6
+    dy = torch.ones((tokens, 1), dtype=BF16, device="cuda")
+    dW, db = mb.mgrit_q8_weight_grad(dy, x8)
+    assert float(dW[0, 0]) == tokens and float(db[0]) == tokens
+    del x8, dy
+    torch.cuda.empty_cache()

@@ -169,3 +169,13 @@ def test_other_adjoints_refuse_kept_states():
         mb.mgrit_adjoint_buffered(desc, opts, mb.BufferOpts(0, 0, 0.0), z8, [lam] * wl.N, lam)
     with pytest.raises(ValueError, match="expected a tensor, got Q8Rows"):
         mb.mgrit_forward(desc, opts, z8, [lam] * wl.N)
+
+
+def test_binding_names_what_is_of_the_wrong_kind():
+    x, x8 = torch.zeros(4, 40), mb.q8_empty((4, 40), "cpu")
+    for f, kind in ((lambda: mb.mgrit_q8_pack(x8), "tensor, got Q8Rows"), (lambda: mb.mgrit_q8_unpack(x), "Q8Rows, got Tensor"),
+                    (lambda: mb.mgrit_layer_norm_forward(x8), "tensor, got Q8Rows"),
+                    (lambda: mb.mgrit_layer_norm_backward(x8, x, None, x[:, 0], x[:, 0]), "tensor, got Q8Rows"),
+                    (lambda: mb.mgrit_q8_weight_grad(x8, x8), "tensor, got Q8Rows")):
+        with pytest.raises(ValueError, match=kind):
+            f()
