@@ -54,6 +54,33 @@ def test_as_on_the_unpacked_states(arch, dtype, d, layers, levels, grads, cache)
     assert float((got[0] - exact[0]).norm() / exact[0].norm()) < 0.02
 
 
+@pytest.mark.parametrize("cache", [True, False])
+@pytest.mark.parametrize("arch,dtype,d,layers,levels,batch,seq", [
+    (wls.ARCH_ENCODER, wls.DTYPE_BF16, 40, 64, 3, 1, 1), (wls.ARCH_CAUSAL, wls.DTYPE_F32, 72, 8, 2, 2, 33),
+    (wls.ARCH_CROSS, wls.DTYPE_F32, 8, 16, 2, 1, 5)])
+def test_widths_that_are_not_whole_blocks(arch, dtype, d, layers, levels, batch, seq, cache):
+    """Rows whose last block is filled up, a single token, and launches of many layers."""
+    print(f"[case] adjoint q8, ragged blocks, arch={arch} dtype={dtype} d={d} N={layers} levels={levels} cache={cache}", flush=True)
+    cf = 2 if levels > 1 else 1
+    wl = wls.Workload("q8", arch, d, 1, 2 * d, batch, seq, 7 if arch == wls.ARCH_CROSS else 0, layers, 1.0 / layers, cf, levels, 2, dtype, 78)
+    dm = DeviceModel(wl, weight_std=0.05, keep_host=False)
+    opts = mb.mgrit_opts(wl.N, wl.h, wl.cf, wl.levels, wl.iters)
+    memory = dev(wls.cross_memory(wl)) if wl.mem_seq else None
+    Z, _ = mb.mgrit_forward(dm.desc, opts, dev(wls.initial_state(wl)), dm.blocks, memory=memory)
+    z8, lamN = mb.mgrit_q8_pack(Z), dev(wls.terminal_adjoint(wl))
+    mb.mgrit_set_adjoint_cache(cache)
+    try:
+        runs = []
+        for states in (z8, mb.mgrit_q8_unpack(z8)):
+            g = [torch.zeros(mb.grad_layout(dm.desc).block_bytes, dtype=torch.uint8, device="cuda") for _ in range(wl.N)]
+            lam, res = mb.mgrit_adjoint(dm.desc, opts, states, dm.blocks, lamN, memory=memory, dtheta=g)
+            runs.append([lam, res, *g])
+    finally:
+        mb.mgrit_set_adjoint_cache(True)
+    for p, q in zip(*runs):
+        assert torch.equal(p, q)
+
+
 def test_workspaces_and_refusals():
     print("[case] adjoint q8 refusals", flush=True)
     wl = model(wls.ARCH_ENCODER, wls.DTYPE_F32, 64, 8, 2)
