@@ -2,10 +2,11 @@
 //   dW[m,n] = scale * sum_t dY[t,m] x~[t,n],   db[m] = scale * sum_t dY[t,m]
 // A kept value is 7 bits and a sign times a power of two, so it is a bf16 number as it is; a bf16 dY is one as well, and an
 // fp32 dY is exactly the sum of three of 8 bits each (cut, not rounded: hi = its upper 16 bits, then the same of the rest,
-// then what is left; bits below 2^-133, bf16's last, are lost).  So the products run on the bf16 matrix cores, one or three of them, without any rounding of an
-// operand, and the sums are fp32 either way: what differs from an fp32 product is only the order of the additions.
-// Bound by the matrix cores (2 T M N flops, or three times that).  16384 tokens, 4096 x 4096, bf16: 495 us, 1110 TFLOP/s, where
-// the library's product of bf16 operands in this order reaches 1150; 8192 tokens, 4096 x 2048, fp32: 366 us, 375 TFLOP/s (1126
+// then what is left; bits below 2^-133, bf16's last, are lost).  So the products run on the bf16 matrix cores, one or three of
+// them, without any rounding of an operand, and the sums are fp32 either way: what differs from an fp32 product is only the
+// order of the additions.
+// Bound by the matrix cores (2 T M N flops, or three times that).  16384 tokens, 4096 x 4096, bf16: 482 us, 1140 TFLOP/s, where
+// the library's product of bf16 operands in this order reaches 1150; 8192 tokens, 4096 x 2048, fp32: 346 us, 397 TFLOP/s (1190
 // of bf16 products; the fp32 matrix cores' own limit is 157).
 //
 // Both operands are token-major and the reduction runs over the tokens, so the tiles are staged as they lie in memory
@@ -14,12 +15,17 @@
 // become bf16 (2.5 instructions per element, once per tile and not per fragment) and an fp32 dY its three parts.  What
 // paid, at 16384 x 4096 x 4096 in bf16: one tile of LDS stored before another is multiplied 721 us; stores, loads and
 // fragment reads between the products 731 (spilling); conversions and addresses of fewer instructions 508; wavefronts of
-// 64 x 128 instead of 128 x 64 in the block 495.  What is left: the matrix cores are busy for 52 % of the cycles (with counters
-// running), LDS for 38 %, wavefronts wait for a free slot to issue in for 37 % and for data or the barrier in 25 %.  A
-// swizzle that spreads the kept rows' stores over all banks, a sixth of the LDS cycles less, gained nothing.  All that the
-// conversions cost: 511 -> 491 us without that of the kept rows (values wrong), fp32, 8192 x 4096 x 2048, 370 -> 346, and 313
-// without the parts of dY; a pass that did them beforehand would take 36 us for its bytes in the one case, 58 in the other.  Rows of dY at
-// odd addresses cost 3 to 12 % (16384 x 4095 x 4096; 4096 x 50257 x 768, aligned to 2, 4, 8 and 16 bytes: 398, 385, 362, 355 us).
+// 64 x 128 instead of 128 x 64 in the block 495; db from the registers on their way to LDS and not from the fragments, shared
+// out over the columns of tiles, 503 -> 484 on another card.  What is left: the matrix cores are busy for 52 % of the cycles
+// (with counters running), LDS for 38 %, wavefronts wait for a free slot to issue in for 37 % and for data or the barrier in
+// 25 %.  Loads that are waited for one by one and not at a tile's start gained nothing, nor did a swizzle that spreads the kept
+// rows' stores over all banks, a sixth of the LDS cycles less.  The conversions cost 511 -> 491 us for the kept rows (values wrong
+// without), and with fp32, 8192 x 4096 x 2048, 370 -> 346, and 313 without the parts of dY; a pass that did them beforehand would
+// take 36 us for its bytes in the one case, 58 in the other.  Rows of dY at odd addresses cost 3 to 12 % (16384 x 4095 x 4096;
+// 4096 x 50257 x 768, aligned to 2, 4, 8 and 16 bytes: 398, 385, 362, 355 us).
+#include <climits>
+#include <type_traits>
+
 #include "kernels.h"
 #include "lds_limit.h"
 #include "prof.h"
@@ -101,14 +107,12 @@ __device__ __forceinline__ u32x2 kept_bf16(unsigned q, float step) {
   return u32x2{upper(signed_byte<0>(q) * step, signed_byte<1>(q) * step), upper(signed_byte<2>(q) * step, signed_byte<3>(q) * step)};
 }
 
-// the sum of a fragment's 8 values
-__device__ __forceinline__ float fragment_sum(bf16x8 v) {
-  const u32x4 u = __builtin_bit_cast(u32x4, v);
-  float t[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) t[i] = bits_f(u[i] << 16) + bits_f(u[i] & 0xffff0000u);
-  return (t[0] + t[1]) + (t[2] + t[3]);
-}
+// A thread's sums of db carry their errors, but for the largest bf16 tile, which has no 8 registers left for them (values of 8
+// bits lose little: 3e-8 of db's size after 16384 tokens, 4e-8 with the errors).
+struct PlainSum {
+  float sum = 0.f;
+  __device__ __forceinline__ void add(float x) { sum += x; }
+};
 
 // The work of a launch: `whole` tiles in one piece, then `rest` tiles of `slices` slices each.  Blocks go to the 8 XCDs in
 // turn; each XCD takes a contiguous run of either kind, so that what it works on at a time shares panels of the operands in
@@ -134,7 +138,7 @@ struct Items {
 
 template <typename T, int BM, int BN, int BK, int WM, int WN, int OCC>
 __global__ void __launch_bounds__(64 * WM * WN, OCC * WM * WN / 4)
-q8_grad_kernel(const Q8GradArgs a, int tiles_n, Items it, float* partial) {
+q8_grad_kernel(const Q8GradArgs a, int tiles_n, Items it, float* partial, float* column) {
   constexpr int NT = 64 * WM * WN, PARTS = std::is_same<T, float>::value ? 3 : 1;
   constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
   constexpr int RA = BM * 2, RB = BN * 2;                // bytes per LDS row
@@ -222,13 +226,27 @@ q8_grad_kernel(const Q8GradArgs a, int tiles_n, Items it, float* partial) {
       }
     }
   };
-  // The first column of tiles adds up dY as well, from the fragments: of the WN wavefronts that read the same ones each
-  // takes every WN-th 16 tokens.
-  const bool sums = tn == 0 && a.db;
-  CarrySum bias[TM];
-  float run[TM];
+  // dY is added up as well, as it lies in the registers between memory and LDS: all of a thread's chunks have the same 8
+  // features.  With `column`, every column of tiles takes its share of the token tiles and leaves its sums there; else the first
+  // one takes them all.
+  const bool sums = a.db && (column || tn == 0);
+  const int share = column ? tiles_n : 1;
+  int due = !sums ? INT_MIN : column ? tn : 0;            // the next token tile of the share, counted from the slice's first
+  if (sums && kt0) {                                      // (a row of tiles may have whole ones and slices: shares are of all tokens)
+    const int at = __builtin_amdgcn_readfirstlane(kt0 % share);
+    due += due < at ? share - at : -at;
+  }
+  typename std::conditional<(BM < 256), CarrySum, PlainSum>::type total[8];
+  auto add_tile = [&] {
 #pragma unroll
-  for (int i = 0; i < TM; ++i) run[i] = 0.f;
+    for (int e = 0; e < 8; ++e) {
+      float t = ra[0].at(e);
+#pragma unroll
+      for (int j = 1; j < A_CH; ++j) t += ra[j].at(e);
+      total[e].add(t);
+    }
+    due += share;
+  };
 
   // fragments: tokens 8*(lane/32).., one column per lane
   const int lh = lane >> 5, trow = 8 * lh + ((lane & 15) >> 2), low = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
@@ -272,10 +290,6 @@ q8_grad_kernel(const Q8GradArgs a, int tiles_n, Items it, float* partial) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) xb[j] = tr_value(fb[ks & 1][j]);
     __builtin_amdgcn_sched_barrier(0);
-    if (sums && wave % WN == ks % WN) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) run[i] += fragment_sum(xa[i]);
-    }
 #pragma unroll
     for (int q = 0; q < NM; ++q) {
       const int i = q / TN, j = q % TN;
@@ -288,6 +302,7 @@ q8_grad_kernel(const Q8GradArgs a, int tiles_n, Items it, float* partial) {
           else read_b(Int<r>{}, read_off, u < TM ? 0 : u - TM);
         }
       if constexpr (decltype(jobs)::value) {
+        if (s == 0 && q == 0 && kt + 1 == due) add_tile();
         const int slot = s * NM + q;
 #pragma unroll
         for (int u = 0; u < JOBS; ++u)
@@ -314,10 +329,6 @@ q8_grad_kernel(const Q8GradArgs a, int tiles_n, Items it, float* partial) {
       }
     };
     go(go, Int<0>{});
-    if (sums) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) { bias[i].add(run[i]); run[i] = 0.f; }
-    }
     cur ^= 1;
   };
   auto every_load = [&](int kt) {
@@ -325,6 +336,7 @@ q8_grad_kernel(const Q8GradArgs a, int tiles_n, Items it, float* partial) {
     for (int j = 0; j < JOBS; ++j) load(std::false_type{}, j, kt);
   };
   every_load(0);
+  if (due == 0) add_tile();
 #pragma unroll
   for (int j = 0; j < JOBS; ++j) store(j, 0);
   if (KT > 1) every_load(1);
@@ -351,15 +363,16 @@ q8_grad_kernel(const Q8GradArgs a, int tiles_n, Items it, float* partial) {
     scale = 1.f;
   }
   if (sums) {                                             // block-uniform
-    float* red = reinterpret_cast<float*>(smem);          // [WN][2 halves of the tokens][BM]
+    float* red = reinterpret_cast<float*>(smem);          // [A_ROWS][BM]
 #pragma unroll
-    for (int i = 0; i < TM; ++i) red[((wave % WN) * 2 + lh) * BM + wm0 + 32 * i + (lane & 31)] = bias[i].sum;
+    for (int e = 0; e < 8; ++e) red[ar * BM + ac + e] = total[e].sum;
     __syncthreads();
     for (int m = threadIdx.x; m < BM && m0 + m < M; m += NT) {
       CarrySum t;
 #pragma unroll
-      for (int g = 0; g < 2 * WN; ++g) t.add(red[g * BM + m]);
+      for (int g = 0; g < A_ROWS; ++g) t.add(red[g * BM + m]);
       if (part) part[BM * BN + m] = t.sum;
+      else if (column) column[(long)tile * BM + m] = t.sum;
       else a.db[m0 + m] = scale * t.sum;
     }
   }
@@ -381,23 +394,40 @@ q8_grad_kernel(const Q8GradArgs a, int tiles_n, Items it, float* partial) {
   }
 }
 
-// The tiles that were cut into slices: the slices' sums, in order.  A block takes 1024 elements of a tile, or a tile's bias.
-__global__ void __launch_bounds__(256) q8_grad_join_kernel(const Q8GradArgs a, const float* partial, int whole, int slices, int BM, int BN, int tiles_n) {
-  const int tile = whole + blockIdx.y, tm = tile / tiles_n, tn = tile - tm * tiles_n;
+// The tiles that were cut into slices: the slices' sums, in order, 1024 elements of a tile per block.  Blocks behind those add
+// up db: 16 features each, their columns of tiles and slices in 16 runs.
+__global__ void __launch_bounds__(256) q8_grad_join_kernel(const Q8GradArgs a, const float* partial, const float* column, int whole, int rest, int slices, int BM, int BN, int tiles_n) {
   const long each = (long)BM * BN + BM;
-  const float* p = partial + (long)blockIdx.y * slices * each;
-  const int e = (blockIdx.x * 256 + threadIdx.x) * 4;
-  if (e >= BM * BN) {                                     // BM is a multiple of 4
-    const int m = tm * BM + e - BM * BN;
-    if (tn != 0 || !a.db || e >= each) return;
-    for (int i = 0; i < 4 && m + i < a.M; ++i) {
+  if ((int)blockIdx.y >= rest) {
+    __shared__ float red[16][16];
+    const int k = threadIdx.x & 15, run = threadIdx.x >> 4;
+    const long blocks = (long)(gridDim.y - rest) * gridDim.x;
+    for (long b = ((long)blockIdx.y - rest) * gridDim.x + blockIdx.x; b * 16 < a.M; b += blocks) {
+      const long m = b * 16 + k;
       CarrySum t;
-      for (int s = 0; s < slices; ++s) t.add(p[s * each + e + i]);
-      a.db[m + i] = a.scale * t.sum;
+      if (m < a.M) {
+        const int tm = (int)(m / BM), r = (int)(m - (long)tm * BM);
+#pragma unroll 4
+        for (int p = run; p < tiles_n * slices; p += 16) {
+          const int tn = p / slices, s = p - tn * slices, tile = tm * tiles_n + tn;
+          if (tile >= whole) t.add(partial[((long)(tile - whole) * slices + s) * each + BM * BN + r]);
+          else if (s == 0) t.add(column[(long)tile * BM + r]);
+        }
+      }
+      __syncthreads();
+      red[run][k] = t.sum;
+      __syncthreads();
+      if (run == 0 && m < a.M) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) t.add(red[i][k]);
+        a.db[m] = a.scale * t.sum;
+      }
     }
     return;
   }
-  const int r = e / BN, m = tm * BM + r, n = tn * BN + e - r * BN;
+  const int tile = whole + blockIdx.y, tm = tile / tiles_n, tn = tile - tm * tiles_n;
+  const float* p = partial + (long)blockIdx.y * slices * each;
+  const int e = (blockIdx.x * 256 + threadIdx.x) * 4, r = e / BN, m = tm * BM + r, n = tn * BN + e - r * BN;
   if (m >= a.M || n >= a.N) return;
   CarrySum acc[4];
 #pragma unroll 4
@@ -431,7 +461,17 @@ constexpr Tile TILES_F32[] = {{128, 256, 64, 1, 6.3, {36.3}}, {128, 128, 32, 2, 
                               {64, 64, 32, 4, 4.7, {20.1, 23.5, 30.7, 38.0}}};
 constexpr double J0 = 1.6, J1 = 0.43, J_BYTES = 4.8e6;                     // us, us a slice, bytes per us
 constexpr int MOST_SLICES = 64;
-struct Plan { int cfg, tiles_m, tiles_n, whole, slices; };
+// db: the first column of tiles takes all of it, or the columns share it out and the join adds up theirs.  The first column's
+// blocks take up to 1.3 us per 1000 tokens more than the others, and a launch of few rounds waits for them; a join that would not
+// run otherwise takes 3 to 7 us.  One column and all of them, us, bf16: joined anyway, 12608 tokens, 384 x 384, 23.0, 21.2; 4096,
+// 50257 x 768, 354, 349; 8192, 20000 x 1024, 353, 344; fp32 12608, 2048 x 1000, 150.7, 147.2; not joined otherwise, 16384, 4096 x 4096, 500, 484;
+// 8192, 8192 x 4096, 505, 501; 4096, 4096 x 4096, 134, 131, but 4096, 32000 x 512, 141, 145 and 2048, 4096 x 4096, 73.8, 74.2.
+constexpr long SPREAD_ROWS = 8192;
+struct Plan {
+  int cfg, tiles_m, tiles_n, whole, slices;
+  int rest() const { return tiles_m * tiles_n - whole; }
+  bool spread(long rows) const { return rest() || (tiles_n > 1 && rows >= SPREAD_ROWS); }
+};
 Plan plan(long rows, int M, int N, bool dy_bf16) {
   Plan best = {};
   double best_cost = 1e300;
@@ -457,14 +497,18 @@ template <typename T, int BM, int BN, int BK, int WM, int WN, int OCC>
 hipError_t launch_tile(const Q8GradArgs& a, const Plan& p, float* partial, hipStream_t st) {
   constexpr int PARTS = std::is_same<T, float>::value ? 3 : 1;
   const size_t smem = 2 * (size_t)BK * 2 * (PARTS * BM + BN);
-  static_assert(2 * WN * BM * 4 <= 2 * BK * 2 * (PARTS * BM + BN), "the bias sums fit");
+  static_assert(64 * WM * WN * 8 * 4 <= 2 * BK * 2 * (PARTS * BM + BN), "the sums of db fit");
   auto kern = q8_grad_kernel<T, BM, BN, BK, WM, WN, OCC>;
   static unsigned long raised = 0;
   if (const hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kern), (int)smem, raised); e != hipSuccess) return e;
   const Items it(p.tiles_m * p.tiles_n, p.whole, p.slices);
-  hipLaunchKernelGGL(kern, dim3(it.blocks()), dim3(64 * WM * WN), smem, st, a, p.tiles_n, it, partial);
-  if (const hipError_t e = hipGetLastError(); e != hipSuccess || !it.rest) return e;
-  hipLaunchKernelGGL(q8_grad_join_kernel, dim3((BM * BN + BM + 1023) / 1024, it.rest), dim3(256), 0, st, a, partial, p.whole, p.slices, BM, BN, p.tiles_n);
+  float* column = p.spread(a.rows) ? partial + (size_t)it.rest * p.slices * (BM * BN + BM) : nullptr;
+  hipLaunchKernelGGL(kern, dim3(it.blocks()), dim3(64 * WM * WN), smem, st, a, p.tiles_n, it, partial, column);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  constexpr int X = BM * BN / 1024;
+  const int sums = a.db && column ? (a.M + 16 * X - 1) / (16 * X) : 0, y = it.rest + (sums < 1024 ? sums : 1024);
+  if (!y) return hipSuccess;
+  hipLaunchKernelGGL(q8_grad_join_kernel, dim3(X, y), dim3(256), 0, st, a, partial, column, p.whole, it.rest, p.slices, BM, BN, p.tiles_n);
   return hipGetLastError();
 }
 
@@ -474,7 +518,7 @@ size_t q8_grad_partial_floats(long rows, int M, int N, bool dy_bf16) {
   if (rows <= 0) return 0;
   const Plan p = plan(rows, M, N, dy_bf16);
   const Tile& t = dy_bf16 ? TILES_BF16[p.cfg] : TILES_F32[p.cfg];
-  return (size_t)(p.tiles_m * p.tiles_n - p.whole) * p.slices * (t.bm * t.bn + t.bm);
+  return (size_t)p.rest() * p.slices * (t.bm * t.bn + t.bm) + (p.spread(rows) ? (size_t)p.whole * t.bm : 0);
 }
 
 hipError_t launch_q8_grad(const Q8GradArgs& a, bool dy_bf16, float* partial, hipStream_t st) {

@@ -411,6 +411,12 @@ def test_weight_grad_of_large_weights(rows, m, k, dtype):
     close(db, 0.5 * n64(dy).sum(0), 0.5 * (rows + 64) * U * np.abs(n64(dy)).sum(0), "db")
 
 
+@pytest.mark.parametrize("rows,m,k,dtype", [(8200, 4000, 4030, BF16), (8200, 2047, 4033, F32), (8191, 4000, 4030, BF16)])
+def test_weight_grad_of_whole_rounds(rows, m, k, dtype):
+    """Tiles that fill the chip without slices: db from all columns of tiles, from 8192 tokens on, and from the first one."""
+    test_weight_grad_of_large_weights(rows, m, k, dtype)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("m", [24, 200, 256])
 def test_weight_grad_of_slices_of_wider_rows(m, dtype):
