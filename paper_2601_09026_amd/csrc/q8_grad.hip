@@ -16,9 +16,9 @@
 // paid, at 16384 x 4096 x 4096 in bf16: one tile of LDS stored before another is multiplied 721 us; stores, loads and
 // fragment reads between the products 731 (spilling); conversions and addresses of fewer instructions 508; wavefronts of
 // 64 x 128 instead of 128 x 64 in the block 495; db from the registers on their way to LDS and not from the fragments, shared
-// out over the columns of tiles, 503 -> 484 on another card.  What is left: the matrix cores are busy for 52 % of the cycles
-// (with counters running), LDS for 38 %, wavefronts wait for a free slot to issue in for 37 % and for data or the barrier in
-// 25 %.  Loads that are waited for one by one and not at a tile's start gained nothing, nor did a swizzle that spreads the kept
+// out over the columns of tiles, 503 -> 484 on another card.  What is left: the clock, 1.7 GHz under this load,
+// and of its cycles the matrix cores are busy for 58 %, LDS for 43 %; wavefronts wait for a slot to issue in for 40 % of theirs and
+// for data or the barrier for 24 %.  Loads that are waited for one by one and not at a tile's start gained nothing, nor did a swizzle that spreads the kept
 // rows' stores over all banks, a sixth of the LDS cycles less.  The conversions cost 511 -> 491 us for the kept rows (values wrong
 // without), and with fp32, 8192 x 4096 x 2048, 370 -> 346, and 313 without the parts of dY; a pass that did them beforehand would
 // take 36 us for its bytes in the one case, 58 in the other.  Rows of dY at odd addresses cost 3 to 12 % (16384 x 4095 x 4096;
