@@ -816,7 +816,11 @@ def _check_vector(t: Optional[torch.Tensor], n: int, name: str, device: int) -> 
 def _on(stream: Optional[torch.cuda.Stream], device: int):
     """(handle, stream if it is not the current one): where a call is enqueued."""
     current = torch._C._cuda_getCurrentRawStream(device)
-    if stream is None or stream.cuda_stream == current:
+    if stream is None:
+        return current, None
+    if stream.device_index != device:
+        raise ValueError(f"stream: expected one of the current device, got one of device {stream.device_index}")
+    if stream.cuda_stream == current:
         return current, None
     return stream.cuda_stream, stream
 

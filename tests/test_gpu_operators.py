@@ -4,6 +4,7 @@ bit, LayerNorm of rows and the gradients from kept rows within bounds that follo
 u = 2^-24 is half a step of fp32, relative; sums that are taken in fp32 err by at most (additions in sequence) * u * (sum
 of magnitudes); an output of fewer bits adds half of its step."""
 import threading
+import types
 
 import numpy as np
 import pytest
@@ -753,3 +754,15 @@ def test_the_most_tokens():
     assert float(dW[0, 0]) == tokens and float(db[0]) == tokens
     del x8, dy
     torch.cuda.empty_cache()
+
+
+def test_a_stream_of_another_device_is_refused():
+    say("a stream of another device")
+    x, other = rand(1, 4, 64), types.SimpleNamespace(device_index=torch.cuda.current_device() + 1, cuda_stream=0)
+    x8 = mb.mgrit_q8_pack(x, stream=torch.cuda.current_stream())
+    _, mean, rstd = mb.mgrit_layer_norm_forward(x)
+    for f in (lambda: mb.mgrit_q8_pack(x, stream=other), lambda: mb.mgrit_q8_unpack(x8, stream=other),
+              lambda: mb.mgrit_layer_norm_forward(x, stream=other), lambda: mb.mgrit_layer_norm_backward(x, x, None, mean, rstd, stream=other),
+              lambda: mb.mgrit_q8_weight_grad(x, x8, stream=other)):
+        with pytest.raises(ValueError, match="current device"):
+            f()
