@@ -448,18 +448,18 @@ __global__ void __launch_bounds__(256) q8_grad_zero_kernel(long mn, int M, float
 // Tile and slices of a launch.  Tiles that fill whole rounds of the chip are computed in one piece; those of the last
 // round, which would leave part of it idle, are cut along the tokens into slices that fill it, which costs writing and
 // adding up the slices' sums.  The time of a round is fixed + tokens * per_token[blocks on a CU], that of joining slices
-// J0 + J1 * slices and their bytes, fitted to 1100 launches (64 to 70001 tokens, 64 x 64 to 50257 x 768 weights, both
-// types) and within 6-9 % of them; the pick is 0.6 % slower than the best of all tiles and slices on average, 10 % at worst.
-// One piece or slices of the last round: 4096 tokens, 50257 x 768, bf16, 363 against 348 us; 16384 x 4096 x 1024 394
-// against 148.  Large tiles or small ones: 16384 x 4096 x 4096 495, 685, 1415 us; 2048 x 384 x 384 23, 14, 12.7.
+// J0 + J1 * slices and their bytes, fitted to 1232 launches (64 to 70001 tokens, 64 x 64 to 50257 x 768 weights, both
+// types) and within 7-10 % of them; the pick is 0.7 % slower than the best of all tiles and slices on average, 15 % at worst
+// (3000 tokens, 9000 x 130).  One piece or slices of the last round: 16384 tokens, 4096 x 1024, bf16, 372 against 151 us.  Large
+// tiles or small ones: 16384 tokens, 4096 x 4096, 470, 630, 1510 us; 2048, 384 x 384, each with its best slices, 22, 15, 11.7.
 // CUS is a constant: the plan, and with it the order of the sums, follows from the sizes alone.
 constexpr int CUS = 256;
 struct Tile { int bm, bn, bk, per_cu; double fixed, per_token[4]; };       // us, us per 1000 tokens
-constexpr Tile TILES_BF16[] = {{256, 256, 64, 1, 6.3, {24.7}}, {128, 128, 64, 2, 6.0, {14.7, 18.6}},
-                               {64, 64, 64, 4, 4.8, {7.6, 9.4, 12.8, 16.1}}};
-constexpr Tile TILES_F32[] = {{128, 256, 64, 1, 6.3, {36.3}}, {128, 128, 32, 2, 5.6, {36.0, 46.3}},
-                              {64, 64, 32, 4, 4.7, {20.1, 23.5, 30.7, 38.0}}};
-constexpr double J0 = 1.6, J1 = 0.43, J_BYTES = 4.8e6;                     // us, us a slice, bytes per us
+constexpr Tile TILES_BF16[] = {{256, 256, 64, 1, 6.6, {24.6}}, {128, 128, 64, 2, 6.35, {13.6, 18.8}},
+                               {64, 64, 64, 4, 5.4, {7.8, 9.6, 14.0, 18.3}}};
+constexpr Tile TILES_F32[] = {{128, 256, 64, 1, 6.5, {33.7}}, {128, 128, 32, 2, 5.75, {32.9, 45.3}},
+                              {64, 64, 32, 4, 5.15, {18.5, 22.2, 30.9, 39.6}}};
+constexpr double J0 = 2.1, J1 = 0.07, J_BYTES = 5.1e6;                     // us, us a slice, bytes per us
 constexpr int MOST_SLICES = 64;
 // db: the first column of tiles takes all of it, or the columns share it out and the join adds up theirs.  The first column's
 // blocks take up to 1.3 us per 1000 tokens more than the others, and a launch of few rounds waits for them; a join that would not
