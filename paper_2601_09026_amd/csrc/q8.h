@@ -64,16 +64,17 @@ template <typename T> __device__ __forceinline__ f32x4 load4_row(const T* row, i
 // (after load4_row, where the 4 elements may reach past the row's end)
 __device__ __forceinline__ f32x4 settle4(f32x4 v, int c, int cols) {
   if (cols < 4) return v;
-  const int past = c + 4 - cols;                          // elements past the end
+  const int past = 4 - (cols - c);                        // elements past the end (c + 4 can pass 32 bits)
   f32x4 r = v;
   r = past & 1 ? f32x4{r[1], r[2], r[3], 0.f} : r;
   r = past & 2 ? f32x4{r[2], r[3], 0.f, 0.f} : r;
   r = past >= 4 ? f32x4{0.f, 0.f, 0.f, 0.f} : r;
   return past > 0 ? r : v;
 }
-// stores those of the 4 elements that lie inside the row
+// stores those of the 4 elements that lie inside the row (its length is at most 2^31 - 1, so c + 4 can pass 32 bits; c + 3
+// cannot, and neither can the difference)
 template <typename T> __device__ __forceinline__ void store4_row(T* row, int c, int cols, f32x4 v) {
-  if (c + 4 <= cols) {
+  if (cols - c >= 4) {
     store4u<T>(row + c, v);
   } else {
 #pragma unroll

@@ -766,3 +766,31 @@ def test_a_stream_of_another_device_is_refused():
               lambda: mb.mgrit_q8_weight_grad(x, x8, stream=other)):
         with pytest.raises(ValueError, match="current device"):
             f()
+
+
+@pytest.mark.parametrize("cols", [(1 << 31) - 1, (1 << 31) - 2, (1 << 31) - 31, (1 << 31) - 32, (1 << 31) - 33])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_the_longest_rows(cols, dtype):
+    """A row of nearly 2^31 elements: its last block ends inside the row, at its end or behind it, where columns pass 32 bits.
+    What lies behind the row stays as it was.  Steps are 1 (a 127 in every block), so that all values are whole numbers."""
+    say("the longest rows", cols, dtype)
+    blocks = mb.mgrit_q8_blocks(cols)
+    x8 = mb.q8_empty((1, cols))
+    torch.randint(-127, 128, x8.q.shape, dtype=torch.int8, device="cuda", out=x8.q)
+    x8.q[0, ::32] = 127
+    x8.q[0, cols:] = 0
+    x8.scale.fill_(127)
+    store = torch.full((cols + 64,), 5.0, dtype=dtype, device="cuda")
+    x = store[:cols].view(1, cols)
+    mb.mgrit_q8_unpack(x8, out=x)
+    assert (store[cols:] == 5).all()
+    for at in range(0, cols, 1 << 28):
+        n = min(1 << 28, cols - at)
+        assert torch.equal(store[at:at + n], x8.q[0, at:at + n].to(dtype)), at
+    again = mb.q8_empty((1, cols))
+    again.q.fill_(99)
+    again.scale.fill_(99)
+    mb.mgrit_q8_pack(x, out=again)
+    assert again.scale.shape == (1, blocks) and (again.scale == 127).all() and torch.equal(again.q, x8.q)
+    del x8, x, store, again
+    torch.cuda.empty_cache()
