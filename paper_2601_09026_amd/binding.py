@@ -464,7 +464,8 @@ def mgrit_adjoint(desc: ModelDesc, opts: Opts, Z_all, theta: List[torch.Tensor],
     [batch*mem_seq, d] device tensor filled with the gradient of the cross-attention memory.
     linearised: call mgrit_adjoint_linearised (workspace = the adjoint_workspace that mgrit_forward filled).
     Z_all may be Q8Rows of that shape, mgrit_q8_pack(Z_all): mgrit_adjoint_q8 (workspace:
-    mgrit_adjoint_q8_workspace_bytes)."""
+    mgrit_adjoint_q8_workspace_bytes).
+    stream: where the call is enqueued, behind what the caller has put before it there; what is allocated here belongs to it."""
     T, d = desc.batch * desc.seq, desc.d_model
     q8 = isinstance(Z_all, Q8Rows)
     if q8:
@@ -478,11 +479,12 @@ def mgrit_adjoint(desc: ModelDesc, opts: Opts, Z_all, theta: List[torch.Tensor],
     _check_state(lambda_N, (T, d), "lambda_N")
     if len(theta) != opts.N:
         raise ValueError("theta must hold N blocks")
+    handle, other = _on(stream, lambda_N.get_device())
     if lambda_all is None:
-        lambda_all = torch.empty((opts.N + 1, T, d), dtype=torch.float32, device=Z_all.device)
+        lambda_all = _new((opts.N + 1, T, d), torch.float32, Z_all.device, other)
     _check_state(lambda_all, (opts.N + 1, T, d), "lambda_all")
     if resnorm is None:
-        resnorm = torch.zeros(max(opts.iters, 1), dtype=torch.float32, device=Z_all.device)
+        resnorm = _new_zeros(max(opts.iters, 1), Z_all.device, other)
     if dtheta is not None and len(dtheta) != opts.N:
         raise ValueError("dtheta must hold N blocks")
     if dmemory is not None:
@@ -490,22 +492,18 @@ def mgrit_adjoint(desc: ModelDesc, opts: Opts, Z_all, theta: List[torch.Tensor],
     query = mgrit_adjoint_q8_workspace_bytes if q8 else mgrit_workspace_bytes
     need = query(desc, opts, 2 if (dtheta is not None or dmemory is not None) else 1)
     if workspace is None:
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=Z_all.device)
+        workspace = _new((max(need, 256),), torch.uint8, Z_all.device, other)
     if linearised and workspace is None:
         raise ValueError("linearised: pass the adjoint workspace that the forward call filled")
-    if q8:
-        st = lib().mgrit_adjoint_q8(C.byref(desc), C.byref(opts), _ptr(Z_all.q), _ptr(Z_all.scale), _ptr_array(theta),
-                                    _ptr(memory), _ptr(lambda_N), _ptr(lambda_all), _ptr(dmemory), _ptr_array(dtheta),
-                                    _ptr(resnorm), _ptr(workspace), workspace.numel(), _stream_handle(stream))
-        if st != MGRIT_OK:
-            raise MgritError(st, "mgrit_adjoint_q8")
-        return lambda_all, resnorm
-    entry = lib().mgrit_adjoint_linearised if linearised else lib().mgrit_adjoint
-    st = entry(C.byref(desc), C.byref(opts), _ptr(Z_all), _ptr_array(theta), _ptr(memory),
-               _ptr(lambda_N), _ptr(lambda_all), _ptr(dmemory), _ptr_array(dtheta), _ptr(resnorm),
-               _ptr(workspace), workspace.numel(), _stream_handle(stream))
+    name = "mgrit_adjoint_q8" if q8 else "mgrit_adjoint_linearised" if linearised else "mgrit_adjoint"
+    states = (_ptr(Z_all.q), _ptr(Z_all.scale)) if q8 else (_ptr(Z_all),)
+    st = getattr(lib(), name)(C.byref(desc), C.byref(opts), *states, _ptr_array(theta), _ptr(memory),
+                              _ptr(lambda_N), _ptr(lambda_all), _ptr(dmemory), _ptr_array(dtheta), _ptr(resnorm),
+                              _ptr(workspace), workspace.numel(), handle)
     if st != MGRIT_OK:
-        raise MgritError(st, "mgrit_adjoint_linearised" if linearised else "mgrit_adjoint")
+        raise MgritError(st, name)
+    if other is not None:
+        _in_use(other, Z_all, *theta, memory, lambda_N, lambda_all, dmemory, *(dtheta or ()), resnorm, workspace)
     return lambda_all, resnorm
 
 
@@ -831,6 +829,12 @@ def _new(shape, dtype: torch.dtype, device: torch.device, other: Optional[torch.
         return torch.empty(*shape, dtype=dtype, device=device)          # (a tuple as it is takes 0.8 us longer)
     with torch.cuda.stream(other):
         return torch.empty(*shape, dtype=dtype, device=device)
+
+
+def _new_zeros(n: int, device: torch.device, other: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """fp32 zeros, filled on the stream the call is enqueued on."""
+    with torch.cuda.stream(other):
+        return torch.zeros(n, dtype=torch.float32, device=device)
 
 
 def _new_q8(shape, device: torch.device, other: Optional[torch.cuda.Stream]) -> Q8Rows:

@@ -1,5 +1,7 @@
 """The adjoint from states that were kept in 8 bits: bit-identical to the adjoint on the unpacked states, with and without
 the linearisation cache, and a whole training step with the last LayerNorm and kept rows."""
+import types
+
 import numpy as np
 import pytest
 import torch
@@ -161,3 +163,65 @@ def test_captured_calls_replay_bit_identically(cache):
                 assert torch.equal(p, q), f"replay {rep}"
     finally:
         mb.mgrit_set_adjoint_cache(True)
+
+
+@pytest.mark.parametrize("cache", [True, False])
+@pytest.mark.parametrize("form", ["kept", "unpacked"])
+def test_another_stream_than_the_current_one(form, cache):
+    """stream=: outputs and workspace are the call's own and belong to its stream, operands are kept for it.  First the other
+    stream is held up, so that the call has returned, its temporaries are gone and their memory is asked for again before
+    it runs; then the current one, so that nothing of the call may wait there."""
+    print(f"[case] adjoint on another stream, {form}, cache={cache}", flush=True)
+    wl = model(wls.ARCH_CROSS, wls.DTYPE_F32, 96, 8, 2)
+    dm = DeviceModel(wl, weight_std=0.05, keep_host=False)
+    opts = mb.mgrit_opts(wl.N, wl.h, wl.cf, wl.levels, wl.iters)
+    memory, lamN = dev(wls.cross_memory(wl)), dev(wls.terminal_adjoint(wl))
+    Z, _ = mb.mgrit_forward(dm.desc, opts, dev(wls.initial_state(wl)), dm.blocks, memory=memory)
+    z8 = mb.mgrit_q8_pack(Z)
+    copy = lambda t: mb.Q8Rows(t.q.clone(), t.scale.clone(), t.cols) if isinstance(t, mb.Q8Rows) else t.clone()  # noqa: E731
+    states = z8 if form == "kept" else Z
+
+    def adjoint(stream):
+        """On copies of the operands that go when this returns."""
+        g = [torch.zeros(mb.grad_layout(dm.desc).block_bytes, dtype=torch.uint8, device="cuda") for _ in range(wl.N)]
+        args = copy(states), [copy(b) for b in dm.blocks], copy(lamN), copy(memory)
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                torch.cuda._sleep(100_000_000)
+        lam, res = mb.mgrit_adjoint(dm.desc, opts, *args[:3], memory=args[3], dtheta=g, stream=stream)
+        return [lam, res, *g]
+
+    mb.mgrit_set_adjoint_cache(cache)
+    try:
+        want = adjoint(None)
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        s = torch.cuda.Stream()
+        need = (mb.mgrit_adjoint_q8_workspace_bytes if form == "kept" else mb.mgrit_workspace_bytes)(dm.desc, opts, 2)
+        got = adjoint(s)
+        sizes = [need, *[t.numel() * t.element_size() for t in (Z, lamN, memory, z8.q, z8.scale, *dm.blocks)]]
+        junk = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes]
+        torch.cuda.synchronize()
+        assert all(bool((j == 255).all()) for j in junk)
+        for p, q in zip(got, want):
+            assert torch.equal(p, q)
+        torch.cuda._sleep(100_000_000)                     # the current stream
+        lam, res = mb.mgrit_adjoint(dm.desc, opts, states, dm.blocks, lamN, memory=memory, stream=s)
+        s.synchronize()
+        torch.cuda.synchronize()
+        assert torch.equal(lam, want[0]) and torch.equal(res, want[1])
+    finally:
+        mb.mgrit_set_adjoint_cache(True)
+
+
+def test_adjoint_on_a_stream_of_another_device_is_refused():
+    print("[case] adjoint on a stream of another device", flush=True)
+    wl = model(wls.ARCH_ENCODER, wls.DTYPE_F32, 64, 8, 2)
+    dm = DeviceModel(wl, keep_host=False)
+    opts = mb.mgrit_opts(wl.N, wl.h, wl.cf, wl.levels, wl.iters)
+    Z, lamN = dev(np.zeros((wl.N + 1, wl.tokens, wl.d_model))), dev(wls.terminal_adjoint(wl))
+    other = types.SimpleNamespace(device_index=torch.cuda.current_device() + 1, cuda_stream=0)
+    for states in (Z, mb.mgrit_q8_pack(Z)):
+        with pytest.raises(ValueError, match="current device"):
+            mb.mgrit_adjoint(dm.desc, opts, states, dm.blocks, lamN, stream=other)
