@@ -428,28 +428,30 @@ def mgrit_forward(desc: ModelDesc, opts: Opts, Z0: torch.Tensor, theta: List[tor
     _check_state(Z0, (T, d), "Z0")
     if len(theta) != opts.N:
         raise ValueError("theta must hold N blocks")
+    handle, other = _on(stream, Z0.get_device())
     if Z_all is None:
-        Z_all = torch.empty((opts.N + 1, T, d), dtype=torch.float32, device=Z0.device)
+        Z_all = _new((opts.N + 1, T, d), torch.float32, Z0.device, other)
     _check_state(Z_all, (opts.N + 1, T, d), "Z_all")
     if resnorm is None:
-        resnorm = torch.zeros(max(opts.iters, 1), dtype=torch.float32, device=Z0.device)
+        resnorm = _new_zeros(max(opts.iters, 1), Z0.device, other)
     if workspace is None:
         need = (mgrit_workspace_bytes(desc, opts, False) if adjoint_workspace is None else
                 mgrit_linearising_workspace_bytes(desc, opts))
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=Z0.device)
+        workspace = _new((max(need, 256),), torch.uint8, Z0.device, other)
     if adjoint_workspace is not None:
         st = lib().mgrit_forward_linearising(C.byref(desc), C.byref(opts), _ptr(Z0), _ptr_array(theta), _ptr(memory),
                                              _ptr(Z_all), _ptr(resnorm), _ptr(workspace), workspace.numel(),
                                              _ptr(adjoint_workspace), adjoint_workspace.numel(),
-                                             int(bool(with_gradients)), _stream_handle(stream))
+                                             int(bool(with_gradients)), handle)
         if st != MGRIT_OK:
             raise MgritError(st, "mgrit_forward_linearising")
-        return Z_all, resnorm
-    st = lib().mgrit_forward(C.byref(desc), C.byref(opts), _ptr(Z0), _ptr_array(theta), _ptr(memory),
-                             _ptr(Z_all), _ptr(resnorm), _ptr(workspace), workspace.numel(),
-                             _stream_handle(stream))
-    if st != MGRIT_OK:
-        raise MgritError(st, "mgrit_forward")
+    else:
+        st = lib().mgrit_forward(C.byref(desc), C.byref(opts), _ptr(Z0), _ptr_array(theta), _ptr(memory),
+                                 _ptr(Z_all), _ptr(resnorm), _ptr(workspace), workspace.numel(), handle)
+        if st != MGRIT_OK:
+            raise MgritError(st, "mgrit_forward")
+    if other is not None:
+        _in_use(other, Z0, *theta, memory, Z_all, resnorm, workspace, adjoint_workspace)
     return Z_all, resnorm
 
 
@@ -517,14 +519,17 @@ def layer_step_batched(desc: ModelDesc, adjoint: bool, inputs: List[torch.Tensor
     T, d = desc.batch * desc.seq, desc.d_model
     for t in list(inputs) + list(outputs) + list(lin_state or []) + list(rhs or []):
         _check_state(t, (T, d), "state")
+    handle, other = _on(stream, inputs[0].get_device() if inputs else torch.cuda.current_device())
     need = mgrit_layer_step_workspace_bytes(desc, adjoint, G)
     if workspace is None:
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=inputs[0].device)
+        workspace = _new((max(need, 256),), torch.uint8, inputs[0].device, other)
     st = lib().layer_step_batched(C.byref(desc), int(adjoint), G, _ptr_array(inputs), _ptr_array(outputs),
                                   _ptr_array(theta), _ptr_array(lin_state), _ptr_array(rhs), _ptr(memory),
-                                  float(hstep), _ptr(workspace), workspace.numel(), _stream_handle(stream))
+                                  float(hstep), _ptr(workspace), workspace.numel(), handle)
     if st != MGRIT_OK:
         raise MgritError(st, "layer_step_batched")
+    if other is not None:
+        _in_use(other, *inputs, *outputs, *theta, *(lin_state or ()), *(rhs or ()), memory, workspace)
     return outputs
 
 
@@ -545,11 +550,14 @@ def layer_step_batched_static(desc: ModelDesc, adjoint: bool, inputs: List[torch
     T, d = desc.batch * desc.seq, desc.d_model
     for t in list(inputs) + list(outputs) + list(lin_state or []) + list(rhs or []):
         _check_state(t, (T, d), "state")
+    handle, other = _on(stream, inputs[0].get_device() if inputs else torch.cuda.current_device())
     st = lib().layer_step_batched_static(C.byref(desc), int(adjoint), G, _ptr_array(inputs), _ptr_array(outputs),
                                          _ptr_array(theta), _ptr_array(lin_state), _ptr_array(rhs), _ptr(memory),
-                                         float(hstep), _stream_handle(stream))
+                                         float(hstep), handle)
     if st != MGRIT_OK:
         raise MgritError(st, "layer_step_batched_static")
+    if other is not None:
+        _in_use(other, *inputs, *outputs, *theta, *(lin_state or ()), *(rhs or ()), memory)
     return outputs
 
 
@@ -573,23 +581,25 @@ def mgrit_forward_buffered(desc: ModelDesc, opts: Opts, buf: BufferOpts, Z0: tor
     _check_state(Z0, (T, d), "Z0")
     if len(theta) != n:
         raise ValueError("theta must hold n_open + N + n_close blocks")
-    Z_all = torch.empty((n + 1, T, d), dtype=torch.float32, device=Z0.device)
-    resnorm = torch.zeros(max(opts.iters, 1), dtype=torch.float32, device=Z0.device)
-    ws = torch.empty(max(mgrit_buffered_workspace_bytes(desc, opts, buf, 0), 256), dtype=torch.uint8, device=Z0.device)
+    handle, other = _on(stream, Z0.get_device())
+    Z_all = _new((n + 1, T, d), torch.float32, Z0.device, other)
+    resnorm = _new_zeros(max(opts.iters, 1), Z0.device, other)
+    ws = _new((max(mgrit_buffered_workspace_bytes(desc, opts, buf, 0), 256),), torch.uint8, Z0.device, other)
     if adjoint_workspace is not None:
         st = lib().mgrit_forward_buffered_linearising(C.byref(desc), C.byref(opts), C.byref(buf), _ptr(Z0),
                                                       _ptr_array(theta), _ptr(memory), _ptr(Z_all), _ptr(resnorm),
                                                       _ptr(ws), ws.numel(), _ptr(adjoint_workspace),
                                                       adjoint_workspace.numel(), int(bool(with_gradients)),
-                                                      _stream_handle(stream))
+                                                      handle)
         if st != MGRIT_OK:
             raise MgritError(st, "mgrit_forward_buffered_linearising")
-        return Z_all, resnorm
-    st = lib().mgrit_forward_buffered(C.byref(desc), C.byref(opts), C.byref(buf), _ptr(Z0), _ptr_array(theta),
-                                      _ptr(memory), _ptr(Z_all), _ptr(resnorm), _ptr(ws), ws.numel(),
-                                      _stream_handle(stream))
-    if st != MGRIT_OK:
-        raise MgritError(st, "mgrit_forward_buffered")
+    else:
+        st = lib().mgrit_forward_buffered(C.byref(desc), C.byref(opts), C.byref(buf), _ptr(Z0), _ptr_array(theta),
+                                          _ptr(memory), _ptr(Z_all), _ptr(resnorm), _ptr(ws), ws.numel(), handle)
+        if st != MGRIT_OK:
+            raise MgritError(st, "mgrit_forward_buffered")
+    if other is not None:
+        _in_use(other, Z0, *theta, memory, Z_all, resnorm, ws, adjoint_workspace)
     return Z_all, resnorm
 
 
@@ -606,18 +616,21 @@ def mgrit_adjoint_buffered(desc: ModelDesc, opts: Opts, buf: BufferOpts, Z_all: 
     _check_state(lambda_N, (T, d), "lambda_N")
     if len(theta) != n or (dtheta is not None and len(dtheta) != n):
         raise ValueError("theta / dtheta must hold n_open + N + n_close blocks")
-    lambda_all = torch.empty_like(Z_all)
-    resnorm = torch.zeros(max(opts.iters, 1), dtype=torch.float32, device=Z_all.device)
+    handle, other = _on(stream, Z_all.get_device())
+    lambda_all = _new(Z_all.shape, torch.float32, Z_all.device, other)
+    resnorm = _new_zeros(max(opts.iters, 1), Z_all.device, other)
     if linearised and workspace is None:
         raise ValueError("linearised: pass the adjoint workspace that the forward call filled")
     need = mgrit_buffered_workspace_bytes(desc, opts, buf, 2 if dtheta is not None else 1)
-    ws = workspace if workspace is not None else torch.empty(max(need, 256), dtype=torch.uint8, device=Z_all.device)
+    ws = workspace if workspace is not None else _new((max(need, 256),), torch.uint8, Z_all.device, other)
     entry = lib().mgrit_adjoint_buffered_linearised if linearised else lib().mgrit_adjoint_buffered
     st = entry(C.byref(desc), C.byref(opts), C.byref(buf), _ptr(Z_all), _ptr_array(theta),
                _ptr(memory), _ptr(lambda_N), _ptr(lambda_all), None, _ptr_array(dtheta),
-               _ptr(resnorm), _ptr(ws), ws.numel(), _stream_handle(stream))
+               _ptr(resnorm), _ptr(ws), ws.numel(), handle)
     if st != MGRIT_OK:
         raise MgritError(st, "mgrit_adjoint_buffered_linearised" if linearised else "mgrit_adjoint_buffered")
+    if other is not None:
+        _in_use(other, Z_all, *theta, memory, lambda_N, lambda_all, *(dtheta or ()), resnorm, ws)
     return lambda_all, resnorm
 
 
@@ -642,28 +655,30 @@ def mgrit_forward_stacked(desc: ModelDesc, opts: Opts, n_enc: int, Z0: torch.Ten
     _check_state(Z0, (T, d), "Z0")
     if len(theta) != opts.N:
         raise ValueError("theta must hold N blocks")
+    handle, other = _on(stream, Z0.get_device())
     if Z_all is None:
-        Z_all = torch.empty((opts.N + 1, T, d), dtype=torch.float32, device=Z0.device)
+        Z_all = _new((opts.N + 1, T, d), torch.float32, Z0.device, other)
     _check_state(Z_all, (opts.N + 1, T, d), "Z_all")
     if resnorm is None:
-        resnorm = torch.zeros(max(opts.iters, 1), dtype=torch.float32, device=Z0.device)
+        resnorm = _new_zeros(max(opts.iters, 1), Z0.device, other)
     if workspace is None:
-        workspace = torch.empty(max(mgrit_stacked_workspace_bytes(desc, opts, n_enc, 0), 256), dtype=torch.uint8,
-                                device=Z0.device)
+        need = mgrit_stacked_workspace_bytes(desc, opts, n_enc, 0)
+        workspace = _new((max(need, 256),), torch.uint8, Z0.device, other)
     if adjoint_workspace is not None:
         st = lib().mgrit_forward_stacked_linearising(C.byref(desc), C.byref(opts), int(n_enc), _ptr(Z0),
                                                      _ptr_array(theta), _ptr(Z_all), _ptr(resnorm), _ptr(workspace),
                                                      workspace.numel(), _ptr(adjoint_workspace),
                                                      adjoint_workspace.numel(), int(bool(with_gradients)),
-                                                     _stream_handle(stream))
+                                                     handle)
         if st != MGRIT_OK:
             raise MgritError(st, "mgrit_forward_stacked_linearising")
-        return Z_all, resnorm
-    st = lib().mgrit_forward_stacked(C.byref(desc), C.byref(opts), int(n_enc), _ptr(Z0), _ptr_array(theta),
-                                     _ptr(Z_all), _ptr(resnorm), _ptr(workspace), workspace.numel(),
-                                     _stream_handle(stream))
-    if st != MGRIT_OK:
-        raise MgritError(st, "mgrit_forward_stacked")
+    else:
+        st = lib().mgrit_forward_stacked(C.byref(desc), C.byref(opts), int(n_enc), _ptr(Z0), _ptr_array(theta),
+                                         _ptr(Z_all), _ptr(resnorm), _ptr(workspace), workspace.numel(), handle)
+        if st != MGRIT_OK:
+            raise MgritError(st, "mgrit_forward_stacked")
+    if other is not None:
+        _in_use(other, Z0, *theta, Z_all, resnorm, workspace, adjoint_workspace)
     return Z_all, resnorm
 
 
@@ -680,20 +695,23 @@ def mgrit_adjoint_stacked(desc: ModelDesc, opts: Opts, n_enc: int, Z_all: torch.
     _check_state(lambda_N, (T, d), "lambda_N")
     if len(theta) != opts.N or (dtheta is not None and len(dtheta) != opts.N):
         raise ValueError("theta / dtheta must hold N blocks")
+    handle, other = _on(stream, Z_all.get_device())
     if lambda_all is None:
-        lambda_all = torch.empty_like(Z_all)
+        lambda_all = _new(Z_all.shape, torch.float32, Z_all.device, other)
     _check_state(lambda_all, (opts.N + 1, T, d), "lambda_all")
     if resnorm is None:
-        resnorm = torch.zeros(max(opts.iters, 1), dtype=torch.float32, device=Z_all.device)
+        resnorm = _new_zeros(max(opts.iters, 1), Z_all.device, other)
     if workspace is None:
         need = mgrit_stacked_workspace_bytes(desc, opts, n_enc, 2 if dtheta is not None else 1)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=Z_all.device)
+        workspace = _new((max(need, 256),), torch.uint8, Z_all.device, other)
     entry = lib().mgrit_adjoint_stacked_linearised if linearised else lib().mgrit_adjoint_stacked
     st = entry(C.byref(desc), C.byref(opts), int(n_enc), _ptr(Z_all), _ptr_array(theta),
                _ptr(lambda_N), _ptr(lambda_all), _ptr_array(dtheta), _ptr(resnorm),
-               _ptr(workspace), workspace.numel(), _stream_handle(stream))
+               _ptr(workspace), workspace.numel(), handle)
     if st != MGRIT_OK:
         raise MgritError(st, "mgrit_adjoint_stacked_linearised" if linearised else "mgrit_adjoint_stacked")
+    if other is not None:
+        _in_use(other, Z_all, *theta, lambda_N, lambda_all, *(dtheta or ()), resnorm, workspace)
     return lambda_all, resnorm
 
 
