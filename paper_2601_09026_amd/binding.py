@@ -468,6 +468,8 @@ def mgrit_adjoint(desc: ModelDesc, opts: Opts, Z_all, theta: List[torch.Tensor],
     Z_all may be Q8Rows of that shape, mgrit_q8_pack(Z_all): mgrit_adjoint_q8 (workspace:
     mgrit_adjoint_q8_workspace_bytes).
     stream: where the call is enqueued, behind what the caller has put before it there; what is allocated here belongs to it."""
+    if linearised and workspace is None:
+        raise ValueError("linearised: pass the adjoint workspace that the forward call filled")
     T, d = desc.batch * desc.seq, desc.d_model
     q8 = isinstance(Z_all, Q8Rows)
     if q8:
@@ -495,8 +497,6 @@ def mgrit_adjoint(desc: ModelDesc, opts: Opts, Z_all, theta: List[torch.Tensor],
     need = query(desc, opts, 2 if (dtheta is not None or dmemory is not None) else 1)
     if workspace is None:
         workspace = _new((max(need, 256),), torch.uint8, Z_all.device, other)
-    if linearised and workspace is None:
-        raise ValueError("linearised: pass the adjoint workspace that the forward call filled")
     name = "mgrit_adjoint_q8" if q8 else "mgrit_adjoint_linearised" if linearised else "mgrit_adjoint"
     states = (_ptr(Z_all.q), _ptr(Z_all.scale)) if q8 else (_ptr(Z_all),)
     st = getattr(lib(), name)(C.byref(desc), C.byref(opts), *states, _ptr_array(theta), _ptr(memory),
@@ -610,6 +610,8 @@ def mgrit_adjoint_buffered(desc: ModelDesc, opts: Opts, buf: BufferOpts, Z_all: 
                            linearised: bool = False):
     """Returns (lambda_all, resnorm) of the buffered network; dtheta as in mgrit_adjoint.
     linearised: mgrit_adjoint_buffered_linearised on the workspace the forward call filled."""
+    if linearised and workspace is None:
+        raise ValueError("linearised: pass the adjoint workspace that the forward call filled")
     T, d = desc.batch * desc.seq, desc.d_model
     n = buf.n_open + opts.N + buf.n_close
     _check_state(Z_all, (n + 1, T, d), "Z_all")
@@ -619,8 +621,6 @@ def mgrit_adjoint_buffered(desc: ModelDesc, opts: Opts, buf: BufferOpts, Z_all: 
     handle, other = _on(stream, Z_all.get_device())
     lambda_all = _new(Z_all.shape, torch.float32, Z_all.device, other)
     resnorm = _new_zeros(max(opts.iters, 1), Z_all.device, other)
-    if linearised and workspace is None:
-        raise ValueError("linearised: pass the adjoint workspace that the forward call filled")
     need = mgrit_buffered_workspace_bytes(desc, opts, buf, 2 if dtheta is not None else 1)
     ws = workspace if workspace is not None else _new((max(need, 256),), torch.uint8, Z_all.device, other)
     entry = lib().mgrit_adjoint_buffered_linearised if linearised else lib().mgrit_adjoint_buffered
@@ -690,6 +690,8 @@ def mgrit_adjoint_stacked(desc: ModelDesc, opts: Opts, n_enc: int, Z_all: torch.
     """Returns (lambda_all, resnorm) of the stacked grid; dtheta as in mgrit_adjoint (encoder
     layers' blocks in the encoder's fp32 layout, decoder layers' in the decoder's).
     linearised: mgrit_adjoint_stacked_linearised on the workspace the forward call filled."""
+    if linearised and workspace is None:
+        raise ValueError("linearised: pass the adjoint workspace that the forward call filled")
     T, d = desc.batch * (desc.mem_seq + desc.seq), desc.d_model
     _check_state(Z_all, (opts.N + 1, T, d), "Z_all")
     _check_state(lambda_N, (T, d), "lambda_N")

@@ -309,3 +309,17 @@ def test_workspace_grows_with_groups_and_levels():
     two = mb.mgrit_workspace_bytes(desc, mb.mgrit_opts(64, 1 / 64, 4, 2, 2), False)
     three = mb.mgrit_workspace_bytes(desc, mb.mgrit_opts(64, 1 / 64, 4, 3, 2), False)
     assert three > two
+
+
+def test_linearised_adjoints_want_the_forward_calls_workspace():
+    """A workspace made by the adjoint call itself would hold no linearisation: without the one that the forward solve filled, the
+    call is refused, before it looks at a tensor."""
+    wl = wls.named_workloads()["tiny_encoder"]
+    desc, opts = mb.model_desc(wl), mb.mgrit_opts(wl.N, wl.h, wl.cf, wl.levels, wl.iters)
+    sw = wls.named_workloads()["mt_decoder"]
+    ddesc, dopts = mb.model_desc(sw), mb.mgrit_opts(32, 1 / 32, 4, 2, 2)
+    for f in (lambda: mb.mgrit_adjoint(desc, opts, None, [], None, linearised=True),
+              lambda: mb.mgrit_adjoint_buffered(desc, opts, mb.BufferOpts(0, 0, 0.0), None, [], None, linearised=True),
+              lambda: mb.mgrit_adjoint_stacked(ddesc, dopts, 16, None, [], None, linearised=True)):
+        with pytest.raises(ValueError, match="linearised: pass the adjoint workspace"):
+            f()
