@@ -150,7 +150,7 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
   STCHK(check_rows(rows, out_features, dy, dy_stride, dy_dtype));
   if (rows && dy_stride > MOST_FEATURES) return MGRIT_UNSUPPORTED;        // a tile's offsets have 32 bits
   STCHK(check_q8(rows, x_q8, x_q8_scale));
-  if (!dW || !aligned(dW, 4) || !aligned(db, 4) || !isfinite(scale)) return MGRIT_INVALID_ARG;
+  if (!dW || !aligned(dW, 4) || !aligned(db, 4) || dW == db || !isfinite(scale)) return MGRIT_INVALID_ARG;
   STCHK(check_workspace(mgrit_q8_weight_grad_workspace_bytes(rows, out_features, in_features, dy_dtype), workspace, workspace_bytes));
   std::lock_guard<std::recursive_mutex> call_lock(call_mutex());
   Q8GradArgs a = {};

@@ -179,3 +179,10 @@ def test_binding_names_what_is_of_the_wrong_kind():
                     (lambda: mb.mgrit_q8_weight_grad(x8, x8), "tensor, got Q8Rows")):
         with pytest.raises(ValueError, match=kind):
             f()
+
+
+def test_weight_grad_refuses_one_array_for_two_results():
+    def call(dW, db, rows=4):
+        return mb.lib().mgrit_q8_weight_grad(rows, 24, 1, 0, P, 24, 2 * P, 3 * P, 1.0, dW, db, 6 * P, 1 << 24, None)
+    # (one input feature: dW and db have the same size)
+    assert call(4 * P, 4 * P) == INVALID and call(4 * P, 4 * P, rows=0) == INVALID
