@@ -389,8 +389,8 @@ int mgrit_q8_unpack(int64_t rows, int32_t cols, int dtype, const void* q, const 
  *   x_q8, x_q8_scale   optional out: the 8-bit rows of x, as mgrit_q8_pack writes them, from the same pass
  *   y_q8, y_q8_scale   optional out: the 8-bit rows of y (of the values stored in y)
  * y may be x itself (same type and stride).  A row with a NaN or an infinity has NaN in y, and in rstd; others are not
- * touched by it.  Sums are fp32: a row whose sum of squared differences passes its range (differences beyond 1e19) has an
- * rstd of 0. */
+ * touched by it.  Sums are fp32: a finite row whose sum of squared differences passes its range (differences beyond 1e19)
+ * has its mean, an rstd of 0 and y = beta (and in the backward pass an xhat and a dx of 0). */
 typedef struct mgrit_norm_desc {
   int64_t rows;
   int32_t cols;

@@ -249,8 +249,49 @@ __global__ void __launch_bounds__(block_threads<LPR>()) norm_forward_kernel(cons
       rest += mu - own;
       m2 = sq;
     }
-    // (a row with a NaN, or with an infinity, has NaN throughout)
-    const float rstd = 1.0f / sqrtf(m2 * n + a.eps);
+    float rstd = 1.0f / sqrtf(m2 * n + a.eps);
+    if (__builtin_expect(__any(!(rstd > 0.f)), 0)) {
+      // A row with a NaN or an infinity, which has NaN throughout; or a finite one whose sums pass fp32's range.  Of such a
+      // row a 2^16th is summed up again: 2^14 differences of a 2^16th of any two numbers stay inside.  Its mean is right
+      // then; where the sum of squares itself is past the range, rstd is 0 and y is beta.  (Rows of one wavefront go
+      // through it together; of a row of several wavefronts all know the same rstd.)
+      const bool past = !(rstd > 0.f);
+      Row<TX, LPR, NV, TINY> again;
+      again.load(x + row * a.ldx, lane, cols);           // (in place as well: it is stored further down)
+      f32x4 w[NV];
+      float all = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        w[i] = again.value(i, lane, cols) * 0x1p-16f;
+        all += sum4(w[i]);
+      }
+      row_sums<LPR>(all, none, exchange);
+      const float base = rounded_product(all, n);
+      float left = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        w[i] = w[i] - base;
+        if (i == NV - 1) w[i] = inside(w[i], (i * LPR + lane) * 4, cols);
+        left += sum4(w[i]);
+      }
+      row_sums<LPR>(left, none, exchange);
+      const float shift = left / (float)cols;            // (exact for a row of one value, a product may not be)
+      float sq = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        w[i] = (w[i] - shift) * 0x1p16f;
+        if (i == NV - 1) w[i] = inside(w[i], (i * LPR + lane) * 4, cols);
+        sq += dot4(w[i], w[i]);
+      }
+      row_sums<LPR>(sq, none, exchange);
+      const bool mend = past && __builtin_isfinite(all);
+      mu = mend ? (base + shift) * 0x1p16f : mu;
+      rest = mend ? 0.f : rest;
+      rstd = mend ? 1.0f / sqrtf(sq * n + a.eps) : rstd;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)                       // (with a wavefront to itself, a NaN's row needs no values: registers)
+        if (LPR >= 64 || mend) v[i] = sq < __builtin_inff() ? w[i] : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     if (live && lane == 0) {
       if (a.mean) a.mean[row] = mu;
       if (a.rstd) a.rstd[row] = rstd;
@@ -301,11 +342,11 @@ __global__ void __launch_bounds__(block_threads<LPR>()) norm_backward_kernel(con
     float mu, rstd;
   } ring[AHEAD + 1];
   auto load = [&](Rows2& f, long row) {
+    f.mu = a.mean[row];                                  // (first: both are needed for the row's first element)
+    f.rstd = a.rstd[row];
     if constexpr (std::is_same<TX, Kept>::value) f.x.load(a.xq + row * a.blocks * Q8_BLOCK, a.xs + row * a.blocks, lane, a.blocks);
     else f.x.load(static_cast<const TX*>(a.x) + row * a.ldx, lane, cols);
     f.dy.load(static_cast<const TY*>(a.dy) + row * a.ldy, lane, cols);
-    f.mu = a.mean[row];
-    f.rstd = a.rstd[row];
   };
 #pragma unroll
   for (int k = 0; k < AHEAD; ++k) load(ring[k], at(k));
@@ -317,10 +358,11 @@ __global__ void __launch_bounds__(block_threads<LPR>()) norm_backward_kernel(con
     const long row = at(t);
     f32x4 x[NV], dy[NV];
     float s1 = 0.f, s2 = 0.f;
+    const float mu = f.rstd == 0.f ? 0.f : f.mu;         // (past fp32's range x - mu may be infinite, and 0 times it NaN)
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * LPR + lane) * 4;
-      x[i] = (f.x.value(i, lane, cols) - f.mu) * f.rstd;
+      x[i] = (f.x.value(i, lane, cols) - mu) * f.rstd;
       if (i == NV - 1) x[i] = inside(x[i], c, cols);
       dy[i] = f.dy.value(i, lane, cols);
       if (live) {

@@ -794,3 +794,95 @@ def test_the_longest_rows(cols, dtype):
     assert again.scale.shape == (1, blocks) and (again.scale == 127).all() and torch.equal(again.q, x8.q)
     del x8, x, store, again
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------ finite rows past fp32's range
+MOST = float(torch.finfo(F32).max)
+
+
+def far_out(cols, dtype):
+    """Finite rows whose sums, differences or squares pass fp32's range, whatever their length, and ordinary ones between them.
+    Returns (x, the rows that are far out and flat, far out and not flat)."""
+    x = rand(cols, 19, cols, spread=2.0)
+    most = MOST if dtype == F32 else float(torch.finfo(BF16).max)
+    g = rand(7, cols)
+    x[1] = 1e38 + 1e37 * g.clamp(-9, 9)                    # one sign: the sum
+    x[3] = -x[1]
+    x[4] = 3e38 * g.clamp(-1, 1)                           # both: differences
+    x[6] = most
+    x[7] = -most
+    x[9] = most * torch.where(torch.arange(cols, device="cuda") % 2 == 0, 1.0, -1.0)
+    x[10] = 0.0
+    x[10, cols // 2] = 2.5e38                              # one large value
+    x[12] = 1e30
+    x[13] = 1e30 * g
+    x[15] = 1e24 * g + 1e25
+    x[16, 0] = -most
+    steep = [1, 3, 4, 9, 10, 13, 15, 16]
+    return x.to(dtype), [6, 7, 12] + (steep if cols == 1 else []), [] if cols == 1 else steep
+
+
+@pytest.mark.parametrize("x_dtype,y_dtype", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("cols", [1, 2, 3, 4, 33, 64, 100, 128, 129, 768, 1000, 2050, 4096, 5000, 8192, 8200, 16383, 16384])
+def test_norm_of_finite_rows_past_the_range(cols, x_dtype, y_dtype):
+    """Such a row has its mean, an rstd of 0 and y = beta (a flat one: its own rstd); NaNs come from NaNs and infinities only.
+    And back: its xhat is 0, so that dx is 0 and dgamma that of the other rows."""
+    say("norm of far rows", cols, x_dtype, y_dtype)
+    gamma, beta = rand(3, cols, offset=1.0), rand(4, cols)
+    x, flat, steep = far_out(cols, x_dtype)
+    near = [r for r in range(19) if r not in flat + steep]
+    kx, ky = mb.q8_empty(x.shape), mb.q8_empty(x.shape)
+    y, mean, rstd = mb.mgrit_layer_norm_forward(x, gamma, beta, y_dtype=y_dtype, x_q8=kx, y_q8=ky)
+    same_rows(kx, kept(x))
+    same_rows(ky, kept(y))
+    xs = n64(x)
+    # the mean's bound is that of ordinary rows: its sums are of numbers scaled by a power of two
+    ref, spread = xs.mean(1), np.abs(xs - xs.mean(1, keepdims=True)).mean(1)
+    close(mean, ref, 1.01 * U * (3 * np.abs(ref) + 50 * spread), "mean")
+    assert (rstd[steep] == 0).all()
+    assert torch.equal(rstd[flat], mb.mgrit_layer_norm_forward(torch.zeros_like(x), gamma, beta)[2][:len(flat)])
+    for r in flat + steep:
+        assert torch.equal(y[r], beta.to(y_dtype)), r
+    alone = mb.mgrit_layer_norm_forward(x[near].contiguous(), gamma, beta, y_dtype=y_dtype)
+    for got, want in zip((y, mean, rstd), alone):
+        assert torch.equal(got[near], want)
+    if x_dtype == y_dtype:                                 # in place: the row is read again before it is written
+        z = x.clone()
+        assert torch.equal(mb.mgrit_layer_norm_forward(z, gamma, beta, y=z)[0], y)
+    # backward, from x and from its 8-bit rows (not those whose blocks stand for NaNs, nor flat ones, which are flat no more)
+    dy = rand(5, 19, cols, dtype=y_dtype)
+    m, r = n64(mean), n64(rstd)
+    for form, value in ((x, xs), (kx, oo.q8_unpack(kx.q.cpu().numpy(), kx.scale.cpu().numpy(), cols))):
+        rows = list(range(19))
+        if form is kx:
+            rows = [i for i in rows if np.isfinite(value[i]).all() and i not in flat]
+            form = mb.Q8Rows(kx.q[rows], kx.scale[rows], cols)
+        got = mb.mgrit_layer_norm_backward(dy[rows].contiguous(), form, gamma, mean[rows].contiguous(), rstd[rows].contiguous(),
+                                           dx_dtype=x_dtype)
+        d, g = n64(dy)[rows], n64(gamma)
+        want = oo.norm_backward(d, value[rows], g, m[rows], r[rows])
+        xhat, gd = np.abs((value[rows] - m[rows, None]) * r[rows, None]), np.abs(d * g)
+        e_dx = r[rows, None] * U * (8 * gd + 56 * gd.mean(1, keepdims=True) + 64 * xhat * (gd * xhat).mean(1, keepdims=True))
+        close(got[0], want[0], e_dx * 1.01 + HALF_STEP[x_dtype] * (np.abs(want[0]) + e_dx), "dx")
+        close(got[1], want[1], 102 * U * (np.abs(d) * xhat).sum(0), "dgamma")
+        close(got[2], want[2], 98 * U * np.abs(d).sum(0), "dbeta")
+
+
+def test_infinities_and_nans_beside_finite_rows_past_the_range():
+    """Rows that share a wavefront: each has what it has alone."""
+    say("NaN, infinity and far rows")
+    for cols in (3, 40, 100, 768, 5000):
+        x = rand(5, 12, cols)
+        x[1], x[2, 0], x[3, cols - 1], x[4, 1], x[6] = 3e38, float("nan"), float("inf"), float("-inf"), -3e38
+        x[8, 0], x[8, 1] = float("inf"), float("-inf")
+        x[9, 0], x[9, 1] = MOST, -MOST
+        y, mean, rstd = mb.mgrit_layer_norm_forward(x)
+        bad = [2, 3, 4, 8]
+        for r in range(12):
+            one = mb.mgrit_layer_norm_forward(x[r:r + 1].contiguous())
+            if r in bad:
+                assert torch.isnan(y[r]).all() and torch.isnan(rstd[r])
+            else:
+                assert torch.isfinite(y[r]).all() and torch.isfinite(mean[r])
+                assert torch.equal(y[r], one[0][0]) and mean[r] == one[1][0] and rstd[r] == one[2][0]
+        assert (y[1] == 0).all() and (y[6] == 0).all() and rstd[9] == 0
