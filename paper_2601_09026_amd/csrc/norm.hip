@@ -445,19 +445,19 @@ __global__ void __launch_bounds__(256) norm_zero_kernel(int cols, float* dgamma,
 
 // Lanes per row and vectors per lane, by the row's length.  f(LPR, NV, TINY) is called with the three as types.
 template <int V> using Int = std::integral_constant<int, V>;
-template <int LPR, int MOST, typename F> hipError_t by_vectors(int cols, F f) {
+template <int LPR, int LEAST, int MOST, typename F> hipError_t by_vectors(int cols, F f) {
   const int nv = (cols + 4 * LPR - 1) / (4 * LPR);         // no fewer than the row needs: only the last vector is ever cut off
-  if constexpr (MOST >= 2) if (nv < MOST) return by_vectors<LPR, MOST - 1>(cols, f);
+  if constexpr (MOST > LEAST) if (nv < MOST) return by_vectors<LPR, LEAST, MOST - 1>(cols, f);
   return f(Int<LPR>{}, Int<MOST>{}, std::false_type{});
 }
 template <typename F> hipError_t by_width(int cols, F f) {
   if (cols < 4) return f(Int<16>{}, Int<1>{}, std::true_type{});
-  if (cols <= 64) return by_vectors<16, 1>(cols, f);
-  if (cols <= 128) return by_vectors<32, 1>(cols, f);
-  if (cols <= 1024) return by_vectors<64, 4>(cols, f);
-  if (cols <= 4096) return by_vectors<256, 4>(cols, f);
-  if (cols <= 8192) return by_vectors<512, 4>(cols, f);
-  return by_vectors<1024, 4>(cols, f);
+  if (cols <= 64) return by_vectors<16, 1, 1>(cols, f);
+  if (cols <= 128) return by_vectors<32, 1, 1>(cols, f);
+  if (cols <= 1024) return by_vectors<64, 1, 4>(cols, f);
+  if (cols <= 4096) return by_vectors<256, 2, 4>(cols, f);
+  if (cols <= 8192) return by_vectors<512, 3, 4>(cols, f);
+  return by_vectors<1024, 3, 4>(cols, f);
 }
 
 // Blocks of a launch.  Forward 4 per CU (32768 x 1024, bf16: 28.2 us, with 6 31.2, with 16 32; 16384 x 4096 53.2, 55.6, 72).
