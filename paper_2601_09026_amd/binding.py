@@ -853,6 +853,8 @@ def _new(shape, dtype: torch.dtype, device: torch.device, other: Optional[torch.
 
 def _new_zeros(n: int, device: torch.device, other: Optional[torch.cuda.Stream]) -> torch.Tensor:
     """fp32 zeros, filled on the stream the call is enqueued on."""
+    if other is None:
+        return torch.zeros(n, dtype=torch.float32, device=device)
     with torch.cuda.stream(other):
         return torch.zeros(n, dtype=torch.float32, device=device)
 
