@@ -227,8 +227,10 @@ int mgrit_adjoint_linearised(const mgrit_model_desc* desc, const mgrit_opts* opt
  * Everything else as in mgrit_adjoint; results are bit-identical to mgrit_adjoint on the unpacked states.  With the
  * linearisation cache the call brings all states back at its start (N*T*d_model floats of workspace more); with the cache
  * switched off (mgrit_set_adjoint_cache(0)) every launch chunk brings back those of its own layers, so that the states
- * never exist in 32 bits at one time.  Workspace: mgrit_adjoint_q8_workspace_bytes (adjoint: 1 or 2, as in
- * mgrit_workspace_bytes; 0 on invalid arguments; host only). */
+ * never exist in 32 bits at one time.  (During the call itself, kept and restored states together are a quarter of the
+ * states' bytes more than mgrit_adjoint has to hold, with the cache; without it they are less by most of them.)
+ * Workspace: mgrit_adjoint_q8_workspace_bytes (adjoint: 1 or 2, as in mgrit_workspace_bytes; 0 on invalid arguments; host
+ * only). */
 size_t mgrit_adjoint_q8_workspace_bytes(const mgrit_model_desc* desc, const mgrit_opts* opts, int adjoint);
 int mgrit_adjoint_q8(const mgrit_model_desc* desc, const mgrit_opts* opts,
                      const void* Z_q8, const void* Z_q8_scale, const void* const* theta, const void* memory,

@@ -718,6 +718,8 @@ def mgrit_adjoint_stacked(desc: ModelDesc, opts: Opts, n_enc: int, Z_all: torch.
 
 
 # ---- operators around the solves: 8-bit rows, LayerNorm of rows, gradients from 8-bit rows ------------
+# Like the solves, the operators are outside autograd: what they return has no graph behind it, also where an operand requires a
+# gradient.  A program calls the backward pass itself (or wraps both in a torch.autograd.Function).
 # (Small calls take as long as the host needs for them: what is asked of tensors below is what costs least.)
 Q8_BLOCK = 32                        # MGRIT_Q8_BLOCK of the header
 MOST_COLS = 2 ** 31 - 1              # a row's length has 32 bits in the header, and ctypes cuts what has more
@@ -947,7 +949,8 @@ def mgrit_layer_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = No
                              x_q8: Optional[Q8Rows] = None, y_q8: Optional[Q8Rows] = None,
                              stream: Optional[torch.cuda.Stream] = None):
     """Returns (y, mean, rstd): LayerNorm of the rows of x (fp32 or bf16, [..., cols]) with y of y_dtype (x's own by
-    default) and the rows' statistics, fp32 [rows].  x_q8, y_q8: 8-bit rows (q8_empty) filled from the same pass."""
+    default) and the rows' statistics, fp32 [rows].  x_q8, y_q8: 8-bit rows (q8_empty) filled from the same pass.
+    Not recorded by autograd: gradients come from mgrit_layer_norm_backward."""
     device = _device_of(x, "x")
     rows, cols, ldx = _check_rows(x, "x", device)
     handle, other = _on(stream, device)

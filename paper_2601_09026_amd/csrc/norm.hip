@@ -3,14 +3,17 @@
 //   mu = mean x,  rstd = (mean (x - mu)^2 + eps)^-1/2,  xhat = (x - mu) rstd,  y = xhat gamma + beta
 //   g = dy gamma,  dx = rstd (g - mean g - xhat mean(g xhat)),  dgamma = sum_rows dy xhat,  dbeta = sum_rows dy
 // A row lies in the registers of LPR lanes, NV vectors of 4 in each, so that it is read once; all arithmetic is fp32.  Bound
-// by moving its rows: 16384 x 4096, bf16, forward 45.6 us, 5.9 TB/s; 32768 x 768, fp32 x and bf16 dy, backward 41.4 us and
-// 4.7 for joining the partial sums, 5.5 TB/s together (a copy reaches 5.7); what goes to and comes from memory are the
-// algorithm's bytes.  Few or short rows wait for one chain of load, sums and store: 1 x 768 3.2 us, 64 x 64 backward 4.3,
-// 12608 x 384 from kept rows 11.5 where its bytes need 6.
+// by moving its rows: 16384 x 4096, bf16, forward 46.6 us, 5.8 TB/s; 32768 x 768, fp32 x and bf16 dy, backward 41.8 us and
+// 4.2 for joining the partial sums, 5.5 TB/s together (a copy reaches 5.7); what goes to and comes from memory are the
+// algorithm's bytes.  Few or short rows wait for one chain of load, sums and store: 1 x 768 3.2 us, 64 x 64 backward 4.2,
+// 12608 x 384 from kept rows 11.2 where its bytes need 6.
 // What paid: the next row's loads in flight while a row is reduced, and one exchange through LDS for a row of several
 // wavefronts instead of two (forward, 16384 x 4096, bf16, 70 -> 54 us a call; backward, 32768 x 768, 59.6 -> 53).  What did not: blocks of
 // 512 and 1024 lanes where 256 hold the row (equal); non-temporal stores of y (faster alone, slower with the kernel that
 // reads y next).
+// Rows past fp32's range are taken care of off that path, and their test costs up to 1.6 % (65536 x 64, bf16, 7.6 -> 7.7 us;
+// 16384 x 4096 47.6 -> 47.9); mean and rstd of a row loaded before the row and not behind it: 8192 x 8192, bf16, 100 -> 83 us,
+// other backward passes within 1 to 3 %.
 #include <type_traits>
 
 #include "kernels.h"
@@ -460,10 +463,14 @@ template <typename F> hipError_t by_width(int cols, F f) {
   return by_vectors<1024, 3, 4>(cols, f);
 }
 
-// Blocks of a launch.  Forward 4 per CU (32768 x 1024, bf16: 28.2 us, with 6 31.2, with 16 32; 16384 x 4096 53.2, 55.6, 72).
-// Backward 2 per CU, of more than 4 wavefronts 1 (2 and 3 of them, us: 32768 x 768, fp32 and bf16, 53.1, 55.1; 16384 x
-// 4096, bf16, 81, 94; 1 and 2: 8192 x 8192 100, 108; 4096 x 16384 141, 158): each leaves a row of partial sums.  Few rows take
-// one block, whose sums are final, and no second launch.
+// Blocks of a launch.  Forward 4 per CU (32768 x 1024, bf16: 23.3 us, with 6 24.7, with 16 26.1; 16384 x 4096 46.7, 47.1, 44.3).
+// Backward 2 per CU, of more than 4 wavefronts 1 (2 and 3 of them, us: 32768 x 768, fp32 and bf16, 43.1, 44.0; 16384 x
+// 4096, bf16, 83.9, 88.5; 1 and 2: 8192 x 8192 81.7, 89.5; 4096 x 16384 100, 113): each leaves a row of partial sums.
+// Few rows, up to 8 trips, take one block, whose sums are final, and no second launch and workspace, for which the host takes
+// longer than the block's trips: calls back to back, one block and as many as rows allow with a join, us, fp32: 64 x 64
+// 12.6, 16.5; 32 x 1024 12.8, 16.8; 8 x 4096 12.6, 16.7; 4 x 16384 13.5, 16.7.  The other way round it is where 8 rows are
+// as wide as they can be, 8 x 16384 24.1, 16.7, and in captured graphs, which hold the kernels' time alone: 64 x 64 4.8, 6.0;
+// 128 x 64 6.1, 6.0; 2 x 16384 8.7, 11.1; 32 x 1024 9.9, 6.9; 8 x 4096 11.6, 6.9; 8 x 16384 24.6, 11.7.
 constexpr int CUS = 256, FWD_BLOCKS = 4 * CUS, ONE_BLOCK_TRIPS = 8;
 int backward_blocks(long rows, int threads, int rows_per_block) {
   const long want = (rows + rows_per_block - 1) / rows_per_block, most = threads > 256 ? CUS : 2 * CUS;

@@ -16,13 +16,14 @@
 // paid, at 16384 x 4096 x 4096 in bf16: one tile of LDS stored before another is multiplied 721 us; stores, loads and
 // fragment reads between the products 731 (spilling); conversions and addresses of fewer instructions 508; wavefronts of
 // 64 x 128 instead of 128 x 64 in the block 495; db from the registers on their way to LDS and not from the fragments, shared
-// out over the columns of tiles, 503 -> 484 on another card.  What is left: the clock, 1.7 GHz under this load,
-// and of its cycles the matrix cores are busy for 58 %, LDS for 43 %; wavefronts wait for a slot to issue in for 40 % of theirs and
-// for data or the barrier for 24 %.  Loads that are waited for one by one and not at a tile's start gained nothing, nor did a swizzle that spreads the kept
+// out over the columns of tiles, 503 -> 484 on another card.  What is left: 910 k cycles of an XCD, whatever the card's clock
+// under this load (506 us at 1.80 GHz with the counters on, 539 at 1.69 on another card; 482 us are 1.89), of which the matrix
+// cores are busy for 58 %, LDS for 43 %; wavefronts wait for a slot to issue in for 40 % of theirs and
+// for data or the barrier for 25 %.  Loads that are waited for one by one and not at a tile's start gained nothing, nor did a swizzle that spreads the kept
 // rows' stores over all banks, a sixth of the LDS cycles less.  The conversions cost 511 -> 491 us for the kept rows (values wrong
 // without), and with fp32, 8192 x 4096 x 2048, 370 -> 346, and 313 without the parts of dY; a pass that did them beforehand would
 // take 36 us for its bytes in the one case, 58 in the other.  Rows of dY at odd addresses cost 3 to 12 % (16384 x 4095 x 4096;
-// 4096 x 50257 x 768, aligned to 2, 4, 8 and 16 bytes: 398, 385, 362, 355 us).
+// 4096 x 50257 x 768, aligned to 2, 4, 8 and 16 bytes, on a slow card: 398, 385, 362, 355 us; on others the first takes 343 to 358).
 #include <climits>
 #include <type_traits>
 
@@ -107,8 +108,10 @@ __device__ __forceinline__ u32x2 kept_bf16(unsigned q, float step) {
   return u32x2{upper(signed_byte<0>(q) * step, signed_byte<1>(q) * step), upper(signed_byte<2>(q) * step, signed_byte<3>(q) * step)};
 }
 
-// A thread's sums of db carry their errors, but for the largest bf16 tile, which has no 8 registers left for them (values of 8
-// bits lose little: 3e-8 of db's size after 16384 tokens, 4e-8 with the errors).
+// A thread's sums of db carry their errors, but for the largest bf16 tile, which has no 8 registers left for them.  Values of 8
+// bits lose little: 16384 tokens, 4096 x 4096, 3.7e-8 of db's size (chains of 16 tiles of 64 tokens), 131072 tokens 4.8e-8 (128),
+// and with one column of tiles, 65536 tokens, 65536 x 200, 6.4e-8 (1024), at worst 1.7e-7 of an element whose terms have one
+// sign.  Half a step of fp32 is 6e-8.
 struct PlainSum {
   float sum = 0.f;
   __device__ __forceinline__ void add(float x) { sum += x; }
@@ -451,7 +454,7 @@ __global__ void __launch_bounds__(256) q8_grad_zero_kernel(long mn, int M, float
 // J0 + J1 * slices and their bytes, fitted to 1232 launches (64 to 70001 tokens, 64 x 64 to 50257 x 768 weights, both
 // types) and within 7-10 % of them; the pick is 0.7 % slower than the best of all tiles and slices on average, 15 % at worst
 // (3000 tokens, 9000 x 130).  One piece or slices of the last round: 16384 tokens, 4096 x 1024, bf16, 372 against 151 us.  Large
-// tiles or small ones: 16384 tokens, 4096 x 4096, 470, 630, 1510 us; 2048, 384 x 384, each with its best slices, 22, 15, 11.7.
+// tiles or small ones, in one run: 16384 tokens, 4096 x 4096, 470, 630, 1510 us; 2048, 384 x 384, each with its best slices, 22, 15, 11.7.
 // CUS is a constant: the plan, and with it the order of the sums, follows from the sizes alone.
 constexpr int CUS = 256;
 struct Tile { int bm, bn, bk, per_cu; double fixed, per_token[4]; };       // us, us per 1000 tokens
