@@ -431,6 +431,75 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
                          const void* dy, int64_t dy_stride, const void* x_q8, const void* x_q8_scale, float scale,
                          float* dW, float* db, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Between a head's logits and the gradient that enters the network again.  A row of `cols` logits z (at most 2^24, and 2^31 - 1
+ * rows: MGRIT_UNSUPPORTED beyond) is a distribution over ids 0 .. cols-1:
+ *   p = softmax(z / temperature),  lse = ln sum exp(z / temperature),  ln p_i = z_i / temperature - lse,
+ *   entropy H = - sum p_i ln p_i
+ * Ids are 32- or 64-bit integers (id_dtype), contiguous.  Values are fp32, contiguous, and computed in fp32; dlogits has the logits'
+ * type, rounded once, and may be the logits themselves (same stride), which it then replaces.
+ *   A logit of -infinity is a masked one: p = 0.  A finite one whose quotient by the temperature passes fp32's range counts as infinite.
+ *   A row of -infinity alone has no distribution: lse and every log probability -infinity, entropy 0, gradient 0.
+ *   A row with a NaN or +infinity has NaN for all its values and its gradient, and -1 for its alternatives' ids.
+ * Work that a given row needs nothing of (no token, no teacher) leaves zeros whatever the row holds.
+ *
+ * Log probabilities of given tokens, with entropy and the most likely alternatives:
+ *   tokens             device [rows]; below 0: the row has none, its log probability is 0 and no gradient goes through it;
+ *                      cols and more: NaN for both.  May be NULL if logprob is
+ *   logprob, entropy   device [rows] out, each may be NULL, as lse; the backward pass takes lse, and entropy with g_entropy
+ *   top_k              0 to MGRIT_TOP_MOST, at most cols: top_ids, top_logprobs, device [rows, top_k] out, get the ids of the
+ *                      largest logits in descending order, equal ones by their id, and their log probabilities
+ * Backward:  dlogits_i = (g_logprob ([i = token] - p_i) - g_entropy p_i (ln p_i + H)) / temperature
+ *   g_logprob          device [rows];  g_entropy  device [rows], or NULL for 0
+ * _step does both in one call that reads the logits once where a row fits, for cotangents that are known beforehand (a mean
+ * of cross entropies: g_logprob = -1 / count); logprob and entropy may be NULL, lse may be NULL.
+ * Workspace of _forward and _step: 256-byte aligned, mgrit_token_logprobs_workspace_bytes (host only; 0, also on invalid arguments:
+ * none is needed and it may be NULL; _step: top_k 0). */
+#define MGRIT_TOP_MOST 64
+enum { MGRIT_IDS_I32 = 0, MGRIT_IDS_I64 = 1 };
+typedef struct mgrit_logits_desc {
+  int64_t rows;
+  int32_t cols;
+  int32_t dtype;                 /* of the logits and dlogits, MGRIT_DTYPE_* */
+  int32_t id_dtype;              /* MGRIT_IDS_* */
+  float   temperature;           /* 1e-4 to 1e4 */
+} mgrit_logits_desc;
+size_t mgrit_token_logprobs_workspace_bytes(const mgrit_logits_desc* desc, int32_t top_k);
+int mgrit_token_logprobs_forward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const void* tokens,
+                                 float* logprob, float* entropy, float* lse, int32_t top_k, void* top_ids, float* top_logprobs,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+int mgrit_token_logprobs_backward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const void* tokens,
+                                  const float* lse, const float* g_logprob, const float* entropy, const float* g_entropy,
+                                  void* dlogits, int64_t dlogits_stride, void* stream);
+int mgrit_token_logprobs_step(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const void* tokens,
+                              const float* g_logprob, const float* g_entropy, float* logprob, float* entropy, float* lse,
+                              void* dlogits, int64_t dlogits_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Distillation from a teacher's top logits: per row the ids of `kept` logits and their values y, at most MGRIT_KEPT_MOST,
+ *   q = softmax(y / temperature) over the row's kept, or exp(y / temperature - teacher lse) where that is given (then their
+ *       probabilities under the whole teacher, which need not sum to 1)
+ *   loss = sum_j q_j (ln q_j - ln p_id(j)),  dlogits_i = g_loss / temperature (p_i sum_j q_j - sum_{j: id(j) = i} q_j)
+ * p: the student's, as above.  Ids below 0 fill up shorter lists; a row without any id, or with q = 0 throughout, has loss and
+ * gradient 0; an id of cols and more, or a value that is NaN or +infinity, gives NaN for both.  An id may come twice: its
+ * shares add up.  top_ids and top_logprobs of a teacher's rows at temperature 1 are such a list.
+ *   g_loss             device [rows], or NULL for 1;  lse  device [rows] out, may be NULL; the backward pass takes it
+ * Everything else as above. */
+#define MGRIT_KEPT_MOST 256
+typedef struct mgrit_teacher {
+  int32_t      kept;
+  int32_t      dtype;            /* of logits, MGRIT_DTYPE_* */
+  const void*  ids;              /* device [rows, kept], of the logits' id_dtype */
+  const void*  logits;           /* device [rows, kept] */
+  const float* lse;              /* device [rows] at the same temperature, or NULL */
+} mgrit_teacher;
+size_t mgrit_distill_workspace_bytes(const mgrit_logits_desc* desc, int32_t kept);
+int mgrit_distill_forward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const mgrit_teacher* teacher,
+                          float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+int mgrit_distill_backward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const mgrit_teacher* teacher,
+                           const float* lse, const float* g_loss, void* dlogits, int64_t dlogits_stride, void* stream);
+int mgrit_distill_step(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const mgrit_teacher* teacher,
+                       const float* g_loss, float* loss, float* lse, void* dlogits, int64_t dlogits_stride,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- adaptive control of the inexactness (sec. 3.2.3), host only ---------------------------
  * The convergence factor of MGRIT iteration k is ||r^(k+1)|| / ||r^(k)||, the ratio of consecutive
  * entries of the `resnorm` output above.  Policy of the paper: every `probe_every` batches run one
@@ -517,7 +586,8 @@ void mgrit_set_adjoint_cache(int on);
  * several groups (relaxation sweeps), 16+e the same over a single group (the serial coarse
  * chain); e: 0 store, 1 bias+GELU, 2 sublayer sum, 3 Euler update, 4 multiply by GELU',
  * 5 fp32 store, 6 GELU' of the cache pass; 24 the row-local chains of narrow layers; 25 rows to 8 bits and back,
- * 26 and 27 LayerNorm of rows forward and backward, 28 weight gradients from 8-bit rows.
+ * 26 and 27 LayerNorm of rows forward and backward, 28 weight gradients from 8-bit rows, 29 to 31 rows of logits: values,
+ * gradients, both.
  * Returns 0, -1 for a bad class, -3 if the pool overflowed. */
 int  mgrit_profile_enable(int max_records);
 void mgrit_profile_reset(void);

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Dict, List, Optional, Sequence
+from typing import Dict, List, NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -52,6 +52,14 @@ class Opts(C.Structure):
 class NormDesc(C.Structure):
     _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32),
                 ("eps", C.c_float)]
+
+
+class LogitsDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("dtype", C.c_int32), ("id_dtype", C.c_int32), ("temperature", C.c_float)]
+
+
+class Teacher(C.Structure):
+    _fields_ = [("kept", C.c_int32), ("dtype", C.c_int32), ("ids", C.c_void_p), ("logits", C.c_void_p), ("lse", C.c_void_p)]
 
 
 class ThetaLayout(C.Structure):
@@ -118,6 +126,18 @@ def lib() -> C.CDLL:
         L.mgrit_q8_pack.restype = C.c_int
         L.mgrit_q8_unpack.argtypes = [i64, i32, C.c_int, vp, vp, vp, i64, vp]
         L.mgrit_q8_unpack.restype = C.c_int
+        ld, size, tp = C.POINTER(LogitsDesc), C.c_size_t, C.POINTER(Teacher)
+        for name, args in (("mgrit_token_logprobs_forward", [vp, vp, vp, vp, i32, vp, vp, vp, size, vp]),
+                           ("mgrit_token_logprobs_backward", [vp, vp, vp, vp, vp, vp, i64, vp]),
+                           ("mgrit_token_logprobs_step", [vp, vp, vp, vp, vp, vp, vp, i64, vp, size, vp]),
+                           ("mgrit_distill_forward", [tp, vp, vp, vp, size, vp]),
+                           ("mgrit_distill_backward", [tp, vp, vp, vp, i64, vp]),
+                           ("mgrit_distill_step", [tp, vp, vp, vp, vp, i64, vp, size, vp])):
+            getattr(L, name).argtypes = [ld, vp, i64, *args]
+            getattr(L, name).restype = C.c_int
+        for name in ("mgrit_token_logprobs_workspace_bytes", "mgrit_distill_workspace_bytes"):
+            getattr(L, name).argtypes = [ld, i32]
+            getattr(L, name).restype = size
         L.mgrit_layer_norm_forward.argtypes = [nd, vp, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp]
         L.mgrit_layer_norm_forward.restype = C.c_int
         L.mgrit_layer_norm_backward_workspace_bytes.argtypes = [nd]
@@ -315,7 +335,8 @@ PROFILE_CLASSES = {0: "gemm_generic", 1: "attn_fwd", 2: "attn_bwd", 3: "ln_fwd",
 PROFILE_CLASSES.update({c + 8: n.replace("gemm_mfma_", "gemm_mfma_single_") for c, n in list(PROFILE_CLASSES.items())
                         if c >= 8})
 PROFILE_CLASSES[24] = "chain"
-PROFILE_CLASSES.update({25: "q8", 26: "norm_fwd", 27: "norm_bwd", 28: "q8_weight_grad"})
+PROFILE_CLASSES.update({25: "q8", 26: "norm_fwd", 27: "norm_bwd", 28: "q8_weight_grad",
+                        29: "logits", 30: "logits_grad", 31: "logits_step"})
 
 
 def mgrit_profile_enable(max_records: int) -> None:
@@ -847,6 +868,8 @@ def _on(stream: Optional[torch.cuda.Stream], device: int):
 
 def _new(shape, dtype: torch.dtype, device: torch.device, other: Optional[torch.cuda.Stream]) -> torch.Tensor:
     """A new tensor that belongs to the stream its call is enqueued on."""
+    if not shape:
+        shape = ((),)                                                    # one value
     if other is None:
         return torch.empty(*shape, dtype=dtype, device=device)          # (a tuple as it is takes 0.8 us longer)
     with torch.cuda.stream(other):
@@ -1055,3 +1078,247 @@ def mgrit_q8_weight_grad(dy: torch.Tensor, x: Q8Rows, scale: float = 1.0, dW: Op
     if other is not None:
         _in_use(other, dy, x, dW, db, ws)
     return dW, db
+
+
+# ---- between a head's logits and the gradient that enters the network again --------------------------------
+TOP_MOST, KEPT_MOST = 64, 256        # MGRIT_TOP_MOST, MGRIT_KEPT_MOST
+_ID_DTYPES = {torch.int32: 0, torch.int64: 1}
+
+
+class TokenLogprobs(NamedTuple):
+    """Per row of logits [..., cols], all of shape [...] (top_*: [..., top_k]): ln p of its token, the entropy and the
+    log-sum-exp of its distribution, the ids of the largest logits and their ln p.  What was not asked for is None."""
+    logprob: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_ids: Optional[torch.Tensor] = None
+    top_logprobs: Optional[torch.Tensor] = None
+
+
+def _floats(t: torch.Tensor, shape, name: str, device: int) -> int:
+    """Address of an fp32 argument of one value per row."""
+    _check_device(t, name, device)
+    if t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous fp32 values of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _ids(t: torch.Tensor, shape, name: str, device: int) -> int:
+    _check_device(t, name, device)
+    if t.dtype not in _ID_DTYPES or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous int32 or int64 ids of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _out(given: Optional[torch.Tensor], shape, name: str, device: int, like: torch.Tensor, other):
+    """(tensor, address) of an fp32 result: the caller's, or a new one."""
+    if given is None:
+        given = _new(shape, torch.float32, like.device, other)
+        return given, given.data_ptr()
+    return given, _floats(given, shape, name, device)
+
+
+def _dlogits(given: Optional[torch.Tensor], logits: torch.Tensor, cols: int, device: int, other):
+    """(tensor, stride) of the logits' gradient."""
+    if given is None:
+        return _new(logits.shape, logits.dtype, logits.device, other), cols
+    _, _, stride = _check_rows(given, "dlogits", device, logits.shape)
+    if given.dtype != logits.dtype:
+        raise ValueError(f"dlogits: expected {logits.dtype}, got {given.dtype}")
+    return given, stride
+
+
+def _logits_desc(logits: torch.Tensor, rows: int, cols: int, ids: torch.dtype, temperature: float) -> LogitsDesc:
+    return LogitsDesc(rows, cols, _DTYPES[logits.dtype], _ID_DTYPES[ids], temperature)
+
+
+def mgrit_token_logprobs_workspace_bytes(rows: int, cols: int, dtype: torch.dtype, top_k: int = 0) -> int:
+    return int(lib().mgrit_token_logprobs_workspace_bytes(LogitsDesc(rows, _c_int32(cols), _DTYPES[dtype], 0, 1.0), top_k))
+
+
+def mgrit_token_logprobs_forward(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0, temperature: float = 1.0,
+                                 logprob: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                                 lse: Optional[torch.Tensor] = None, top_ids: Optional[torch.Tensor] = None,
+                                 top_logprobs: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                 stream: Optional[torch.cuda.Stream] = None) -> TokenLogprobs:
+    """Log probabilities of tokens (int32 or int64, [...]; below 0: none, 0) under logits / temperature (fp32 or bf16,
+    [..., cols]), each row's entropy and log-sum-exp, and its top_k alternatives (ids of the tokens' type, int64 without
+    tokens).  Not recorded by autograd: gradients come from mgrit_token_logprobs_backward."""
+    device = _device_of(logits, "logits")
+    rows, cols, stride = _check_rows(logits, "logits", device)
+    lead = logits.shape[:-1]
+    handle, other = _on(stream, device)
+    tokens_at = logprob_at = ids_at = top_at = None
+    if tokens is not None:
+        tokens_at = _ids(tokens, lead, "tokens", device)
+        logprob, logprob_at = _out(logprob, lead, "logprob", device, logits, other)
+        id_dtype = tokens.dtype
+    else:
+        if logprob is not None:
+            raise ValueError("logprob: expected tokens as well")
+        id_dtype = torch.int64 if top_ids is None else top_ids.dtype
+    entropy, entropy_at = _out(entropy, lead, "entropy", device, logits, other)
+    lse, lse_at = _out(lse, lead, "lse", device, logits, other)
+    if top_k:
+        if not 0 < top_k <= TOP_MOST:
+            raise ValueError(f"top_k: expected 0 to {TOP_MOST}, got {top_k}")
+        of = (*lead, top_k)
+        if top_ids is None:
+            top_ids = _new(of, id_dtype, logits.device, other)
+        elif top_ids.dtype != id_dtype:
+            raise ValueError(f"top_ids: expected {id_dtype} as the tokens, got {top_ids.dtype}")
+        ids_at = _ids(top_ids, of, "top_ids", device)
+        top_logprobs, top_at = _out(top_logprobs, of, "top_logprobs", device, logits, other)
+    elif top_ids is not None or top_logprobs is not None:
+        raise ValueError("top_ids, top_logprobs: expected a top_k")
+    L, desc = lib(), _logits_desc(logits, rows, cols, id_dtype, temperature)
+    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_token_logprobs_workspace_bytes(desc, top_k), logits.device, other)
+    st = L.mgrit_token_logprobs_forward(desc, logits.data_ptr(), stride, tokens_at, logprob_at, entropy_at, lse_at, top_k, ids_at, top_at,
+                                        ws_at, ws_bytes, handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_token_logprobs_forward")
+    if other is not None:
+        _in_use(other, logits, tokens, logprob, entropy, lse, top_ids, top_logprobs, ws)
+    return TokenLogprobs(logprob, entropy, lse, top_ids, top_logprobs)
+
+
+def mgrit_token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: torch.Tensor, g_logprob: torch.Tensor,
+                                  entropy: Optional[torch.Tensor] = None, g_entropy: Optional[torch.Tensor] = None,
+                                  temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None,
+                                  stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The logits' gradient for cotangents g_logprob (and g_entropy) of mgrit_token_logprobs_forward's values; lse and
+    entropy as it returned them.  dlogits may be the logits themselves, which it then replaces."""
+    device = _device_of(logits, "logits")
+    rows, cols, stride = _check_rows(logits, "logits", device)
+    lead = logits.shape[:-1]
+    handle, other = _on(stream, device)
+    tokens_at = _ids(tokens, lead, "tokens", device)
+    lse_at, g_at = _floats(lse, lead, "lse", device), _floats(g_logprob, lead, "g_logprob", device)
+    entropy_at = h_at = None
+    if g_entropy is not None:
+        h_at = _floats(g_entropy, lead, "g_entropy", device)
+        entropy_at = _floats(entropy, lead, "entropy", device)
+    dlogits, dstride = _dlogits(dlogits, logits, cols, device, other)
+    st = lib().mgrit_token_logprobs_backward(_logits_desc(logits, rows, cols, tokens.dtype, temperature), logits.data_ptr(), stride,
+                                             tokens_at, lse_at, g_at, entropy_at, h_at, dlogits.data_ptr(), dstride, handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_token_logprobs_backward")
+    if other is not None:
+        _in_use(other, logits, tokens, lse, g_logprob, entropy, g_entropy, dlogits)
+    return dlogits
+
+
+def mgrit_token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, g_logprob: torch.Tensor, g_entropy: Optional[torch.Tensor] = None,
+                              temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None,
+                              entropy: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                              workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Returns (TokenLogprobs, dlogits): mgrit_token_logprobs_forward and _backward in one call, for cotangents that are
+    known beforehand."""
+    device = _device_of(logits, "logits")
+    rows, cols, stride = _check_rows(logits, "logits", device)
+    lead = logits.shape[:-1]
+    handle, other = _on(stream, device)
+    tokens_at, g_at = _ids(tokens, lead, "tokens", device), _floats(g_logprob, lead, "g_logprob", device)
+    h_at = None if g_entropy is None else _floats(g_entropy, lead, "g_entropy", device)
+    logprob, logprob_at = _out(logprob, lead, "logprob", device, logits, other)
+    entropy, entropy_at = _out(entropy, lead, "entropy", device, logits, other)
+    lse, lse_at = _out(lse, lead, "lse", device, logits, other)
+    dlogits, dstride = _dlogits(dlogits, logits, cols, device, other)
+    L, desc = lib(), _logits_desc(logits, rows, cols, tokens.dtype, temperature)
+    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_token_logprobs_workspace_bytes(desc, 0), logits.device, other)
+    st = L.mgrit_token_logprobs_step(desc, logits.data_ptr(), stride, tokens_at, g_at, h_at, logprob_at, entropy_at, lse_at,
+                                     dlogits.data_ptr(), dstride, ws_at, ws_bytes, handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_token_logprobs_step")
+    if other is not None:
+        _in_use(other, logits, tokens, g_logprob, g_entropy, logprob, entropy, lse, dlogits, ws)
+    return TokenLogprobs(logprob, entropy, lse), dlogits
+
+
+def mgrit_distill_workspace_bytes(rows: int, cols: int, dtype: torch.dtype, kept: int) -> int:
+    return int(lib().mgrit_distill_workspace_bytes(LogitsDesc(rows, _c_int32(cols), _DTYPES[dtype], 0, 1.0), _c_int32(kept)))
+
+
+def _teacher(logits: torch.Tensor, ids: torch.Tensor, values: torch.Tensor, lse: Optional[torch.Tensor], device: int) -> Teacher:
+    _check_device(ids, "teacher_ids", device)
+    kept = ids.shape[-1] if ids.dim() else 0
+    if not 0 < kept <= KEPT_MOST:
+        raise ValueError(f"teacher_ids: expected lists of 1 to {KEPT_MOST} ids, got shape {tuple(ids.shape)}")
+    of = (*logits.shape[:-1], kept)
+    ids_at = _ids(ids, of, "teacher_ids", device)
+    _check_device(values, "teacher_logits", device)
+    if values.dtype not in _DTYPES or values.shape != of or not values.is_contiguous():
+        raise ValueError(f"teacher_logits: expected contiguous fp32 or bf16 values of shape {of}, got {values.dtype} {tuple(values.shape)}")
+    lse_at = None if lse is None else _floats(lse, logits.shape[:-1], "teacher_lse", device)
+    return Teacher(kept, _DTYPES[values.dtype], ids_at, values.data_ptr(), lse_at)
+
+
+def mgrit_distill_forward(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, temperature: float = 1.0,
+                          teacher_lse: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None,
+                          lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                          stream: Optional[torch.cuda.Stream] = None):
+    """Returns (loss, lse) per row of logits [..., cols]: sum q (ln q - ln p) over a teacher's kept ids and logits [..., kept],
+    p = softmax(logits / temperature), q = softmax(teacher_logits / temperature) over those kept, or, with the teacher's
+    log-sum-exp at that temperature, their probabilities.  Ids below 0 fill up shorter lists.  Not recorded by autograd."""
+    device = _device_of(logits, "logits")
+    rows, cols, stride = _check_rows(logits, "logits", device)
+    lead = logits.shape[:-1]
+    handle, other = _on(stream, device)
+    teacher = _teacher(logits, teacher_ids, teacher_logits, teacher_lse, device)
+    loss, loss_at = _out(loss, lead, "loss", device, logits, other)
+    lse, lse_at = _out(lse, lead, "lse", device, logits, other)
+    L, desc = lib(), _logits_desc(logits, rows, cols, teacher_ids.dtype, temperature)
+    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_distill_workspace_bytes(desc, teacher.kept), logits.device, other)
+    st = L.mgrit_distill_forward(desc, logits.data_ptr(), stride, teacher, loss_at, lse_at, ws_at, ws_bytes, handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_distill_forward")
+    if other is not None:
+        _in_use(other, logits, teacher_ids, teacher_logits, teacher_lse, loss, lse, ws)
+    return loss, lse
+
+
+def mgrit_distill_backward(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, lse: torch.Tensor,
+                           g_loss: Optional[torch.Tensor] = None, temperature: float = 1.0, teacher_lse: Optional[torch.Tensor] = None,
+                           dlogits: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The logits' gradient of mgrit_distill_forward's losses for cotangents g_loss (1 without); lse as it returned it.  dlogits
+    may be the logits themselves, which it then replaces."""
+    device = _device_of(logits, "logits")
+    rows, cols, stride = _check_rows(logits, "logits", device)
+    lead = logits.shape[:-1]
+    handle, other = _on(stream, device)
+    teacher = _teacher(logits, teacher_ids, teacher_logits, teacher_lse, device)
+    lse_at = _floats(lse, lead, "lse", device)
+    g_at = None if g_loss is None else _floats(g_loss, lead, "g_loss", device)
+    dlogits, dstride = _dlogits(dlogits, logits, cols, device, other)
+    st = lib().mgrit_distill_backward(_logits_desc(logits, rows, cols, teacher_ids.dtype, temperature), logits.data_ptr(), stride, teacher,
+                                      lse_at, g_at, dlogits.data_ptr(), dstride, handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_distill_backward")
+    if other is not None:
+        _in_use(other, logits, teacher_ids, teacher_logits, teacher_lse, lse, g_loss, dlogits)
+    return dlogits
+
+
+def mgrit_distill_step(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, g_loss: Optional[torch.Tensor] = None,
+                       temperature: float = 1.0, teacher_lse: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+                       loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None):
+    """Returns (loss, lse, dlogits): mgrit_distill_forward and _backward in one call, for cotangents that are known beforehand."""
+    device = _device_of(logits, "logits")
+    rows, cols, stride = _check_rows(logits, "logits", device)
+    lead = logits.shape[:-1]
+    handle, other = _on(stream, device)
+    teacher = _teacher(logits, teacher_ids, teacher_logits, teacher_lse, device)
+    g_at = None if g_loss is None else _floats(g_loss, lead, "g_loss", device)
+    loss, loss_at = _out(loss, lead, "loss", device, logits, other)
+    lse, lse_at = _out(lse, lead, "lse", device, logits, other)
+    dlogits, dstride = _dlogits(dlogits, logits, cols, device, other)
+    L, desc = lib(), _logits_desc(logits, rows, cols, teacher_ids.dtype, temperature)
+    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_distill_workspace_bytes(desc, teacher.kept), logits.device, other)
+    st = L.mgrit_distill_step(desc, logits.data_ptr(), stride, teacher, g_at, loss_at, lse_at, dlogits.data_ptr(), dstride, ws_at, ws_bytes,
+                              handle)
+    if st != MGRIT_OK:
+        raise MgritError(st, "mgrit_distill_step")
+    if other is not None:
+        _in_use(other, logits, teacher_ids, teacher_logits, teacher_lse, g_loss, loss, lse, dlogits, ws)
+    return loss, lse, dlogits

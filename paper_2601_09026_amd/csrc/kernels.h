@@ -180,6 +180,29 @@ struct Q8GradArgs {
 size_t q8_grad_partial_floats(long rows, int M, int N, bool dy_bf16);
 hipError_t launch_q8_grad(const Q8GradArgs& a, bool dy_bf16, float* partial, hipStream_t st);
 
+// ---- logits.hip: between a head's logits and the gradient that enters the network again --------------------------
+struct LogitsArgs {
+  long rows; int cols;
+  const void* z; long ld;                                 // the logits
+  float tau;
+  bool wide_ids;                                          // ids have 64 bits
+  const void* tokens;                                     // log probabilities: optional
+  float *logprob, *entropy, *lse;                         // [rows], each optional
+  int top_k; void* top_ids; float* top_logprobs;          // [rows, top_k]
+  int kept; const void* teacher_ids; const void* teacher; // distillation: [rows, kept]
+  bool teacher_bf16; const float* teacher_lse;            // the latter optional
+  float* loss;
+  const float *lse_in, *entropy_in;                       // the gradient alone: what the forward pass left
+  const float *g, *h;                                     // cotangents of log probability or loss, of entropy (optional)
+  void* dz; long lddz;                                    // null: values alone
+  // set by the launch
+  int parts, part_cols, runs, run_cols, points;
+  f32x4* part_sums; unsigned long long* part_lists; float* part_points;
+};
+constexpr int LOGITS_TOP_MOST = 64, LOGITS_KEPT_MOST = 256;
+size_t logits_workspace_bytes(long rows, int cols, bool is_bf16, int top_k, int points);
+hipError_t launch_logits(LogitsArgs a, int mode, bool is_bf16, void* workspace, hipStream_t st);   // mode 0: log probabilities, 1: distillation
+
 // ---- attention.hip -----------------------------------------------------------
 struct AttnArgs {
   int n_groups, B, H, dh, Sq, Sk, causal;

@@ -1,0 +1,691 @@
+// Between a head's logits and the gradient that enters the network again: log probabilities of given tokens with entropy
+// and the most likely alternatives, distillation from a teacher's top logits, and the gradients of both.  Over a row z:
+//   p = softmax(z / tau),  lse = log sum exp(z / tau),  H = lse - sum p z / tau
+//   log p_i = z_i / tau - lse,  dz_i = 1 / tau (g ([i = token] - p_i) - h p_i (log p_i + H))
+//   L = sum_j q_j (log q_j - log p_id(j)),  dz_i = g / tau (Q p_i - sum_{j: id(j) = i} q_j),  Q = sum q
+// A row is read in 16-byte vectors from its first 16-byte address on, the elements before and behind them one by one.
+#include <math.h>
+
+#include <type_traits>
+
+#include "kernels.h"
+#include "prof.h"
+#include "q8.h"
+
+namespace mg {
+namespace {
+
+constexpr float LOWEST = -3.402823466e38f, LOG2E = 1.44269504088896340736f;
+constexpr int THREADS = 256, WAVES = THREADS / WAVE;
+constexpr int STEP = 4;                                  // vectors of a lane that are loaded together
+constexpr int LIST = 256;                                // candidates of a wavefront
+typedef unsigned long long u64;
+
+template <typename T> constexpr int vec() { return 16 / (int)sizeof(T); }
+
+// ---- a run of elements in memory -------------------------------------------------
+template <typename T> struct Run {
+  T* p;
+  int head, vecs, odd;                                   // odd: elements outside the vectors, head of them in front
+  __device__ __forceinline__ Run(const void* base, long at, int n) {
+    p = static_cast<T*>(const_cast<void*>(base)) + at;
+    const int lead = (int)((16u - ((unsigned)reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / (int)sizeof(T);
+    head = lead < n ? lead : n;
+    vecs = (n - head) / vec<T>();
+    odd = n - vecs * vec<T>();
+  }
+  __device__ __forceinline__ int odd_at(int i) const { return i < head ? i : i + vecs * vec<T>(); }
+  __device__ __forceinline__ int vec_at(int v) const { return head + v * vec<T>(); }
+};
+
+template <typename T> __device__ __forceinline__ void decode(u32x4 r, float (&x)[vec<T>()]);
+template <> __device__ __forceinline__ void decode<float>(u32x4 r, float (&x)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = bits_f(r[j]);
+}
+template <> __device__ __forceinline__ void decode<bf16>(u32x4 r, float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[2 * j] = bits_f(r[j] << 16);
+    x[2 * j + 1] = bits_f(r[j] & 0xffff0000u);
+  }
+}
+template <typename T> __device__ __forceinline__ u32x4 encode(const float (&x)[vec<T>()]);
+template <> __device__ __forceinline__ u32x4 encode<float>(const float (&x)[4]) {
+  return u32x4{f_bits(x[0]), f_bits(x[1]), f_bits(x[2]), f_bits(x[3])};
+}
+template <> __device__ __forceinline__ u32x4 encode<bf16>(const float (&x)[8]) {
+  bf16x8 b;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) b[j] = (bf16)x[j];
+  return __builtin_bit_cast(u32x4, b);
+}
+
+__device__ __forceinline__ long id_of(const void* ids, long i, bool wide) {
+  return wide ? static_cast<const int64_t*>(ids)[i] : (long)static_cast<const int32_t*>(ids)[i];
+}
+
+// ---- sums of exponentials ----------------------------------------------------------
+// s = sum 2^((x - m) c), t = sum (x - m) c 2^((x - m) c) over the values seen, m their maximum, c = log2(e) / tau.  The
+// difference is taken before it is scaled: equal values of any size have the exponent 0.  A NaN or +infinity makes s NaN.
+// Exponents of -160 and less, -infinity among them, have 2^a = 0, and 0 in t.
+struct Sums { float m = LOWEST, s = 0.f, t = 0.f; };
+__device__ __forceinline__ float bounded(float a) { return fmaxf(a, -160.f); }
+
+__device__ __forceinline__ void raise(Sums& a, float m, float c) {
+  const float d = bounded((a.m - m) * c), f = __builtin_amdgcn_exp2f(d);
+  a.t = f * (a.t + d * a.s);
+  a.s = f * a.s;
+  a.m = m;
+}
+__device__ __forceinline__ void merge(Sums& a, Sums b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  raise(a, m, c);
+  raise(b, m, c);
+  a.s += b.s;
+  a.t += b.t;
+}
+template <int N> __device__ __forceinline__ void add(Sums& a, const float (&x)[N], float top, float c) {
+  raise(a, fmaxf(a.m, top), c);
+  float s = 0.f, t = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = (x[i] - a.m) * c, e = __builtin_amdgcn_exp2f(d);
+    s += e;
+    t = fmaf(bounded(d), e, t);
+  }
+  a.s += s;
+  a.t += t;
+}
+__device__ __forceinline__ void wave_merge(Sums& a, float c) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) merge(a, Sums{__shfl_xor(a.m, o, 64), __shfl_xor(a.s, o, 64), __shfl_xor(a.t, o, 64)}, c);
+}
+
+// What a row's sums come to.  lse: +-infinity where the row's largest quotient by tau is: no distribution (-infinity: zeros
+// in place of p) or, as with a NaN among the logits, NaN.
+struct RowSums {
+  float top, lse, log_s, inv_tau;                        // log p = (z - top) inv_tau - log_s
+  float entropy;
+  bool bad, none;
+  __device__ __forceinline__ RowSums(Sums a, float tau) {
+    inv_tau = 1.0f / tau;
+    top = a.m;
+    log_s = logf(a.s);
+    lse = a.m / tau + log_s;
+    bad = !(a.s >= 0.f) || lse == __builtin_inff();
+    none = !bad && !(lse > -__builtin_inff());
+    entropy = none ? 0.f : fmaxf(log_s - 0.69314718055994530942f * a.t / a.s, 0.f);
+    if (bad) lse = entropy = __builtin_nanf("");
+  }
+  __device__ __forceinline__ float logprob(float z, float tau) const {
+    return bad ? __builtin_nanf("") : none ? -__builtin_inff() : (z - top) / tau - log_s;
+  }
+};
+
+// ---- the largest elements ------------------------------------------------------------
+// A candidate is one number: the value's order in the upper half, the complement of its index below, so that the greater
+// of two comes first and equal values come by index.  Each wavefront has a list of candidates in LDS, the threshold below
+// which nothing can be among the row's k largest, and sorts the list down to k when it is full.
+__device__ __forceinline__ u64 candidate(float x, int index) {
+  const unsigned b = f_bits(x + 0.f);                    // (-0 and 0 are equal)
+  return (u64)(b ^ ((unsigned)((int)b >> 31) | 0x80000000u)) << 32 | (unsigned)~index;
+}
+__device__ __forceinline__ float value_of(u64 key) {
+  const unsigned b = (unsigned)(key >> 32);
+  return bits_f(b ^ (b & 0x80000000u ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ int index_of(u64 key) { return (int)~(unsigned)key; }
+__device__ __forceinline__ u64 uniform(u64 v) {
+  return (u64)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ __forceinline__ void wave_sync() {            // LDS accesses of a wavefront keep their order
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+struct Top {
+  u64* list;                                             // [LIST] of this wavefront
+  int k, n;                                              // n: candidates in it
+  u64 floor;                                             // only what is greater is taken
+  float bar;                                             // the value of floor
+  __device__ __forceinline__ void start(u64* lds, int want) { list = lds; k = want; n = 0; floor = 0; bar = -__builtin_inff(); }
+  // A value that at least k lanes reach (all of them, if fewer have any)
+  __device__ __forceinline__ void first_bar(float most) {
+    int above = 0;
+    for (int l = 0; l < WAVE; ++l) above += bits_f((unsigned)__builtin_amdgcn_readlane((int)f_bits(most), l)) > most;
+    float b = above < k ? most : __builtin_inff();
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) b = fminf(b, __shfl_xor(b, o, 64));
+    bar = b;
+    floor = uniform(candidate(b, -1));                   // (the lowest of that value)
+  }
+  // sorts the list, k of it stay
+  __device__ __forceinline__ void settle() {
+    const int lane = threadIdx.x & 63;
+    wave_sync();
+    u64 own[LIST / WAVE];
+    int rank[LIST / WAVE];
+#pragma unroll
+    for (int i = 0; i < LIST / WAVE; ++i) {
+      own[i] = i * WAVE + lane < n ? list[i * WAVE + lane] : 0;
+      rank[i] = 0;
+    }
+    for (int j = 0; j < n; ++j) {
+      const u64 other = list[j];
+#pragma unroll
+      for (int i = 0; i < LIST / WAVE; ++i) rank[i] += other > own[i];
+    }
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < LIST / WAVE; ++i)
+      if (i * WAVE + lane < n && rank[i] < k) list[rank[i]] = own[i];
+    wave_sync();
+    if (n >= k) {
+      n = k;
+      floor = uniform(list[k - 1]);
+      bar = value_of(floor);
+    }
+  }
+  // the lanes' keys, where one is given
+  __device__ __forceinline__ void take(bool given, u64 key) {
+    const u64 who = __ballot(given && key > floor);
+    if (!who) return;
+    const int lane = threadIdx.x & 63;
+    if (who >> lane & 1) list[n + __popcll(who & ((1ull << lane) - 1))] = key;
+    n += __popcll(who);
+    if (n > LIST - WAVE) settle();
+  }
+  // a vector per lane
+  template <int N> __device__ __forceinline__ void vector(const float (&x)[N], float most, int index, bool inside) {
+    if (!__any(inside && most >= bar)) return;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (__any(inside && x[j] >= bar)) take(inside && x[j] >= bar, candidate(x[j], index + j));
+  }
+  // the rest of the list is empty
+  __device__ __forceinline__ void finish() {
+    settle();
+    const int lane = threadIdx.x & 63;
+    if (lane >= n && lane < k) list[lane] = 0;
+    wave_sync();
+  }
+};
+
+// ---- a row's sums (and its largest elements), by `team` lanes -------------------------
+template <typename T, bool TOP> __device__ __forceinline__ void read_run(const Run<T>& r, int lane, int team, int index, float c, Sums& sums, Top& top) {
+  constexpr int N = vec<T>();
+  const float none = -__builtin_inff();
+  for (int v0 = 0; v0 < r.vecs; v0 += STEP * team) {
+    u32x4 raw[STEP];
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      const int v = v0 + u * team + lane;
+      raw[u] = ld_stream(reinterpret_cast<const u32x4*>(r.p + r.vec_at(v < r.vecs ? v : r.vecs - 1)));
+    }
+    float x[STEP * N], most[STEP], all = none;
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      const bool inside = v0 + u * team + lane < r.vecs;
+      float e[N];
+      decode<T>(raw[u], e);
+      most[u] = none;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        x[u * N + j] = inside ? e[j] : none;
+        most[u] = fmaxf(most[u], x[u * N + j]);
+      }
+      all = fmaxf(all, most[u]);
+    }
+    add(sums, x, all, c);
+    if constexpr (TOP) {
+      if (v0 == 0) top.first_bar(all);
+#pragma unroll
+      for (int u = 0; u < STEP; ++u) {
+        const int v = v0 + u * team + lane;
+        float e[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) e[j] = x[u * N + j];
+        top.vector(e, most[u], index + r.vec_at(v), v < r.vecs);
+      }
+    }
+  }
+  if (r.odd) {
+    const bool inside = lane < r.odd;                    // (odd < 2 N, no more than a wavefront)
+    const float x[1] = {inside ? to_f(r.p[r.odd_at(lane)]) : none};
+    add(sums, x, x[0], c);
+    if constexpr (TOP) top.vector(x, x[0], index + r.odd_at(lane), inside);
+  }
+}
+
+// What a team of several wavefronts found, in the first wavefront.  (All of the block's threads.)
+template <int W, bool TOP> __device__ __forceinline__ void join_waves(Sums& sums, Top& top, f32x4* lds_sums, u64* lds_lists, float c) {
+  wave_merge(sums, c);
+  if constexpr (TOP) top.finish();
+  if constexpr (W > 1) {
+    const int wave = threadIdx.x / WAVE;
+    if ((threadIdx.x & 63) == 0) lds_sums[wave] = f32x4{sums.m, sums.s, sums.t, 0.f};
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int w = 1; w < W; ++w) merge(sums, Sums{lds_sums[w][0], lds_sums[w][1], lds_sums[w][2]}, c);
+      if constexpr (TOP) {
+        const int lane = threadIdx.x & 63;
+        for (int w = 1; w < W; ++w) top.take(lane < top.k, lane < top.k ? lds_lists[w * LIST + lane] : 0);
+        top.finish();
+      }
+    }
+  }
+}
+
+// ---- what a row is measured by ----------------------------------------------------------
+// Ids with weights w that sum to `mass`.  Log probabilities (MODE 0): the token, w = 1, in the first lane.  Distillation
+// (MODE 1): the teacher's kept ids with w = q, id j in lane j % 64.  mass 0: the row has none; NaN: one is out of range (or a
+// teacher's logit is no number).  Held by one wavefront.
+constexpr int KEPT = 256;
+template <int MODE> struct Points {
+  static constexpr int N = MODE == 0 ? 1 : KEPT / WAVE;
+  int id[N];                                             // -1: none
+  float w[N], z[N];                                      // z: the student's logits
+  float mass;
+  __device__ __forceinline__ void load(const LogitsArgs& a, long row) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (MODE == 0) {
+      const long token = a.tokens ? id_of(a.tokens, row, a.wide_ids) : -1;
+      const bool valid = token >= 0 && token < a.cols;
+      id[0] = valid ? (int)token : -1;
+      w[0] = 1.f;
+      mass = valid ? 1.f : token < 0 ? 0.f : __builtin_nanf("");
+    } else {
+      const float none = -__builtin_inff();
+      float y[N], top = none;
+      bool out = false;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int j = lane + i * WAVE;
+        id[i] = -1;
+        y[i] = none;
+        if (j < a.kept) {
+          const long at = row * a.kept + j, v = id_of(a.teacher_ids, at, a.wide_ids);
+          out |= v >= a.cols;
+          if (v >= 0 && v < a.cols) {
+            id[i] = (int)v;
+            y[i] = a.teacher_bf16 ? to_f(static_cast<const bf16*>(a.teacher)[at]) : static_cast<const float*>(a.teacher)[at];
+          }
+        }
+        top = fmaxf(top, y[i]);
+      }
+      if (a.teacher_lse) {
+        const float l = a.teacher_lse[row];
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = id[i] < 0 ? 0.f : expf(y[i] / a.tau - l);
+      } else {
+        top = fmaxf(wave_max(top), LOWEST);
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          w[i] = id[i] < 0 ? 0.f : expf((y[i] - top) / a.tau);
+          s += w[i];
+        }
+        s = wave_sum(s);
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = s != 0.f ? w[i] / s : 0.f;       // (NaN stays)
+      }
+      mass = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) mass += w[i];
+      mass = wave_sum(mass);
+      if (__any(out)) mass = __builtin_nanf("");
+    }
+  }
+  // the logits of the ids among the n from `from` on
+  template <typename T> __device__ __forceinline__ void gather(const T* row, int from, int n) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      z[i] = 0.f;
+      if (id[i] >= from && id[i] - from < n) z[i] = to_f(row[id[i]]);
+    }
+  }
+};
+
+// A row's values, from its sums and points
+template <int MODE> __device__ __forceinline__ void put_values(const LogitsArgs& a, long row, const RowSums& r, const Points<MODE>& pt) {
+  const int lane = threadIdx.x & 63;
+  if (lane == 0) {
+    if (a.lse) a.lse[row] = r.lse;
+    if (MODE == 0 && a.entropy) a.entropy[row] = r.entropy;
+  }
+  if constexpr (MODE == 0) {
+    if (lane == 0 && a.logprob) a.logprob[row] = pt.mass == 1.f ? r.logprob(pt.z[0], a.tau) : pt.mass;
+  } else {
+    float l = 0.f;
+#pragma unroll
+    for (int i = 0; i < Points<MODE>::N; ++i)
+      if (pt.id[i] >= 0 && pt.w[i] != 0.f) l += pt.w[i] * (logf(pt.w[i]) - r.logprob(pt.z[i], a.tau));
+    l = wave_sum(l);
+    if (lane == 0 && a.loss) a.loss[row] = pt.mass == 0.f || pt.mass != pt.mass ? pt.mass : l;
+  }
+}
+__device__ __forceinline__ void put_alternatives(const LogitsArgs& a, long row, const RowSums& r, const u64* list) {
+  const int lane = threadIdx.x & 63;
+  if (lane >= a.top_k) return;
+  const u64 key = list[lane];
+  const long at = row * a.top_k + lane;
+  const int id = r.bad ? -1 : index_of(key);
+  if (a.wide_ids) static_cast<int64_t*>(a.top_ids)[at] = id;
+  else static_cast<int32_t*>(a.top_ids)[at] = id;
+  a.top_logprobs[at] = r.logprob(value_of(key), a.tau);
+}
+
+// ---- values of a row --------------------------------------------------------------------
+// Teams of W wavefronts walk (row, part) pairs; with several parts a row's sums, lists and points go to the workspace.
+template <typename T, int W, bool TOP, int MODE>
+__global__ void __launch_bounds__(THREADS) logits_values_kernel(const LogitsArgs a) {
+  __shared__ u64 lists[TOP ? WAVES * LIST : 1];
+  __shared__ f32x4 waves[WAVES];
+  constexpr int TEAMS = WAVES / W;
+  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % (W * WAVE);
+  const float c = LOG2E / a.tau;
+  const long tasks = a.rows * a.parts;
+  // (a team of the whole block always has a row; one of a single wavefront meets no barrier)
+  for (long task = (long)blockIdx.x * TEAMS + wave / W; task < tasks; task += (long)gridDim.x * TEAMS) {
+    const long row = task / a.parts;
+    const int part = (int)(task - row * a.parts), from = part * a.part_cols;
+    const int n = a.cols - from < a.part_cols ? a.cols - from : a.part_cols;
+    const T* z = static_cast<const T*>(a.z) + row * a.ld;
+    Sums sums;
+    Top top;
+    if constexpr (TOP) top.start(lists + wave * LIST, a.top_k);
+    read_run<T, TOP>(Run<T>(z, from, n), lane, W * WAVE, from, c, sums, top);
+    join_waves<W, TOP>(sums, top, waves, lists, c);
+    if (wave % W == 0) {
+      Points<MODE> pt;
+      if (part == 0 && (a.parts == 1 || a.part_points)) {
+        pt.load(a, row);
+        pt.gather(z, 0, a.cols);
+      }
+      if (a.parts == 1) {
+        const RowSums r(sums, a.tau);
+        put_values<MODE>(a, row, r, pt);
+        if constexpr (TOP) put_alternatives(a, row, r, top.list);
+      } else {
+        if (lane == 0) a.part_sums[task] = f32x4{sums.m, sums.s, sums.t, 0.f};
+        if constexpr (TOP)
+          if (lane < a.top_k) a.part_lists[task * a.top_k + lane] = top.list[lane];
+        if (part == 0 && a.part_points) {
+#pragma unroll
+          for (int i = 0; i < Points<MODE>::N; ++i)
+            if (i * WAVE + lane < a.points) a.part_points[row * a.points + i * WAVE + lane] = pt.z[i];
+        }
+      }
+    }
+    if constexpr (W > 1) __syncthreads();
+  }
+}
+
+__device__ __forceinline__ Sums joined(const LogitsArgs& a, long row, float c) {
+  Sums all;
+  for (int p = 0; p < a.parts; ++p) {
+    const f32x4 s = a.part_sums[row * a.parts + p];
+    merge(all, Sums{s[0], s[1], s[2]}, c);
+  }
+  return all;
+}
+
+// The parts' results, a wavefront per row
+template <typename T, bool TOP, int MODE>
+__global__ void __launch_bounds__(THREADS) logits_join_kernel(const LogitsArgs a) {
+  __shared__ u64 lists[TOP ? WAVES * LIST : 1];
+  const int wave = threadIdx.x / WAVE, lane = threadIdx.x & 63;
+  for (long row = (long)blockIdx.x * WAVES + wave; row < a.rows; row += (long)gridDim.x * WAVES) {
+    const RowSums r(joined(a, row, LOG2E / a.tau), a.tau);
+    Points<MODE> pt;
+    pt.load(a, row);
+    pt.gather(static_cast<const T*>(a.z) + row * a.ld, 0, a.cols);
+    put_values<MODE>(a, row, r, pt);
+    if constexpr (TOP) {
+      Top top;
+      top.start(lists + wave * LIST, a.top_k);
+      const int all = a.parts * a.top_k;
+      const u64* from = a.part_lists + row * all;
+      for (int i = 0; i < all; i += WAVE) top.take(i + lane < all, i + lane < all ? from[i + lane] : 0);
+      top.finish();
+      put_alternatives(a, row, r, top.list);
+    }
+  }
+}
+
+// ---- gradients of a row -------------------------------------------------------------------
+// dz_i = slope (sum of the points' w at i) - p_i (A + B log p_i)
+struct Slope {
+  float top, off, inv_tau;                               // log p = (z - top) inv_tau - off
+  float A, B, slope;
+  int zero;                                              // nothing but zeros
+  template <bool ENTROPY> __device__ __forceinline__ float at(float z) const {
+    const float lp = fmaf(z - top, inv_tau, -off), p = __builtin_amdgcn_exp2f(lp * LOG2E);
+    return ENTROPY ? -p * fmaf(B, bounded(lp), A) : -p * A;
+  }
+};
+
+template <typename T, bool ENTROPY> __device__ __forceinline__ void write_run(const Run<T>& in, T* out, const Slope& s, int lane, int team) {
+  constexpr int N = vec<T>();
+  for (int v0 = 0; v0 < in.vecs; v0 += STEP * team) {
+    u32x4 raw[STEP];
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      const int v = v0 + u * team + lane;
+      raw[u] = ld_global(reinterpret_cast<const u32x4*>(in.p + in.vec_at(v < in.vecs ? v : in.vecs - 1)));
+    }
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      const int v = v0 + u * team + lane;
+      float x[N];
+      decode<T>(raw[u], x);
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = s.zero ? 0.f : s.template at<ENTROPY>(x[j]);
+      if (v < in.vecs) {
+        typedef __attribute__((address_space(1))) u32x4_u* gptr;
+        const u32x4 w = encode<T>(x);
+        *(gptr)(out + in.vec_at(v)) = u32x4_u{w[0], w[1], w[2], w[3]};
+      }
+    }
+  }
+  if (lane < in.odd) out[in.odd_at(lane)] = from_f<T>(s.zero ? 0.f : s.template at<ENTROPY>(to_f(in.p[in.odd_at(lane)])));
+}
+
+// The ids among a team's elements get their value again, with what the points add.  An id that comes twice is added up in
+// order, by its first.
+template <typename T, int MODE, bool ENTROPY>
+__device__ __forceinline__ void write_points(const Slope& s, const Points<MODE>& pt, T* row, int from, int n, int kept, int* ids, float* ws) {
+  const int lane = threadIdx.x & 63;
+  if constexpr (MODE == 0) {
+    if (lane == 0 && pt.id[0] >= from && pt.id[0] - from < n) row[pt.id[0]] = from_f<T>(s.template at<ENTROPY>(pt.z[0]) + s.slope);
+  } else {
+#pragma unroll
+    for (int i = 0; i < Points<MODE>::N; ++i) {
+      ids[i * WAVE + lane] = pt.id[i];
+      ws[i * WAVE + lane] = pt.w[i];
+    }
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < Points<MODE>::N; ++i) {
+      bool mine = pt.id[i] >= from && pt.id[i] - from < n;
+      if (!__any(mine)) continue;
+      float sum = 0.f;
+      for (int j = 0; j < kept; ++j) {
+        const bool same = ids[j] == pt.id[i];
+        sum += same ? ws[j] : 0.f;
+        mine = mine && !(same && j < i * WAVE + lane);
+      }
+      if (mine) row[pt.id[i]] = from_f<T>(s.template at<ENTROPY>(pt.z[i]) + s.slope * sum);
+    }
+    wave_sync();
+  }
+}
+
+// FROM: where a row's sums come from.  GIVEN: its log-sum-exp (and entropy) are arguments; PARTS: they lie in the workspace;
+// HERE: a team takes them itself, from the whole row.  But for GIVEN the rows' values are written as well.
+// dz may be z itself: what a team needs of its run besides the run is read before any of it is written, and what it
+// needs of other runs lies in the workspace.
+enum { GIVEN = 0, PARTS = 1, HERE = 2 };
+template <typename T, int W, bool ENTROPY, int MODE, int FROM>
+__global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsArgs a) {
+  constexpr int TEAMS = WAVES / W;
+  __shared__ f32x4 waves[WAVES];
+  __shared__ Slope slopes[TEAMS];
+  __shared__ int ids[MODE == 1 ? TEAMS * KEPT : 1];
+  __shared__ float ws[MODE == 1 ? TEAMS * KEPT : 1];
+  const int wave = threadIdx.x / WAVE, team = wave / W, lane = threadIdx.x % (W * WAVE);
+  const float c = LOG2E / a.tau;
+  const long tasks = a.rows * a.runs;
+  for (long task = (long)blockIdx.x * TEAMS + team; task < tasks; task += (long)gridDim.x * TEAMS) {
+    const long row = task / a.runs;
+    const int run = (int)(task - row * a.runs), from = run * a.run_cols;
+    const int n = a.cols - from < a.run_cols ? a.cols - from : a.run_cols;
+    const T* z = static_cast<const T*>(a.z) + row * a.ld;
+    T* dz = static_cast<T*>(a.dz) + row * a.lddz;
+    const Run<T> in(z, from, n);
+    Points<MODE> pt;
+    Sums sums;
+    if constexpr (FROM == HERE) {
+      Top none;
+      read_run<T, false>(in, lane, W * WAVE, 0, c, sums, none);
+      join_waves<W, false>(sums, none, waves, nullptr, c);
+    }
+    if (wave % W == 0) {
+      pt.load(a, row);
+      if constexpr (FROM == PARTS) {
+#pragma unroll
+        for (int i = 0; i < Points<MODE>::N; ++i) pt.z[i] = i * WAVE + lane < a.points ? a.part_points[row * a.points + i * WAVE + lane] : 0.f;
+      } else {
+        pt.gather(z, from, n);
+      }
+      Slope s;
+      float entropy = 0.f;
+      s.inv_tau = 1.0f / a.tau;
+      if constexpr (FROM == GIVEN) {
+        s.top = 0.f;
+        s.off = a.lse_in[row];
+        s.zero = s.off == -__builtin_inff();
+        if (ENTROPY) entropy = a.entropy_in[row];
+      } else {
+        if constexpr (FROM == PARTS) sums = joined(a, row, c);
+        const RowSums r(sums, a.tau);
+        if (run == 0) put_values<MODE>(a, row, r, pt);
+        s.top = r.top;
+        s.off = r.bad ? __builtin_nanf("") : r.log_s;
+        s.zero = r.none;
+        entropy = r.entropy;
+      }
+      s.slope = (MODE == 0 ? 1.f : -1.f) * (a.g ? a.g[row] : 1.f) * s.inv_tau;
+      if (pt.mass == 0.f) s.slope = 0.f;                 // (whatever g holds there)
+      s.A = s.slope * pt.mass;
+      s.B = 0.f;
+      if constexpr (ENTROPY) {
+        s.B = a.h[row] * s.inv_tau;
+        s.A += s.B * entropy;
+      } else {
+        s.zero |= pt.mass == 0.f;
+      }
+      slopes[team] = s;
+    }
+    if constexpr (W > 1) __syncthreads();
+    else wave_sync();
+    const Slope s = slopes[team];
+    write_run<T, ENTROPY>(in, dz + from, s, lane, W * WAVE);
+    if constexpr (W > 1) __syncthreads();
+    else wave_sync();
+    if (wave % W == 0 && !s.zero) write_points<T, MODE, ENTROPY>(s, pt, dz, from, n, a.kept, ids + (MODE == 1 ? team * KEPT : 0), ws + (MODE == 1 ? team * KEPT : 0));
+  }
+}
+
+// ---- launches ---------------------------------------------------------------------------
+constexpr int MOST_BLOCKS = 1 << 20, MOST_PARTS = 16;
+template <typename F> hipError_t with(bool x, F&& f) { return x ? f(std::true_type()) : f(std::false_type()); }
+int blocks_for(long tasks, int teams) {
+  const long b = (tasks + teams - 1) / teams;
+  return (int)(b < MOST_BLOCKS ? b : MOST_BLOCKS);
+}
+// short rows: one wavefront each
+bool short_rows(int cols, bool is_bf16) { return cols <= (is_bf16 ? 2048 : 1024); }
+// Few rows: a row's elements are shared out over several blocks
+int parts_of(long rows, int cols, bool is_bf16) {
+  if (short_rows(cols, is_bf16) || rows >= 512) return 1;
+  const long most = cols / 4096, wanted = 512 / (rows < 1 ? 1 : rows);
+  const long parts = wanted < most ? wanted : most;
+  return (int)(parts < 1 ? 1 : parts > MOST_PARTS ? MOST_PARTS : parts);
+}
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+template <typename T, int W, int MODE> hipError_t values(const LogitsArgs& a, hipStream_t st) {
+  return with(a.top_k > 0 && MODE == 0, [&](auto top) -> hipError_t {
+    constexpr bool TOP = decltype(top)::value && MODE == 0;
+    logits_values_kernel<T, W, TOP, MODE><<<blocks_for(a.rows * a.parts, WAVES / W), THREADS, 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.parts == 1 || a.dz) return e;
+    logits_join_kernel<T, TOP, MODE><<<blocks_for(a.rows, WAVES), THREADS, 0, st>>>(a);
+    return hipGetLastError();
+  });
+}
+template <typename T, int W, int MODE, int FROM> hipError_t gradient(const LogitsArgs& a, hipStream_t st) {
+  return with(MODE == 0 && a.h, [&](auto entropy) -> hipError_t {
+    logits_gradient_kernel<T, W, decltype(entropy)::value && MODE == 0, MODE, FROM><<<blocks_for(a.rows * a.runs, WAVES / W), THREADS, 0, st>>>(a);
+    return hipGetLastError();
+  });
+}
+
+template <typename T, int W, int MODE> hipError_t launch(LogitsArgs a, hipStream_t st) {
+  constexpr bool is_bf16 = sizeof(T) == 2;
+  constexpr int TILE = THREADS * STEP * vec<T>();
+  if (!a.dz) return values<T, W, MODE>(a, st);
+  a.runs = 1;
+  a.run_cols = a.cols;
+  if (a.lse_in || a.parts > 1) {
+    if (W > 1) {
+      a.run_cols = TILE;
+      a.runs = (a.cols + TILE - 1) / TILE;
+    }
+    if (a.lse_in) return gradient<T, W, MODE, GIVEN>(a, st);
+    const hipError_t e = values<T, W, MODE>(a, st);
+    return e != hipSuccess ? e : gradient<T, W, MODE, PARTS>(a, st);
+  }
+  (void)is_bf16;
+  return gradient<T, W, MODE, HERE>(a, st);
+}
+
+}  // namespace
+
+size_t logits_workspace_bytes(long rows, int cols, bool is_bf16, int top_k, int points) {
+  const int parts = parts_of(rows, cols, is_bf16);
+  if (parts == 1) return 0;
+  return up256(rows * parts * sizeof(f32x4)) + up256(rows * parts * top_k * sizeof(u64)) + up256((size_t)rows * points * sizeof(float));
+}
+
+hipError_t launch_logits(LogitsArgs a, int mode, bool is_bf16, void* workspace, hipStream_t st) {
+  if (a.rows == 0) return hipSuccess;
+  const double elems = (double)a.rows * a.cols, size = is_bf16 ? 2 : 4;
+  ProfScope ps(a.lse_in ? PC_LOGITS_GRAD : a.dz ? PC_LOGITS_STEP : PC_LOGITS, elems * (a.dz && !a.lse_in ? 10 : 6), elems * size * (a.dz ? 2 : 1), st);
+  a.parts = a.lse_in ? 1 : parts_of(a.rows, a.cols, is_bf16);
+  a.part_cols = a.cols;
+  a.points = mode == 0 ? 1 : a.kept;
+  if (a.parts > 1) {
+    // whole 128-byte lines apart, but for the rows' own alignment
+    a.part_cols = ((a.cols + a.parts - 1) / a.parts + 63) / 64 * 64;
+    a.parts = (a.cols + a.part_cols - 1) / a.part_cols;
+    char* at = static_cast<char*>(workspace);
+    a.part_sums = reinterpret_cast<f32x4*>(at);
+    at += up256(a.rows * a.parts * sizeof(f32x4));
+    a.part_lists = reinterpret_cast<unsigned long long*>(at);
+    at += up256(a.rows * a.parts * a.top_k * sizeof(u64));
+    a.part_points = a.dz ? reinterpret_cast<float*>(at) : nullptr;
+  }
+  return with(is_bf16, [&](auto b) {
+    typedef typename std::conditional<decltype(b)::value, bf16, float>::type T;
+    return with(short_rows(a.cols, is_bf16), [&](auto s) {
+      constexpr int W = decltype(s)::value ? 1 : WAVES;
+      return with(mode == 0, [&](auto m) { return launch<T, W, decltype(m)::value ? 0 : 1>(a, st); });
+    });
+  });
+}
+
+}  // namespace mg

@@ -1,5 +1,6 @@
-// Exported operators beside the layer solves: rows kept in 8 bits, LayerNorm on its own, gradients from kept rows.
-// Host code that checks arguments and enqueues; the kernels are in q8.hip, norm.hip and q8_grad.hip.
+// Exported operators beside the layer solves: rows kept in 8 bits, LayerNorm on its own, gradients from kept rows, and what
+// lies between logits and their gradient.
+// Host code that checks arguments and enqueues; the kernels are in q8.hip, norm.hip, q8_grad.hip and logits.hip.
 #include <math.h>
 
 #include "../../include/mgrit.h"
@@ -21,6 +22,7 @@ constexpr int64_t MOST_ROWS = 0x7fffffff;
 constexpr int32_t MOST_NORM_COLS = 16384;              // a row lies in the registers of 1024 lanes
 constexpr int64_t MOST_ELEMENTS = (int64_t)1 << 40, MOST_WEIGHTS = (int64_t)1 << 31;
 constexpr int32_t MOST_FEATURES = 1 << 24;
+constexpr int32_t MOST_LOGITS = 1 << 24;
 constexpr int64_t MOST_TOKENS = MOST_ROWS - 255;       // the index of a token behind the last one, in its tile, has 32 bits
 
 bool known(int dtype) { return dtype == MGRIT_DTYPE_F32 || dtype == MGRIT_DTYPE_BF16; }
@@ -60,6 +62,43 @@ int check_workspace(size_t need, const void* workspace, size_t bytes) {
   return bytes < need ? MGRIT_WORKSPACE_TOO_SMALL : MGRIT_OK;
 }
 int enqueued(hipError_t e) { return e == hipSuccess ? MGRIT_OK : hip_failed(e); }
+int check_logits(const mgrit_logits_desc* d) {
+  if (!d || d->rows < 0 || d->cols < 1 || !known(d->dtype) || (d->id_dtype != MGRIT_IDS_I32 && d->id_dtype != MGRIT_IDS_I64)) return MGRIT_INVALID_ARG;
+  if (!(d->temperature >= 1e-4f && d->temperature <= 1e4f)) return MGRIT_INVALID_ARG;
+  return d->cols > MOST_LOGITS || d->rows > MOST_ROWS ? MGRIT_UNSUPPORTED : MGRIT_OK;
+}
+int check_top(const mgrit_logits_desc* d, int32_t top_k) {
+  if (top_k < 0 || top_k > d->cols) return MGRIT_INVALID_ARG;
+  return top_k > MGRIT_TOP_MOST ? MGRIT_UNSUPPORTED : MGRIT_OK;
+}
+int check_kept(int32_t kept) { return kept < 1 ? MGRIT_INVALID_ARG : kept > MGRIT_KEPT_MOST ? MGRIT_UNSUPPORTED : MGRIT_OK; }
+int check_ids(const mgrit_logits_desc* d, const void* ids) {
+  return d->rows == 0 || (ids && aligned(ids, d->id_dtype == MGRIT_IDS_I64 ? 8 : 4)) ? MGRIT_OK : MGRIT_INVALID_ARG;
+}
+int check_floats(const mgrit_logits_desc* d, const float* p) { return d->rows == 0 || (p && aligned(p, 4)) ? MGRIT_OK : MGRIT_INVALID_ARG; }
+int check_teacher(const mgrit_logits_desc* d, const mgrit_teacher* t) {
+  if (!t || !known(t->dtype)) return MGRIT_INVALID_ARG;
+  STCHK(check_kept(t->kept));
+  STCHK(check_ids(d, t->ids));
+  return d->rows && (!t->logits || !element_aligned(t->logits, t->dtype) || !aligned(t->lse, 4)) ? MGRIT_INVALID_ARG : MGRIT_OK;
+}
+// gradients beside the logits, or in their place
+int check_dlogits(const mgrit_logits_desc* d, const void* logits, int64_t stride, const void* dlogits, int64_t dstride) {
+  STCHK(check_rows(d->rows, d->cols, dlogits, dstride, d->dtype));
+  return d->rows && logits == dlogits && stride != dstride ? MGRIT_INVALID_ARG : MGRIT_OK;
+}
+LogitsArgs logits_args(const mgrit_logits_desc* d, const void* logits, int64_t stride) {
+  LogitsArgs a = {};
+  a.rows = d->rows; a.cols = d->cols; a.z = logits; a.ld = stride; a.tau = d->temperature; a.wide_ids = d->id_dtype == MGRIT_IDS_I64;
+  return a;
+}
+void add_teacher(LogitsArgs& a, const mgrit_teacher* t) {
+  a.kept = t->kept; a.teacher_ids = t->ids; a.teacher = t->logits; a.teacher_bf16 = t->dtype == MGRIT_DTYPE_BF16; a.teacher_lse = t->lse;
+}
+int enqueue_logits(const mgrit_logits_desc* d, const LogitsArgs& a, int mode, void* workspace, void* stream) {
+  std::lock_guard<std::recursive_mutex> call_lock(call_mutex());
+  return enqueued(launch_logits(a, mode, d->dtype == MGRIT_DTYPE_BF16, workspace, static_cast<hipStream_t>(stream)));
+}
 Q8Rows kept(int64_t rows, int32_t cols, const void* q, const void* scale) {
   return Q8Rows{static_cast<unsigned char*>(const_cast<void*>(q)), static_cast<unsigned char*>(const_cast<void*>(scale)), rows, cols};
 }
@@ -158,6 +197,114 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
   a.xq = static_cast<const unsigned char*>(x_q8); a.xs = static_cast<const unsigned char*>(x_q8_scale);
   a.blocks = (int)q8_blocks(in_features); a.dW = dW; a.db = db; a.scale = scale;
   return enqueued(launch_q8_grad(a, dy_dtype == MGRIT_DTYPE_BF16, static_cast<float*>(workspace), static_cast<hipStream_t>(stream)));
+}
+
+size_t mgrit_token_logprobs_workspace_bytes(const mgrit_logits_desc* desc, int32_t top_k) {
+  if (check_logits(desc) != MGRIT_OK || check_top(desc, top_k) != MGRIT_OK) return 0;
+  return logits_workspace_bytes(desc->rows, desc->cols, desc->dtype == MGRIT_DTYPE_BF16, top_k, 1);
+}
+
+int mgrit_token_logprobs_forward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const void* tokens, float* logprob,
+                                 float* entropy, float* lse, int32_t top_k, void* top_ids, float* top_logprobs, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  STCHK(check_logits(desc));
+  STCHK(check_top(desc, top_k));
+  STCHK(check_rows(desc->rows, desc->cols, logits, stride, desc->dtype));
+  if (logprob || tokens) STCHK(check_ids(desc, tokens));
+  if (!logprob && !entropy && !lse && !top_k) return MGRIT_INVALID_ARG;
+  if (!aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4)) return MGRIT_INVALID_ARG;
+  if ((logprob && (logprob == entropy || logprob == lse)) || (entropy && entropy == lse)) return MGRIT_INVALID_ARG;
+  if (top_k) {
+    STCHK(check_ids(desc, top_ids));
+    STCHK(check_floats(desc, top_logprobs));
+    if (desc->rows && (top_ids == top_logprobs || top_ids == tokens || top_logprobs == logprob || top_logprobs == entropy || top_logprobs == lse)) return MGRIT_INVALID_ARG;
+  }
+  STCHK(check_workspace(mgrit_token_logprobs_workspace_bytes(desc, top_k), workspace, workspace_bytes));
+  LogitsArgs a = logits_args(desc, logits, stride);
+  a.tokens = tokens; a.logprob = logprob; a.entropy = entropy; a.lse = lse; a.top_k = top_k; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
+  return enqueue_logits(desc, a, 0, workspace, stream);
+}
+
+int mgrit_token_logprobs_backward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const void* tokens, const float* lse,
+                                  const float* g_logprob, const float* entropy, const float* g_entropy, void* dlogits,
+                                  int64_t dlogits_stride, void* stream) {
+  STCHK(check_logits(desc));
+  STCHK(check_rows(desc->rows, desc->cols, logits, stride, desc->dtype));
+  STCHK(check_ids(desc, tokens));
+  STCHK(check_floats(desc, lse));
+  STCHK(check_floats(desc, g_logprob));
+  if (g_entropy) {
+    STCHK(check_floats(desc, entropy));
+    STCHK(check_floats(desc, g_entropy));
+  }
+  STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
+  LogitsArgs a = logits_args(desc, logits, stride);
+  a.tokens = tokens; a.lse_in = lse; a.entropy_in = entropy; a.g = g_logprob; a.h = g_entropy; a.dz = dlogits; a.lddz = dlogits_stride;
+  return enqueue_logits(desc, a, 0, nullptr, stream);
+}
+
+int mgrit_token_logprobs_step(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const void* tokens, const float* g_logprob,
+                              const float* g_entropy, float* logprob, float* entropy, float* lse, void* dlogits, int64_t dlogits_stride,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  STCHK(check_logits(desc));
+  STCHK(check_rows(desc->rows, desc->cols, logits, stride, desc->dtype));
+  STCHK(check_ids(desc, tokens));
+  STCHK(check_floats(desc, g_logprob));
+  if (!aligned(g_entropy, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4)) return MGRIT_INVALID_ARG;
+  if ((logprob && (logprob == entropy || logprob == lse)) || (entropy && entropy == lse)) return MGRIT_INVALID_ARG;
+  STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
+  STCHK(check_workspace(mgrit_token_logprobs_workspace_bytes(desc, 0), workspace, workspace_bytes));
+  LogitsArgs a = logits_args(desc, logits, stride);
+  a.tokens = tokens; a.logprob = logprob; a.entropy = entropy; a.lse = lse; a.g = g_logprob; a.h = g_entropy; a.dz = dlogits; a.lddz = dlogits_stride;
+  return enqueue_logits(desc, a, 0, workspace, stream);
+}
+
+size_t mgrit_distill_workspace_bytes(const mgrit_logits_desc* desc, int32_t kept) {
+  if (check_logits(desc) != MGRIT_OK || check_kept(kept) != MGRIT_OK) return 0;
+  return logits_workspace_bytes(desc->rows, desc->cols, desc->dtype == MGRIT_DTYPE_BF16, 0, kept);
+}
+
+int mgrit_distill_forward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const mgrit_teacher* teacher, float* loss,
+                          float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  STCHK(check_logits(desc));
+  STCHK(check_rows(desc->rows, desc->cols, logits, stride, desc->dtype));
+  STCHK(check_teacher(desc, teacher));
+  STCHK(check_floats(desc, loss));
+  if (!aligned(lse, 4) || (desc->rows && loss == lse)) return MGRIT_INVALID_ARG;
+  STCHK(check_workspace(mgrit_distill_workspace_bytes(desc, teacher->kept), workspace, workspace_bytes));
+  LogitsArgs a = logits_args(desc, logits, stride);
+  add_teacher(a, teacher);
+  a.loss = loss; a.lse = lse;
+  return enqueue_logits(desc, a, 1, workspace, stream);
+}
+
+int mgrit_distill_backward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const mgrit_teacher* teacher, const float* lse,
+                           const float* g_loss, void* dlogits, int64_t dlogits_stride, void* stream) {
+  STCHK(check_logits(desc));
+  STCHK(check_rows(desc->rows, desc->cols, logits, stride, desc->dtype));
+  STCHK(check_teacher(desc, teacher));
+  STCHK(check_floats(desc, lse));
+  if (!aligned(g_loss, 4)) return MGRIT_INVALID_ARG;
+  STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
+  LogitsArgs a = logits_args(desc, logits, stride);
+  add_teacher(a, teacher);
+  a.lse_in = lse; a.g = g_loss; a.dz = dlogits; a.lddz = dlogits_stride;
+  return enqueue_logits(desc, a, 1, nullptr, stream);
+}
+
+int mgrit_distill_step(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const mgrit_teacher* teacher, const float* g_loss,
+                       float* loss, float* lse, void* dlogits, int64_t dlogits_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  STCHK(check_logits(desc));
+  STCHK(check_rows(desc->rows, desc->cols, logits, stride, desc->dtype));
+  STCHK(check_teacher(desc, teacher));
+  STCHK(check_floats(desc, loss));
+  if (!aligned(g_loss, 4) || !aligned(lse, 4) || (desc->rows && loss == lse)) return MGRIT_INVALID_ARG;
+  STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
+  STCHK(check_workspace(mgrit_distill_workspace_bytes(desc, teacher->kept), workspace, workspace_bytes));
+  LogitsArgs a = logits_args(desc, logits, stride);
+  add_teacher(a, teacher);
+  a.loss = loss; a.lse = lse; a.g = g_loss; a.dz = dlogits; a.lddz = dlogits_stride;
+  return enqueue_logits(desc, a, 1, workspace, stream);
 }
 
 }  // extern "C"

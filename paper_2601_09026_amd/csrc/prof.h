@@ -12,7 +12,8 @@ enum ProfClass : int {
   PC_GEMM_MFMA_SINGLE = 16,  // + epilogue id: one group per launch (the serial coarse chain)
   PC_CHAIN = 24,             // row-local chains of a narrow layer
   PC_Q8 = 25, PC_NORM_FWD = 26, PC_NORM_BWD = 27, PC_Q8_GRAD = 28,   // rows in 8 bits, LayerNorm on its own, gradients
-  PC_COUNT = 29
+  PC_LOGITS = 29, PC_LOGITS_GRAD = 30, PC_LOGITS_STEP = 31,   // rows of logits: values, gradients, both
+  PC_COUNT = 32
 };
 
 bool prof_enabled();
