@@ -19,6 +19,8 @@ constexpr float LOWEST = -3.402823466e38f, LOG2E = 1.44269504088896340736f;
 constexpr int THREADS = 256, WAVES = THREADS / WAVE;
 constexpr int STEP = 4;                                  // vectors of a lane that are loaded together
 constexpr int LIST = 256;                                // candidates of a wavefront
+constexpr int ROOM = LIST + 4 + 64;
+constexpr int GROUPS = 8;                                // groups of a lane's elements whose maxima are kept
 typedef unsigned long long u64;
 
 template <typename T> constexpr int vec() { return 16 / (int)sizeof(T); }
@@ -36,6 +38,10 @@ template <typename T> struct Run {
   }
   __device__ __forceinline__ int odd_at(int i) const { return i < head ? i : i + vecs * vec<T>(); }
   __device__ __forceinline__ int vec_at(int v) const { return head + v * vec<T>(); }
+  // Chunks of STEP vectors per lane of W wavefronts; 2^fold of them are a group, at most GROUPS a run
+  template <int W> __device__ __forceinline__ int chunks() const { return vecs ? (vecs - 1) / (STEP * W * WAVE) + 1 : 1; }
+  template <int W> __device__ __forceinline__ int fold() const { return chunks<W>() <= GROUPS ? 0 : 32 - __builtin_clz((chunks<W>() - 1) / GROUPS); }
+  template <int W> __device__ __forceinline__ int groups() const { return ((chunks<W>() - 1) >> fold<W>()) + 1; }
 };
 
 template <typename T> __device__ __forceinline__ void decode(u32x4 r, float (&x)[vec<T>()]);
@@ -61,21 +67,26 @@ template <> __device__ __forceinline__ u32x4 encode<bf16>(const float (&x)[8]) {
   return __builtin_bit_cast(u32x4, b);
 }
 
+__device__ __forceinline__ long block_index() { return (long)blockIdx.y * gridDim.x + blockIdx.x; }
+
 __device__ __forceinline__ long id_of(const void* ids, long i, bool wide) {
   return wide ? static_cast<const int64_t*>(ids)[i] : (long)static_cast<const int32_t*>(ids)[i];
 }
 
 // ---- sums of exponentials ----------------------------------------------------------
-// s = sum 2^((x - m) c), t = sum (x - m) c 2^((x - m) c) over the values seen, m their maximum, c = log2(e) / tau.  The
-// difference is taken before it is scaled: equal values of any size have the exponent 0.  A NaN or +infinity makes s NaN.
-// Exponents of -160 and less, -infinity among them, have 2^a = 0, and 0 in t.
-struct Sums { float m = LOWEST, s = 0.f, t = 0.f; };
+// s = sum 2^((x - m) c), t = sum (x - m) c 2^((x - m) c) over the values seen, m one of them, c = log2(e) / tau.  A NaN or
+// +infinity makes s NaN.  Exponents of -160 and less, -infinity among them, have 2^a = 0, and 0 in t.
+struct Sums { float m, s, t; };
 __device__ __forceinline__ float bounded(float a) { return fmaxf(a, -160.f); }
+__device__ __forceinline__ float exp2_of(float a) { return __builtin_amdgcn_exp2f(a); }
 
+__device__ __forceinline__ void shift(float& s, float& t, float d) {     // every exponent d higher
+  const float f = exp2_of(d);
+  t = f * (t + d * s);
+  s = f * s;
+}
 __device__ __forceinline__ void raise(Sums& a, float m, float c) {
-  const float d = bounded((a.m - m) * c), f = __builtin_amdgcn_exp2f(d);
-  a.t = f * (a.t + d * a.s);
-  a.s = f * a.s;
+  shift(a.s, a.t, bounded((a.m - m) * c));
   a.m = m;
 }
 __device__ __forceinline__ void merge(Sums& a, Sums b, float c) {
@@ -85,22 +96,40 @@ __device__ __forceinline__ void merge(Sums& a, Sums b, float c) {
   a.s += b.s;
   a.t += b.t;
 }
-template <int N> __device__ __forceinline__ void add(Sums& a, const float (&x)[N], float top, float c) {
-  raise(a, fmaxf(a.m, top), c);
-  float s = 0.f, t = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float d = (x[i] - a.m) * c, e = __builtin_amdgcn_exp2f(d);
-    s += e;
-    t = fmaf(bounded(d), e, t);
+__device__ __forceinline__ Sums wave_merge(Sums a, float c) {
+  raise(a, wave_max(a.m), c);
+  return Sums{a.m, wave_sum(a.s), wave_sum(a.t)};
+}
+
+// A wavefront's sums while it reads.  All lanes refer to one m, which lags behind the maximum: it is raised where a value has an
+// exponent above 8, so that nothing is rescaled as a rule and the exponents of the largest terms keep 20 bits behind the point.
+// An exponent is one instruction, x c - P with P = m c rounded; what was rounded off is the same for all, rest = m c - P,
+// and taken out at the end.  Where |m c| is so large that the rest is no small number (FAR) the difference is taken before it is scaled.
+template <bool T_SUM> struct Reader {
+  float c, m, P, rest, s, t;                             // c to rest are the same in all lanes
+  bool far;
+  __device__ __forceinline__ void start(float scale) { c = scale; m = LOWEST; P = rest = s = t = 0.f; far = true; }
+  __device__ __forceinline__ bool low(float most) const { return __any((most - m) * c > 8.f); }
+  __device__ __forceinline__ void lift(float most) {
+    const float top = fmaxf(wave_max(most), m), product = top * c;
+    const bool beyond = !(fabsf(product) < 0x1p20f);
+    const float left = beyond ? 0.f : fmaf(top, c, -product);
+    shift(s, t, bounded((m - top) * c - rest + left));
+    m = top; P = product; rest = left; far = beyond;
   }
-  a.s += s;
-  a.t += t;
-}
-__device__ __forceinline__ void wave_merge(Sums& a, float c) {
+  template <bool FAR, int N> __device__ __forceinline__ void add(const float (&x)[N], float& s_, float& t_) const {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) merge(a, Sums{__shfl_xor(a.m, o, 64), __shfl_xor(a.s, o, 64), __shfl_xor(a.t, o, 64)}, c);
-}
+    for (int j = 0; j < N; ++j) {
+      const float a = FAR ? (x[j] - m) * c : fmaf(x[j], c, -P), e = exp2_of(a);
+      s_ += e;
+      if constexpr (T_SUM) t_ = fmaf(bounded(a), e, t_);
+    }
+  }
+  __device__ __forceinline__ Sums finish() {             // the wavefront's, in all lanes
+    shift(s, t, -rest);
+    return Sums{m, wave_sum(s), T_SUM ? wave_sum(t) : 0.f};
+  }
+};
 
 // What a row's sums come to.  lse: +-infinity where the row's largest quotient by tau is: no distribution (-infinity: zeros
 // in place of p) or, as with a NaN among the logits, NaN.
@@ -125,8 +154,10 @@ struct RowSums {
 
 // ---- the largest elements ------------------------------------------------------------
 // A candidate is one number: the value's order in the upper half, the complement of its index below, so that the greater
-// of two comes first and equal values come by index.  Each wavefront has a list of candidates in LDS, the threshold below
-// which nothing can be among the row's k largest, and sorts the list down to k when it is full.
+// of two comes first and equal values come by index.  While a row is read each lane keeps the largest of its elements, and of
+// each group of them.  A value that k lanes' largest reach is a bar below which nothing can be among the k largest; the
+// groups that reach it, little more than k, are read again.  What they hold goes to a list in LDS, one per wavefront, which
+// is sorted down to k when it is full.
 __device__ __forceinline__ u64 candidate(float x, int index) {
   const unsigned b = f_bits(x + 0.f);                    // (-0 and 0 are equal)
   return (u64)(b ^ ((unsigned)((int)b >> 31) | 0x80000000u)) << 32 | (unsigned)~index;
@@ -145,47 +176,46 @@ __device__ __forceinline__ void wave_sync() {            // LDS accesses of a wa
 }
 
 struct Top {
-  u64* list;                                             // [LIST] of this wavefront
-  int k, n;                                              // n: candidates in it
+  u64* list;                                             // [ROOM] of this wavefront: candidates, zeros behind them, the sorted ones
+  float* groups;                                         // [GROUPS][THREADS], an entry per group for this lane
+  int k, n;                                              // n: candidates in the list
   u64 floor;                                             // only what is greater is taken
-  float bar;                                             // the value of floor
-  __device__ __forceinline__ void start(u64* lds, int want) { list = lds; k = want; n = 0; floor = 0; bar = -__builtin_inff(); }
-  // A value that at least k lanes reach (all of them, if fewer have any)
-  __device__ __forceinline__ void first_bar(float most) {
-    int above = 0;
-    for (int l = 0; l < WAVE; ++l) above += bits_f((unsigned)__builtin_amdgcn_readlane((int)f_bits(most), l)) > most;
-    float b = above < k ? most : __builtin_inff();
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) b = fminf(b, __shfl_xor(b, o, 64));
-    bar = b;
-    floor = uniform(candidate(b, -1));                   // (the lowest of that value)
+  float best, first;                                     // the lane's largest element; its odd element
+  __device__ __forceinline__ void start(u64* lists, float* lds_groups, int want) {
+    list = lists + threadIdx.x / WAVE * ROOM;
+    groups = lds_groups + threadIdx.x;
+    k = want; n = 0; floor = 0; best = first = -__builtin_inff();
   }
-  // sorts the list, k of it stay
+  // The largest number of 16 bits, in the order of candidates' upper halves, that `want` lanes' largest elements reach
+  __device__ __forceinline__ unsigned reached(int want) const {
+    const unsigned mine = (unsigned)(candidate(best, 0) >> 32);
+    unsigned low = 0;
+#pragma unroll
+    for (unsigned bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
+      if (__popcll(__ballot(mine >= (low | bit))) >= want) low |= bit;
+    return low;
+  }
+  // sorts the list, the k first stay
   __device__ __forceinline__ void settle() {
     const int lane = threadIdx.x & 63;
+    if (lane < 4) list[n + lane] = 0;                                   // (read four at a time)
     wave_sync();
-    u64 own[LIST / WAVE];
-    int rank[LIST / WAVE];
+    u64* sorted = list + LIST + 4;
+    for (int i = lane; i - lane < n; i += WAVE) {
+      const u64 own = i < n ? list[i] : 0;
+      int rank = 0;
+      for (int j = 0; j < n; j += 4) {
 #pragma unroll
-    for (int i = 0; i < LIST / WAVE; ++i) {
-      own[i] = i * WAVE + lane < n ? list[i * WAVE + lane] : 0;
-      rank[i] = 0;
-    }
-    for (int j = 0; j < n; ++j) {
-      const u64 other = list[j];
-#pragma unroll
-      for (int i = 0; i < LIST / WAVE; ++i) rank[i] += other > own[i];
+        for (int u = 0; u < 4; ++u) rank += list[j + u] > own;
+      }
+      if (i < n && rank < k) sorted[rank] = own;
     }
     wave_sync();
-#pragma unroll
-    for (int i = 0; i < LIST / WAVE; ++i)
-      if (i * WAVE + lane < n && rank[i] < k) list[rank[i]] = own[i];
+    const int kept = n < k ? n : k;
+    if (lane < kept) list[lane] = sorted[lane];
     wave_sync();
-    if (n >= k) {
-      n = k;
-      floor = uniform(list[k - 1]);
-      bar = value_of(floor);
-    }
+    n = kept;
+    if (n == k) floor = uniform(list[k - 1]);
   }
   // the lanes' keys, where one is given
   __device__ __forceinline__ void take(bool given, u64 key) {
@@ -196,13 +226,6 @@ struct Top {
     n += __popcll(who);
     if (n > LIST - WAVE) settle();
   }
-  // a vector per lane
-  template <int N> __device__ __forceinline__ void vector(const float (&x)[N], float most, int index, bool inside) {
-    if (!__any(inside && most >= bar)) return;
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (__any(inside && x[j] >= bar)) take(inside && x[j] >= bar, candidate(x[j], index + j));
-  }
   // the rest of the list is empty
   __device__ __forceinline__ void finish() {
     settle();
@@ -212,66 +235,169 @@ struct Top {
   }
 };
 
-// ---- a row's sums (and its largest elements), by `team` lanes -------------------------
-template <typename T, bool TOP> __device__ __forceinline__ void read_run(const Run<T>& r, int lane, int team, int index, float c, Sums& sums, Top& top) {
-  constexpr int N = vec<T>();
+// ---- a row's sums (and its largest elements), by W wavefronts ---------------------------
+template <typename T> constexpr unsigned NOTHING = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;          // -infinity
+
+// The team's wavefronts go through the run's chunks of STEP vectors per lane.
+template <typename T, int W, bool T_SUM, bool TOP>
+__device__ __forceinline__ Sums read_run(const Run<T>& r, int lane, float c, Top& top) {
+  constexpr int N = vec<T>(), team = W * WAVE;
   const float none = -__builtin_inff();
-  for (int v0 = 0; v0 < r.vecs; v0 += STEP * team) {
+  Reader<T_SUM> sums;
+  sums.start(c);
+  const bool odd = lane < r.odd;                         // (odd < 2 N: lanes of the first wavefront)
+  const float first[1] = {odd ? to_f(r.p[r.odd_at(lane)]) : none};
+  float group = none;
+  for (int v0 = 0, chunk = 0; v0 == 0 || v0 < r.vecs; v0 += STEP * team, ++chunk) {
     u32x4 raw[STEP];
-#pragma unroll
-    for (int u = 0; u < STEP; ++u) {
-      const int v = v0 + u * team + lane;
-      raw[u] = ld_stream(reinterpret_cast<const u32x4*>(r.p + r.vec_at(v < r.vecs ? v : r.vecs - 1)));
-    }
-    float x[STEP * N], most[STEP], all = none;
-#pragma unroll
-    for (int u = 0; u < STEP; ++u) {
-      const bool inside = v0 + u * team + lane < r.vecs;
-      float e[N];
-      decode<T>(raw[u], e);
-      most[u] = none;
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        x[u * N + j] = inside ? e[j] : none;
-        most[u] = fmaxf(most[u], x[u * N + j]);
-      }
-      all = fmaxf(all, most[u]);
-    }
-    add(sums, x, all, c);
-    if constexpr (TOP) {
-      if (v0 == 0) top.first_bar(all);
+    if (r.vecs) {
 #pragma unroll
       for (int u = 0; u < STEP; ++u) {
         const int v = v0 + u * team + lane;
-        float e[N];
+        raw[u] = ld_stream(reinterpret_cast<const u32x4*>(r.p + r.vec_at(v < r.vecs ? v : r.vecs - 1)));
+      }
+    }
+    auto steps = [&](auto f) {                           // the chunk's vectors
 #pragma unroll
-        for (int j = 0; j < N; ++j) e[j] = x[u * N + j];
-        top.vector(e, most[u], index + r.vec_at(v), v < r.vecs);
+      for (int u = 0; u < STEP; ++u)
+        if (v0 + u * team < r.vecs) {
+          float x[N];
+          u32x4 again = raw[u];
+          asm("" : "+v"(again));                         // (decoded anew in every pass: a chunk's 32 values are not kept)
+          decode<T>(again, x);
+          f(x, u);
+        }
+    };
+    if (v0 + STEP * team > r.vecs) {
+#pragma unroll
+      for (int u = 0; u < STEP; ++u)
+        if (v0 + u * team + lane >= r.vecs) raw[u] = u32x4{NOTHING<T>, NOTHING<T>, NOTHING<T>, NOTHING<T>};
+    }
+    float most[STEP], all = none;
+    auto maxima = [&](const float (&x)[N], int u) {
+      most[u] = none;
+#pragma unroll
+      for (int j = 0; j < N; ++j) most[u] = fmaxf(most[u], x[j]);
+    };
+    auto overall = [&]() {
+      all = first[0];
+      if (v0) all = none;
+#pragma unroll
+      for (int u = 0; u < STEP; ++u) all = fmaxf(all, most[u]);
+    };
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) most[u] = none;
+    if (v0 == 0) {
+      steps(maxima);
+      overall();
+      sums.lift(all);
+      if (r.odd) {
+        if (sums.far) sums.template add<true>(first, sums.s, sums.t);
+        else sums.template add<false>(first, sums.s, sums.t);
+      }
+    }
+    for (;;) {
+      float s = 0.f, t = 0.f;
+      if (sums.far) {
+        steps([&](const float (&x)[N], int u) { maxima(x, u); sums.template add<true>(x, s, t); });
+      } else {
+        steps([&](const float (&x)[N], int u) { maxima(x, u); sums.template add<false>(x, s, t); });
+      }
+      overall();
+      if (!sums.low(all)) {
+        sums.s += s;
+        sums.t += t;
+        break;
+      }
+      sums.lift(all);
+    }
+    if constexpr (TOP) {
+      group = fmaxf(group, all);
+      if (((chunk + 1) & ((1 << r.template fold<W>()) - 1)) == 0 || v0 + STEP * team >= r.vecs) {
+        top.groups[(chunk >> r.template fold<W>()) * THREADS] = group;
+        top.best = fmaxf(top.best, group);
+        group = none;
       }
     }
   }
-  if (r.odd) {
-    const bool inside = lane < r.odd;                    // (odd < 2 N, no more than a wavefront)
-    const float x[1] = {inside ? to_f(r.p[r.odd_at(lane)]) : none};
-    add(sums, x, x[0], c);
-    if constexpr (TOP) top.vector(x, x[0], index + r.odd_at(lane), inside);
-  }
+  if constexpr (TOP) top.first = first[0];
+  return sums.finish();
 }
 
-// What a team of several wavefronts found, in the first wavefront.  (All of the block's threads.)
-template <int W, bool TOP> __device__ __forceinline__ void join_waves(Sums& sums, Top& top, f32x4* lds_sums, u64* lds_lists, float c) {
-  wave_merge(sums, c);
-  if constexpr (TOP) top.finish();
+// The candidates among a lane's elements: those of its groups that reach the bar are read again
+template <typename T, int W> __device__ __forceinline__ void pick(const Run<T>& r, int lane, int index, unsigned low, Top& top) {
+  constexpr int N = vec<T>(), team = W * WAVE;
+  const float bar = low > 0x007fffffu ? value_of((u64)low << 32) : -__builtin_inff();
+  const int fold = r.template fold<W>(), groups = r.template groups<W>();
+  top.take(lane < r.odd && top.first >= bar, candidate(top.first, index + r.odd_at(lane)));
+  unsigned hit = 0;
+  for (int g = 0; g < groups; ++g) hit |= top.groups[g * THREADS] >= bar ? 1u << g : 0u;
+  if (r.vecs == 0) hit = 0;
+  while (__any(hit != 0)) {
+    const int g = hit ? __builtin_ctz(hit) : 0;
+    for (int i = 0; i < 1 << fold; ++i) {
+      const int v0 = ((g << fold) + i) * (STEP * team) + lane;
+      u32x4 raw[STEP];
+#pragma unroll
+      for (int u = 0; u < STEP; ++u) {
+        const int v = v0 + u * team;
+        raw[u] = ld_global(reinterpret_cast<const u32x4*>(r.p + r.vec_at(hit && v < r.vecs ? v : 0)));
+      }
+      unsigned high = 0;                                 // elements that reach it, a bit each
+#pragma unroll
+      for (int u = STEP - 1; u >= 0; --u) {
+        const bool inside = hit && v0 + u * team < r.vecs;
+        float x[N];
+        decode<T>(raw[u], x);
+#pragma unroll
+        for (int j = N - 1; j >= 0; --j) high = high << 1 | (unsigned)(inside && x[j] >= bar);
+      }
+      while (__any(high != 0)) {
+        const int e = high ? __builtin_ctz(high) : 0, u = e / N, j = e % N;
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w[i] = raw[0][i];
+#pragma unroll
+          for (int o = 1; o < STEP; ++o) w[i] = u == o ? raw[o][i] : w[i];
+        }
+        const int d = sizeof(T) == 2 ? j >> 1 : j;
+        const unsigned lo = d & 1 ? w[1] : w[0], hi = d & 1 ? w[3] : w[2], word = d & 2 ? hi : lo;
+        const float x = bits_f(sizeof(T) == 4 ? word : j & 1 ? word & 0xffff0000u : word << 16);
+        top.take(high != 0, candidate(x, index + r.vec_at(v0 + u * team) + j));
+        high &= high - 1;
+      }
+    }
+    hit &= hit - 1;
+  }
+  top.finish();
+}
+
+// What a team's wavefronts found: the sums in all of them, the list in the first.
+template <typename T, int W, bool TOP>
+__device__ __forceinline__ void join_waves(const Run<T>& r, int lane, int index, Sums& sums, Top& top, f32x4* waves, u64* lists, float c) {
+  unsigned low = 0;
+  if constexpr (TOP) low = top.reached((top.k + W - 1) / W);
   if constexpr (W > 1) {
     const int wave = threadIdx.x / WAVE;
-    if ((threadIdx.x & 63) == 0) lds_sums[wave] = f32x4{sums.m, sums.s, sums.t, 0.f};
+    if ((threadIdx.x & 63) == 0) waves[wave] = f32x4{sums.m, sums.s, sums.t, bits_f(low)};
     __syncthreads();
-    if (wave == 0) {
+    Sums all = {waves[0][0], waves[0][1], waves[0][2]};
+    low = f_bits(waves[0][3]);
 #pragma unroll
-      for (int w = 1; w < W; ++w) merge(sums, Sums{lds_sums[w][0], lds_sums[w][1], lds_sums[w][2]}, c);
-      if constexpr (TOP) {
-        const int lane = threadIdx.x & 63;
-        for (int w = 1; w < W; ++w) top.take(lane < top.k, lane < top.k ? lds_lists[w * LIST + lane] : 0);
+    for (int w = 1; w < W; ++w) {
+      merge(all, Sums{waves[w][0], waves[w][1], waves[w][2]}, c);
+      const unsigned other = f_bits(waves[w][3]);        // (k / W of every wavefront's lanes reach the least of these)
+      low = other < low ? other : low;
+    }
+    sums = all;
+  }
+  if constexpr (TOP) {
+    pick<T, W>(r, lane, index, low, top);
+    if constexpr (W > 1) {
+      __syncthreads();
+      if (threadIdx.x < WAVE) {
+        for (int w = 1; w < W; ++w) top.take(lane < top.k, lane < top.k ? lists[w * ROOM + lane] : 0);
         top.finish();
       }
     }
@@ -380,24 +506,26 @@ __device__ __forceinline__ void put_alternatives(const LogitsArgs& a, long row, 
 // ---- values of a row --------------------------------------------------------------------
 // Teams of W wavefronts walk (row, part) pairs; with several parts a row's sums, lists and points go to the workspace.
 template <typename T, int W, bool TOP, int MODE>
-__global__ void __launch_bounds__(THREADS) logits_values_kernel(const LogitsArgs a) {
-  __shared__ u64 lists[TOP ? WAVES * LIST : 1];
+__global__ void __launch_bounds__(THREADS, 6) logits_values_kernel(const LogitsArgs a) {
+  __shared__ u64 lists[TOP ? WAVES * ROOM : 1];
   __shared__ f32x4 waves[WAVES];
+  __shared__ float groups[TOP ? GROUPS * THREADS : 1];
   constexpr int TEAMS = WAVES / W;
   const int wave = threadIdx.x / WAVE, lane = threadIdx.x % (W * WAVE);
   const float c = LOG2E / a.tau;
   const long tasks = a.rows * a.parts;
-  // (a team of the whole block always has a row; one of a single wavefront meets no barrier)
-  for (long task = (long)blockIdx.x * TEAMS + wave / W; task < tasks; task += (long)gridDim.x * TEAMS) {
+  const long task = block_index() * TEAMS + wave / W;
+  if (task >= tasks) return;                             // (a team of a whole block together; one of a wavefront meets no barrier)
+  {
     const long row = task / a.parts;
     const int part = (int)(task - row * a.parts), from = part * a.part_cols;
     const int n = a.cols - from < a.part_cols ? a.cols - from : a.part_cols;
     const T* z = static_cast<const T*>(a.z) + row * a.ld;
-    Sums sums;
     Top top;
-    if constexpr (TOP) top.start(lists + wave * LIST, a.top_k);
-    read_run<T, TOP>(Run<T>(z, from, n), lane, W * WAVE, from, c, sums, top);
-    join_waves<W, TOP>(sums, top, waves, lists, c);
+    if constexpr (TOP) top.start(lists, groups, a.top_k);
+    const Run<T> in(z, from, n);
+    Sums sums = read_run<T, W, MODE == 0, TOP>(in, lane, c, top);
+    join_waves<T, W, TOP>(in, lane, from, sums, top, waves, lists, c);
     if (wave % W == 0) {
       Points<MODE> pt;
       if (part == 0 && (a.parts == 1 || a.part_points)) {
@@ -419,25 +547,27 @@ __global__ void __launch_bounds__(THREADS) logits_values_kernel(const LogitsArgs
         }
       }
     }
-    if constexpr (W > 1) __syncthreads();
   }
 }
 
+// A row's sums from those of its parts (by a wavefront; MOST_PARTS <= 64)
 __device__ __forceinline__ Sums joined(const LogitsArgs& a, long row, float c) {
-  Sums all;
-  for (int p = 0; p < a.parts; ++p) {
-    const f32x4 s = a.part_sums[row * a.parts + p];
-    merge(all, Sums{s[0], s[1], s[2]}, c);
+  const int lane = threadIdx.x & 63;
+  Sums own = {LOWEST, 0.f, 0.f};
+  if (lane < a.parts) {
+    const f32x4 s = a.part_sums[row * a.parts + lane];
+    own = Sums{s[0], s[1], s[2]};
   }
-  return all;
+  return wave_merge(own, c);
 }
 
 // The parts' results, a wavefront per row
 template <typename T, bool TOP, int MODE>
 __global__ void __launch_bounds__(THREADS) logits_join_kernel(const LogitsArgs a) {
-  __shared__ u64 lists[TOP ? WAVES * LIST : 1];
+  __shared__ u64 lists[TOP ? WAVES * ROOM : 1];
   const int wave = threadIdx.x / WAVE, lane = threadIdx.x & 63;
-  for (long row = (long)blockIdx.x * WAVES + wave; row < a.rows; row += (long)gridDim.x * WAVES) {
+  const long row = block_index() * WAVES + wave;
+  if (row < a.rows) {
     const RowSums r(joined(a, row, LOG2E / a.tau), a.tau);
     Points<MODE> pt;
     pt.load(a, row);
@@ -445,9 +575,15 @@ __global__ void __launch_bounds__(THREADS) logits_join_kernel(const LogitsArgs a
     put_values<MODE>(a, row, r, pt);
     if constexpr (TOP) {
       Top top;
-      top.start(lists + wave * LIST, a.top_k);
+      top.start(lists, nullptr, a.top_k);
       const int all = a.parts * a.top_k;
       const u64* from = a.part_lists + row * all;
+      // each of the parts has (k / parts, rounded up) candidates that reach the least of their last
+      u64 low = ~0ull;
+      if (lane < a.parts) low = from[lane * a.top_k + (a.top_k + a.parts - 1) / a.parts - 1];
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) { const u64 other = __shfl_xor(low, o, 64); low = other < low ? other : low; }
+      top.floor = low ? low - 1 : 0;
       for (int i = 0; i < all; i += WAVE) top.take(i + lane < all, i + lane < all ? from[i + lane] : 0);
       top.finish();
       put_alternatives(a, row, r, top.list);
@@ -538,7 +674,9 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
   const int wave = threadIdx.x / WAVE, team = wave / W, lane = threadIdx.x % (W * WAVE);
   const float c = LOG2E / a.tau;
   const long tasks = a.rows * a.runs;
-  for (long task = (long)blockIdx.x * TEAMS + team; task < tasks; task += (long)gridDim.x * TEAMS) {
+  const long task = block_index() * TEAMS + team;
+  if (task >= tasks) return;
+  {
     const long row = task / a.runs;
     const int run = (int)(task - row * a.runs), from = run * a.run_cols;
     const int n = a.cols - from < a.run_cols ? a.cols - from : a.run_cols;
@@ -549,8 +687,8 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
     Sums sums;
     if constexpr (FROM == HERE) {
       Top none;
-      read_run<T, false>(in, lane, W * WAVE, 0, c, sums, none);
-      join_waves<W, false>(sums, none, waves, nullptr, c);
+      sums = read_run<T, W, MODE == 0, false>(in, lane, c, none);
+      join_waves<T, W, false>(in, lane, 0, sums, none, waves, nullptr, c);
     }
     if (wave % W == 0) {
       pt.load(a, row);
@@ -600,11 +738,12 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
 }
 
 // ---- launches ---------------------------------------------------------------------------
-constexpr int MOST_BLOCKS = 1 << 20, MOST_PARTS = 16;
+constexpr long MOST_BLOCKS = 1 << 22;                    // along x (a launch has at most 2^32 threads there)
+constexpr int MOST_PARTS = 16;
 template <typename F> hipError_t with(bool x, F&& f) { return x ? f(std::true_type()) : f(std::false_type()); }
-int blocks_for(long tasks, int teams) {
+dim3 blocks_for(long tasks, int teams) {
   const long b = (tasks + teams - 1) / teams;
-  return (int)(b < MOST_BLOCKS ? b : MOST_BLOCKS);
+  return b <= MOST_BLOCKS ? dim3((unsigned)b) : dim3((unsigned)MOST_BLOCKS, (unsigned)((b + MOST_BLOCKS - 1) / MOST_BLOCKS));
 }
 // short rows: one wavefront each
 bool short_rows(int cols, bool is_bf16) { return cols <= (is_bf16 ? 2048 : 1024); }
@@ -617,6 +756,7 @@ int parts_of(long rows, int cols, bool is_bf16) {
 }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+static_assert(MOST_PARTS <= WAVE, "a lane per part");
 template <typename T, int W, int MODE> hipError_t values(const LogitsArgs& a, hipStream_t st) {
   return with(a.top_k > 0 && MODE == 0, [&](auto top) -> hipError_t {
     constexpr bool TOP = decltype(top)::value && MODE == 0;
