@@ -262,9 +262,8 @@ __device__ __forceinline__ Sums read_run(const Run<T>& r, int lane, float c, Top
       for (int u = 0; u < STEP; ++u)
         if (v0 + u * team < r.vecs) {
           float x[N];
-          u32x4 again = raw[u];
-          asm("" : "+v"(again));                         // (decoded anew in every pass: a chunk's 32 values are not kept)
-          decode<T>(again, x);
+          asm("" : "+v"(raw[u]));                        // (decoded anew in every pass: a chunk's 32 values are not kept)
+          decode<T>(raw[u], x);
           f(x, u);
         }
     };
@@ -528,11 +527,11 @@ __global__ void __launch_bounds__(THREADS, 6) logits_values_kernel(const LogitsA
     join_waves<T, W, TOP>(in, lane, from, sums, top, waves, lists, c);
     if (wave % W == 0) {
       Points<MODE> pt;
-      if (part == 0 && (a.parts == 1 || a.part_points)) {
+      if (part == 0 && (!a.part_sums || a.part_points)) {
         pt.load(a, row);
         pt.gather(z, 0, a.cols);
       }
-      if (a.parts == 1) {
+      if (!a.part_sums) {
         const RowSums r(sums, a.tau);
         put_values<MODE>(a, row, r, pt);
         if constexpr (TOP) put_alternatives(a, row, r, top.list);
@@ -596,150 +595,397 @@ __global__ void __launch_bounds__(THREADS) logits_join_kernel(const LogitsArgs a
 struct Slope {
   float top, off, inv_tau;                               // log p = (z - top) inv_tau - off
   float A, B, slope;
-  int zero;                                              // nothing but zeros
+  bool zero;                                             // nothing but zeros
+  // mass: of the row's points.  sign: 1 for log probabilities, -1 for losses.  What g holds for a row without points is not looked at.
+  template <bool ENTROPY> __device__ __forceinline__ void set(const LogitsArgs& a, long row, float mass, float sign, float entropy) {
+    inv_tau = 1.0f / a.tau;
+    slope = mass == 0.f ? 0.f : sign * (a.g ? a.g[row] : 1.f) * inv_tau;
+    A = slope * mass;
+    B = 0.f;
+    if constexpr (ENTROPY) {
+      B = a.h[row] * inv_tau;
+      A += B * entropy;
+    }
+    zero = !ENTROPY && mass == 0.f;
+  }
+  __device__ __forceinline__ void from_lse(float lse) {
+    top = 0.f;
+    off = lse;
+    zero |= lse == -__builtin_inff();
+  }
+  __device__ __forceinline__ void from_sums(const RowSums& r) {
+    top = r.top;
+    off = r.bad ? __builtin_nanf("") : r.log_s;
+    zero |= r.none;
+  }
   template <bool ENTROPY> __device__ __forceinline__ float at(float z) const {
-    const float lp = fmaf(z - top, inv_tau, -off), p = __builtin_amdgcn_exp2f(lp * LOG2E);
-    return ENTROPY ? -p * fmaf(B, bounded(lp), A) : -p * A;
+    const float lp = fmaf(z - top, inv_tau, -off), p = exp2_of(lp * LOG2E);
+    const float d = ENTROPY ? -p * fmaf(B, bounded(lp), A) : -p * A;
+    return zero ? 0.f : d;
   }
 };
 
-template <typename T, bool ENTROPY> __device__ __forceinline__ void write_run(const Run<T>& in, T* out, const Slope& s, int lane, int team) {
-  constexpr int N = vec<T>();
-  for (int v0 = 0; v0 < in.vecs; v0 += STEP * team) {
-    u32x4 raw[STEP];
+template <typename T> __device__ __forceinline__ void put_vector(T* p, const float (&x)[vec<T>()]) {
+  typedef __attribute__((address_space(1))) u32x4_u* gptr;
+  const u32x4 w = encode<T>(x);
+  *(gptr)p = u32x4_u{w[0], w[1], w[2], w[3]};
+}
+// the gradient of a vector's elements, in place of them; token: its place among them, if it is there
+template <typename T, bool ENTROPY> __device__ __forceinline__ void slope_vector(float (&x)[vec<T>()], const Slope& s, int token) {
 #pragma unroll
-    for (int u = 0; u < STEP; ++u) {
-      const int v = v0 + u * team + lane;
-      raw[u] = ld_global(reinterpret_cast<const u32x4*>(in.p + in.vec_at(v < in.vecs ? v : in.vecs - 1)));
-    }
+  for (int j = 0; j < vec<T>(); ++j) x[j] = s.template at<ENTROPY>(x[j]);
+  if ((unsigned)token < (unsigned)vec<T>()) {
 #pragma unroll
-    for (int u = 0; u < STEP; ++u) {
-      const int v = v0 + u * team + lane;
-      float x[N];
-      decode<T>(raw[u], x);
-#pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = s.zero ? 0.f : s.template at<ENTROPY>(x[j]);
-      if (v < in.vecs) {
-        typedef __attribute__((address_space(1))) u32x4_u* gptr;
-        const u32x4 w = encode<T>(x);
-        *(gptr)(out + in.vec_at(v)) = u32x4_u{w[0], w[1], w[2], w[3]};
-      }
-    }
+    for (int j = 0; j < vec<T>(); ++j) x[j] += token == j ? s.slope : 0.f;
   }
-  if (lane < in.odd) out[in.odd_at(lane)] = from_f<T>(s.zero ? 0.f : s.template at<ENTROPY>(to_f(in.p[in.odd_at(lane)])));
 }
 
-// The ids among a team's elements get their value again, with what the points add.  An id that comes twice is added up in
-// order, by its first.
-template <typename T, int MODE, bool ENTROPY>
-__device__ __forceinline__ void write_points(const Slope& s, const Points<MODE>& pt, T* row, int from, int n, int kept, int* ids, float* ws) {
+// A teacher's ids (MODE 1).  The vectors (and odd elements) that hold one are left out by the team as it writes a run, and written
+// by the first wavefront, from memory: no other touches them, also where the gradient replaces the logits.
+// left_out: a word per lane, bit u for its vector u of the run and the highest for its odd element.
+constexpr int ODD_BIT = 31;
+template <typename T> struct Place { int lane, bit; };
+template <typename T> __device__ __forceinline__ Place<T> place_of(const Run<T>& r, int at, int team) {
+  const int v = (at - r.head) / vec<T>();
+  if (at < r.head) return {at, ODD_BIT};
+  if (v >= r.vecs) return {at - r.vecs * vec<T>(), ODD_BIT};
+  return {v % team, v / team};
+}
+// Marks the ids among the run's n elements from `from` on.  first: a bit per id of the lane that is the first of its vector;
+// twice: two are the same.
+struct Marked { unsigned first; bool twice; };
+template <typename T> __device__ __forceinline__ Marked leave_out(const Run<T>& r, const Points<1>& pt, int from, int n, int team, unsigned* left_out, int* ids, float* ws) {
   const int lane = threadIdx.x & 63;
-  if constexpr (MODE == 0) {
-    if (lane == 0 && pt.id[0] >= from && pt.id[0] - from < n) row[pt.id[0]] = from_f<T>(s.template at<ENTROPY>(pt.z[0]) + s.slope);
-  } else {
+  unsigned first = 0, later = 0;                         // later: in a vector (or odd element) that another has marked
 #pragma unroll
-    for (int i = 0; i < Points<MODE>::N; ++i) {
-      ids[i * WAVE + lane] = pt.id[i];
-      ws[i * WAVE + lane] = pt.w[i];
+  for (int i = 0; i < Points<1>::N; ++i) {
+    ids[i * WAVE + lane] = pt.id[i];
+    ws[i * WAVE + lane] = pt.w[i];
+    if (pt.id[i] >= from && pt.id[i] - from < n) {
+      const Place<T> at = place_of(r, pt.id[i] - from, team);
+      const bool known = atomicOr(left_out + at.lane, 1u << at.bit) >> at.bit & 1;
+      first |= known || at.bit == ODD_BIT ? 0u : 1u << i;
+      later |= known ? 1u << i : 0u;
     }
-    wave_sync();
+  }
+  wave_sync();
+  bool twice = false;
+  for (int i = 0; i < Points<1>::N; ++i)
+    for (u64 who = __ballot(later >> i & 1); who; who &= who - 1) {     // (of two that are the same, one is here)
+      const int from_lane = __builtin_ctzll(who), id = ids[i * WAVE + from_lane];
 #pragma unroll
-    for (int i = 0; i < Points<MODE>::N; ++i) {
-      bool mine = pt.id[i] >= from && pt.id[i] - from < n;
-      if (!__any(mine)) continue;
-      float sum = 0.f;
+      for (int k = 0; k < Points<1>::N; ++k) twice |= pt.id[k] == id && !(k == i && lane == from_lane);
+    }
+  return Marked{first, __any(twice) != 0};
+}
+template <typename T> __device__ __forceinline__ void write_left_out(const Run<T>& r, T* out, const Slope& s, const Points<1>& pt, int from, int n, int kept, Marked marked, const int* ids, const float* ws) {
+  constexpr int N = vec<T>();
+  const int lane = threadIdx.x & 63;
+  float z[Points<1>::N];
+#pragma unroll
+  for (int i = 0; i < Points<1>::N; ++i)
+    if (pt.id[i] >= from && pt.id[i] - from < n) z[i] = to_f(r.p[pt.id[i] - from]);
+  // the vectors without what the points add, by the first in each ..
+#pragma unroll
+  for (int i = 0; i < Points<1>::N; ++i)
+    if (marked.first >> i & 1) {
+      const int at = r.vec_at((pt.id[i] - from - r.head) / N);
+      float x[N];
+      decode<T>(ld_global(reinterpret_cast<const u32x4*>(r.p + at)), x);
+      slope_vector<T, false>(x, s, -1);
+      put_vector<T>(out + at, x);
+    }
+  // .. then the points themselves (a wavefront's stores to an address keep their order).  An id that comes twice is added up in
+  // order, by its first.
+#pragma unroll
+  for (int i = 0; i < Points<1>::N; ++i) {
+    if (i * WAVE >= kept) break;
+    const int at = pt.id[i] - from;
+    bool mine = pt.id[i] >= from && at < n;
+    float sum = pt.w[i];
+    if (marked.twice) {
+      sum = 0.f;
       for (int j = 0; j < kept; ++j) {
         const bool same = ids[j] == pt.id[i];
         sum += same ? ws[j] : 0.f;
         mine = mine && !(same && j < i * WAVE + lane);
       }
-      if (mine) row[pt.id[i]] = from_f<T>(s.template at<ENTROPY>(pt.z[i]) + s.slope * sum);
     }
-    wave_sync();
+    if (mine) out[at] = from_f<T>(s.zero ? 0.f : s.template at<false>(z[i]) + s.slope * sum);
   }
 }
 
-// FROM: where a row's sums come from.  GIVEN: its log-sum-exp (and entropy) are arguments; PARTS: they lie in the workspace;
-// HERE: a team takes them itself, from the whole row.  But for GIVEN the rows' values are written as well.
-// dz may be z itself: what a team needs of its run besides the run is read before any of it is written, and what it
-// needs of other runs lies in the workspace.
-enum { GIVEN = 0, PARTS = 1, HERE = 2 };
+// FROM: where a row's sums come from.  GIVEN: its log-sum-exp (and entropy) are arguments; PARTS: they lie in the workspace, and the
+// rows' values are written as well.  A block (W = 4) writes a run of a row, a wavefront (W = 1) a whole short one.  dz may be z
+// itself: what is needed of other runs lies in the workspace.
+enum { GIVEN = 0, PARTS = 1 };
 template <typename T, int W, bool ENTROPY, int MODE, int FROM>
 __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsArgs a) {
-  constexpr int TEAMS = WAVES / W;
-  __shared__ f32x4 waves[WAVES];
-  __shared__ Slope slopes[TEAMS];
+  constexpr int TEAMS = WAVES / W, N = vec<T>(), team = W * WAVE;
+  __shared__ float mass[TEAMS];
+  __shared__ unsigned left_out[MODE == 1 ? THREADS : 1];
   __shared__ int ids[MODE == 1 ? TEAMS * KEPT : 1];
   __shared__ float ws[MODE == 1 ? TEAMS * KEPT : 1];
-  const int wave = threadIdx.x / WAVE, team = wave / W, lane = threadIdx.x % (W * WAVE);
+  const int wave = threadIdx.x / WAVE, group = wave / W, lane = threadIdx.x % team;
+  const bool leads = wave % W == 0;
   const float c = LOG2E / a.tau;
-  const long tasks = a.rows * a.runs;
-  const long task = block_index() * TEAMS + team;
-  if (task >= tasks) return;
-  {
-    const long row = task / a.runs;
-    const int run = (int)(task - row * a.runs), from = run * a.run_cols;
-    const int n = a.cols - from < a.run_cols ? a.cols - from : a.run_cols;
-    const T* z = static_cast<const T*>(a.z) + row * a.ld;
-    T* dz = static_cast<T*>(a.dz) + row * a.lddz;
-    const Run<T> in(z, from, n);
-    Points<MODE> pt;
-    Sums sums;
-    if constexpr (FROM == HERE) {
-      Top none;
-      sums = read_run<T, W, MODE == 0, false>(in, lane, c, none);
-      join_waves<T, W, false>(in, lane, 0, sums, none, waves, nullptr, c);
-    }
-    if (wave % W == 0) {
-      pt.load(a, row);
-      if constexpr (FROM == PARTS) {
+  const long task = block_index() * TEAMS + group;
+  if (task >= a.rows * a.runs) return;
+  const long row = task / a.runs;
+  const int run = (int)(task - row * a.runs), from = run * a.run_cols;
+  const int n = a.cols - from < a.run_cols ? a.cols - from : a.run_cols;
+  const T* z = static_cast<const T*>(a.z) + row * a.ld;
+  T* out = static_cast<T*>(a.dz) + row * a.lddz + from;
+  const Run<T> in(z, from, n);
+  auto meet = [&]() {
+    if constexpr (W > 1) __syncthreads();
+    else wave_sync();
+  };
+  u32x4 raw[STEP];
+  auto load = [&](int v0) {
 #pragma unroll
-        for (int i = 0; i < Points<MODE>::N; ++i) pt.z[i] = i * WAVE + lane < a.points ? a.part_points[row * a.points + i * WAVE + lane] : 0.f;
-      } else {
-        pt.gather(z, from, n);
-      }
-      Slope s;
-      float entropy = 0.f;
-      s.inv_tau = 1.0f / a.tau;
-      if constexpr (FROM == GIVEN) {
-        s.top = 0.f;
-        s.off = a.lse_in[row];
-        s.zero = s.off == -__builtin_inff();
-        if (ENTROPY) entropy = a.entropy_in[row];
-      } else {
-        if constexpr (FROM == PARTS) sums = joined(a, row, c);
-        const RowSums r(sums, a.tau);
-        if (run == 0) put_values<MODE>(a, row, r, pt);
-        s.top = r.top;
-        s.off = r.bad ? __builtin_nanf("") : r.log_s;
-        s.zero = r.none;
-        entropy = r.entropy;
-      }
-      s.slope = (MODE == 0 ? 1.f : -1.f) * (a.g ? a.g[row] : 1.f) * s.inv_tau;
-      if (pt.mass == 0.f) s.slope = 0.f;                 // (whatever g holds there)
-      s.A = s.slope * pt.mass;
-      s.B = 0.f;
-      if constexpr (ENTROPY) {
-        s.B = a.h[row] * s.inv_tau;
-        s.A += s.B * entropy;
-      } else {
-        s.zero |= pt.mass == 0.f;
-      }
-      slopes[team] = s;
+    for (int u = 0; u < STEP; ++u) {
+      const int v = v0 + u * team + lane;
+      raw[u] = ld_global(reinterpret_cast<const u32x4*>(in.p + in.vec_at(v < in.vecs ? v : in.vecs - 1)));
     }
-    if constexpr (W > 1) __syncthreads();
-    else wave_sync();
-    const Slope s = slopes[team];
-    write_run<T, ENTROPY>(in, dz + from, s, lane, W * WAVE);
-    if constexpr (W > 1) __syncthreads();
-    else wave_sync();
-    if (wave % W == 0 && !s.zero) write_points<T, MODE, ENTROPY>(s, pt, dz, from, n, a.kept, ids + (MODE == 1 ? team * KEPT : 0), ws + (MODE == 1 ? team * KEPT : 0));
+  };
+  if (in.vecs) load(0);
+  Points<MODE> pt;
+  Marked marked = {0, false};
+  unsigned skip = 0;
+  if constexpr (MODE == 0) {
+    pt.load(a, row);
+  } else {
+    left_out[threadIdx.x] = 0;
+    if (leads) pt.load(a, row);
+    meet();
+    if (leads) {
+      marked = leave_out<T>(in, pt, from, n, team, left_out + group * team, ids + group * KEPT, ws + group * KEPT);
+      if (lane == 0) mass[group] = pt.mass;
+    }
+    meet();
+    pt.mass = mass[group];
+    skip = left_out[threadIdx.x];
+  }
+  Slope s;
+  if constexpr (FROM == GIVEN) {
+    s.template set<ENTROPY>(a, row, pt.mass, MODE == 0 ? 1.f : -1.f, ENTROPY ? a.entropy_in[row] : 0.f);
+    s.from_lse(a.lse_in[row]);
+  } else {
+    const RowSums r(joined(a, row, c), a.tau);
+    s.template set<ENTROPY>(a, row, pt.mass, MODE == 0 ? 1.f : -1.f, r.entropy);
+    s.from_sums(r);
+    if (run == 0 && leads) {
+#pragma unroll
+      for (int i = 0; i < Points<MODE>::N; ++i) pt.z[i] = i * WAVE + lane < a.points ? a.part_points[row * a.points + i * WAVE + lane] : 0.f;
+      put_values<MODE>(a, row, r, pt);
+    }
+  }
+  const int token = MODE == 0 && pt.id[0] >= 0 && !s.zero ? pt.id[0] - from : -1;
+  for (int v0 = 0, chunk = 0; v0 < in.vecs; ++chunk) {
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      const int v = v0 + u * team + lane;
+      if (v < in.vecs) {
+        float x[N];
+        decode<T>(raw[u], x);
+        slope_vector<T, ENTROPY>(x, s, MODE == 0 && token >= 0 ? token - in.vec_at(v) : -1);
+        if (MODE == 0 || !(skip >> (chunk * STEP + u) & 1)) put_vector<T>(out + in.vec_at(v), x);
+      }
+    }
+    v0 += STEP * team;
+    if (v0 < in.vecs) load(v0);
+  }
+  if (lane < in.odd && !(skip >> ODD_BIT)) {
+    const int at = in.odd_at(lane);
+    out[at] = from_f<T>(s.template at<ENTROPY>(to_f(in.p[at])) + (MODE == 0 && at == token ? s.slope : 0.f));
+  }
+  if constexpr (MODE == 1)
+    if (leads) write_left_out<T>(in, out, s, pt, from, n, a.kept, marked, ids + group * KEPT, ws + group * KEPT);
+}
+
+// ---- values and gradients of rows that fit the registers of NW wavefronts -------------------------
+// RV vectors per lane.  A row is read once; the next row's loads are issued as its registers are written.
+template <typename T, int NW, int RV, bool ENTROPY, int MODE, int OCC>
+__global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_step_kernel(const LogitsArgs a) {
+  constexpr int N = vec<T>(), team = NW * WAVE, TEAMS = NW == 1 ? WAVES : 1;
+  __shared__ float tops[TEAMS * NW];
+  __shared__ f32x4 waves[TEAMS * NW];
+  __shared__ unsigned left_out[MODE == 1 ? TEAMS * team : 1];
+  __shared__ int ids[MODE == 1 ? TEAMS * KEPT : 1];
+  __shared__ float ws[MODE == 1 ? TEAMS * KEPT : 1];
+  __shared__ float mass[TEAMS];
+  const int group = NW == 1 ? threadIdx.x / WAVE : 0, lane = threadIdx.x % team, wave = lane / WAVE, l = threadIdx.x & 63;
+  const float c = LOG2E / a.tau, none = -__builtin_inff();
+  const T* z = static_cast<const T*>(a.z);
+  const long stride = (long)gridDim.x * TEAMS;
+  auto meet = [&]() {                                    // (of a row's wavefronts; it waits for LDS alone: loads and stores stay in flight)
+    if constexpr (NW == 1) {
+      wave_sync();
+    } else {
+      wait_lgkm();
+      bare_barrier();
+    }
+  };
+  u32x4 raw[RV];
+  float odd;
+  auto load = [&](const Run<T>& r, int u) {
+    const int v = u * team + lane;
+    if (u * team < r.vecs) raw[u] = ld_stream(reinterpret_cast<const u32x4*>(r.p + r.vec_at(v < r.vecs ? v : r.vecs - 1)));
+  };
+  auto load_odd = [&](const Run<T>& r) { odd = lane < r.odd ? to_f(r.p[r.odd_at(lane)]) : none; };
+  if constexpr (MODE == 1) left_out[group * team + lane] = 0;
+  long row = (long)blockIdx.x * TEAMS + group;
+  if (row < a.rows) {
+    const Run<T> r(z, row * a.ld, a.cols);
+#pragma unroll
+    for (int u = 0; u < RV; ++u) load(r, u);
+    load_odd(r);
+  }
+  for (; row < a.rows; row += stride) {
+    const Run<T> r(z, row * a.ld, a.cols);
+    T* out = static_cast<T*>(a.dz) + row * a.lddz;
+    auto each = [&](auto f) {
+#pragma unroll
+      for (int u = 0; u < RV; ++u)
+        if (u * team + wave * WAVE < r.vecs) {           // (the same for a whole wavefront)
+          float x[N];
+          asm("" : "+v"(raw[u]));                        // (decoded anew in every pass: 8 values take more registers than a vector)
+          decode<T>(raw[u], x);
+          f(x, u);
+        }
+    };
+    Points<MODE> pt;
+    Marked marked = {0, false};
+    if (MODE == 0 || wave == 0) pt.load(a, row);
+#pragma unroll
+    for (int u = 0; u < RV; ++u)
+      if (u * team < r.vecs && u * team + lane >= r.vecs) raw[u] = u32x4{NOTHING<T>, NOTHING<T>, NOTHING<T>, NOTHING<T>};
+    float top = odd;
+    each([&](const float (&x)[N], int) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
+    });
+    top = wave_max(top);
+    if (wave == 0) pt.gather(z + row * a.ld, 0, a.cols);
+    if constexpr (NW > 1) {
+      if (l == 0) tops[wave] = top;
+      meet();
+      top = wave_max(tops[l % NW]);
+    }
+    top = fmaxf(top, LOWEST);
+    // Exponents are x c - P as in Reader; `rest` is the part of each that P leaves out.  Where |P| is too large for that the
+    // row's values become their differences to the maximum, which then is 0: those that matter are exact.
+    float base = top, P = top * c;
+    if (!(fabsf(P) < 0x1p20f)) {
+#pragma unroll
+      for (int u = 0; u < RV; ++u)
+        if (u * team + wave * WAVE < r.vecs) {
+          float x[N];
+          decode<T>(raw[u], x);
+#pragma unroll
+          for (int j = 0; j < N; ++j) x[j] -= top;
+          raw[u] = encode<T>(x);
+        }
+      odd -= top;
+      base = P = 0.f;
+    }
+    const float rest = fmaf(base, c, -P);
+    float s = 0.f, t = 0.f;
+    auto add = [&](float x) {
+      const float d = fmaf(x, c, -P), e = exp2_of(d);
+      s += e;
+      if constexpr (MODE == 0) t = fmaf(bounded(d), e, t);
+    };
+    add(odd);
+    each([&](const float (&x)[N], int) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) add(x[j]);
+    });
+    shift(s, t, -rest);
+    s = wave_sum(s);
+    if constexpr (MODE == 0) t = wave_sum(t);
+    if constexpr (MODE == 1) {
+      if (wave == 0) {
+        marked = leave_out<T>(r, pt, 0, a.cols, team, left_out + group * team, ids + group * KEPT, ws + group * KEPT);
+        if (l == 0) mass[group] = pt.mass;
+      }
+    }
+    // (the token's logit on this side of the meeting: behind it others may write in its place)
+    if (NW > 1 && l == 0) waves[wave] = f32x4{s, t, MODE == 0 && wave == 0 ? pt.z[0] : 0.f, 0.f};
+    meet();
+    if constexpr (NW > 1) {
+      const f32x4 w = waves[l % NW];
+      s = wave_sum(l < NW ? w[0] : 0.f);
+      if constexpr (MODE == 0) {
+        t = wave_sum(l < NW ? w[1] : 0.f);
+        pt.z[0] = waves[0][2];
+      }
+    }
+    const RowSums sums(Sums{top, s, t}, a.tau);
+    unsigned skip = 0;
+    float weight = pt.mass;
+    if constexpr (MODE == 1) {
+      weight = mass[group];
+      skip = left_out[group * team + lane];
+      left_out[group * team + lane] = 0;                 // (marked again only behind the next row's first meeting)
+    }
+    Slope slope;
+    slope.template set<ENTROPY>(a, row, weight, MODE == 0 ? 1.f : -1.f, sums.entropy);
+    slope.from_sums(sums);
+    if (wave == 0) put_values<MODE>(a, row, sums, pt);
+    const int token = MODE == 0 && pt.id[0] >= 0 && !slope.zero ? pt.id[0] : -1;
+    const bool more = row + stride < a.rows;
+    const Run<T> next(z, (more ? row + stride : row) * a.ld, a.cols);
+    // log2 p = x c - Q - left: Q is P + rest + log2 s rounded
+    const float tail = rest + slope.off * LOG2E;
+    float Q = P + tail;
+    const float left = (P - Q) + tail, whole = exp2_of(-left);
+    float A = -slope.A * whole, B = -slope.B * 0.69314718055994530942f * whole;
+    if (slope.zero) {
+#pragma unroll
+      for (int u = 0; u < RV; ++u) raw[u] = u32x4{0, 0, 0, 0};
+      odd = Q = A = B = 0.f;
+    }
+    auto gradient = [&](float x) {
+      const float lp = fmaf(x, c, -Q), p = exp2_of(lp);
+      return ENTROPY ? p * fmaf(B, bounded(lp - left), A) : p * A;
+    };
+    if (lane < r.odd && !(skip >> ODD_BIT)) {
+      const int at = r.odd_at(lane);
+      out[at] = from_f<T>(gradient(odd) + (MODE == 0 && at == token ? slope.slope : 0.f));
+    }
+#pragma unroll
+    for (int u = 0; u < RV; ++u) {
+      const int v = u * team + lane;
+      if (v < r.vecs) {
+        float x[N];
+        decode<T>(raw[u], x);
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = gradient(x[j]);
+        if constexpr (MODE == 0) {
+          const unsigned at = token - r.vec_at(v);
+          if (at < (unsigned)N && token >= 0) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[j] += (int)at == j ? slope.slope : 0.f;
+          }
+        }
+        if (MODE == 0 || !(skip >> u & 1)) put_vector<T>(out + r.vec_at(v), x);
+      }
+      if (more) load(next, u);
+    }
+    if (more) load_odd(next);
+    if constexpr (MODE == 1) {
+      if (wave == 0) write_left_out<T>(r, out, slope, pt, 0, a.cols, a.kept, marked, ids + group * KEPT, ws + group * KEPT);
+      if constexpr (NW == 1) wave_sync();
+    }
   }
 }
 
 // ---- launches ---------------------------------------------------------------------------
 constexpr long MOST_BLOCKS = 1 << 22;                    // along x (a launch has at most 2^32 threads there)
 constexpr int MOST_PARTS = 16;
+static_assert(MOST_PARTS <= WAVE, "a lane per part");
 template <typename F> hipError_t with(bool x, F&& f) { return x ? f(std::true_type()) : f(std::false_type()); }
 dim3 blocks_for(long tasks, int teams) {
   const long b = (tasks + teams - 1) / teams;
@@ -754,15 +1000,19 @@ int parts_of(long rows, int cols, bool is_bf16) {
   const long parts = wanted < most ? wanted : most;
   return (int)(parts < 1 ? 1 : parts > MOST_PARTS ? MOST_PARTS : parts);
 }
+// rows that a step keeps in registers
+bool fits(int cols, bool is_bf16) { return cols <= (is_bf16 ? 131072 : 65536); }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+size_t parts_bytes(long rows, int parts, int top_k, int points) {
+  return up256(rows * parts * sizeof(f32x4)) + up256(rows * parts * top_k * sizeof(u64)) + up256((size_t)rows * points * sizeof(float));
+}
 
-static_assert(MOST_PARTS <= WAVE, "a lane per part");
 template <typename T, int W, int MODE> hipError_t values(const LogitsArgs& a, hipStream_t st) {
   return with(a.top_k > 0 && MODE == 0, [&](auto top) -> hipError_t {
     constexpr bool TOP = decltype(top)::value && MODE == 0;
     logits_values_kernel<T, W, TOP, MODE><<<blocks_for(a.rows * a.parts, WAVES / W), THREADS, 0, st>>>(a);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.parts == 1 || a.dz) return e;
+    if (e != hipSuccess || !a.part_sums || a.dz) return e;
     logits_join_kernel<T, TOP, MODE><<<blocks_for(a.rows, WAVES), THREADS, 0, st>>>(a);
     return hipGetLastError();
   });
@@ -773,43 +1023,63 @@ template <typename T, int W, int MODE, int FROM> hipError_t gradient(const Logit
     return hipGetLastError();
   });
 }
+template <typename T, int MODE, int NW, int RV, int OCC> hipError_t step_of(const LogitsArgs& a, hipStream_t st) {
+  constexpr int threads = NW == 1 ? THREADS : NW * WAVE, teams = NW == 1 ? WAVES : 1;
+  // as many blocks as run at once: each walks over its rows
+  const long most = (long)compute_units() * (4 * OCC * WAVE / threads), blocks = (a.rows + teams - 1) / teams;
+  const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+  return with(MODE == 0 && a.h, [&](auto entropy) -> hipError_t {
+    logits_step_kernel<T, NW, RV, decltype(entropy)::value && MODE == 0, MODE, OCC><<<grid, threads, 0, st>>>(a);
+    return hipGetLastError();
+  });
+}
+#ifndef STEP_NW
+#define STEP_NW 16
+#define STEP_RV 8
+#define STEP_OCC 4
+#endif
+template <typename T, int MODE> hipError_t step(const LogitsArgs& a, hipStream_t st) {
+  const int vecs = a.cols / vec<T>();                    // (an odd element less may make one vector less)
+  if (vecs <= 4 * WAVE) return step_of<T, MODE, 1, 4, 4>(a, st);
+  if (vecs <= 4 * 4 * WAVE) return step_of<T, MODE, 4, 4, 4>(a, st);
+  if (vecs <= 4 * 8 * WAVE) return step_of<T, MODE, 4, 8, 4>(a, st);
+  if (vecs <= 8 * 8 * WAVE) return step_of<T, MODE, 8, 8, 4>(a, st);
+  if (vecs <= STEP_NW * STEP_RV * WAVE) return step_of<T, MODE, STEP_NW, STEP_RV, STEP_OCC>(a, st);
+  return step_of<T, MODE, 16, 16, 4>(a, st);
+}
 
-template <typename T, int W, int MODE> hipError_t launch(LogitsArgs a, hipStream_t st) {
-  constexpr bool is_bf16 = sizeof(T) == 2;
+template <typename T, int W, int MODE> hipError_t launch(LogitsArgs a, bool resident, hipStream_t st) {
   constexpr int TILE = THREADS * STEP * vec<T>();
   if (!a.dz) return values<T, W, MODE>(a, st);
+  if (resident) return step<T, MODE>(a, st);
   a.runs = 1;
   a.run_cols = a.cols;
-  if (a.lse_in || a.parts > 1) {
-    if (W > 1) {
-      a.run_cols = TILE;
-      a.runs = (a.cols + TILE - 1) / TILE;
-    }
-    if (a.lse_in) return gradient<T, W, MODE, GIVEN>(a, st);
-    const hipError_t e = values<T, W, MODE>(a, st);
-    return e != hipSuccess ? e : gradient<T, W, MODE, PARTS>(a, st);
+  if (W > 1) {
+    a.run_cols = TILE;
+    a.runs = (a.cols + TILE - 1) / TILE;
   }
-  (void)is_bf16;
-  return gradient<T, W, MODE, HERE>(a, st);
+  if (a.lse_in) return gradient<T, W, MODE, GIVEN>(a, st);
+  const hipError_t e = values<T, W, MODE>(a, st);
+  return e != hipSuccess ? e : gradient<T, W, MODE, PARTS>(a, st);
 }
 
 }  // namespace
 
 size_t logits_workspace_bytes(long rows, int cols, bool is_bf16, int top_k, int points) {
   const int parts = parts_of(rows, cols, is_bf16);
-  if (parts == 1) return 0;
-  return up256(rows * parts * sizeof(f32x4)) + up256(rows * parts * top_k * sizeof(u64)) + up256((size_t)rows * points * sizeof(float));
+  return parts > 1 || !fits(cols, is_bf16) ? parts_bytes(rows, parts, top_k, points) : 0;
 }
 
 hipError_t launch_logits(LogitsArgs a, int mode, bool is_bf16, void* workspace, hipStream_t st) {
   if (a.rows == 0) return hipSuccess;
   const double elems = (double)a.rows * a.cols, size = is_bf16 ? 2 : 4;
   ProfScope ps(a.lse_in ? PC_LOGITS_GRAD : a.dz ? PC_LOGITS_STEP : PC_LOGITS, elems * (a.dz && !a.lse_in ? 10 : 6), elems * size * (a.dz ? 2 : 1), st);
-  a.parts = a.lse_in ? 1 : parts_of(a.rows, a.cols, is_bf16);
+  const bool stepping = a.dz && !a.lse_in, resident = stepping && fits(a.cols, is_bf16);
+  a.parts = a.lse_in || resident ? 1 : parts_of(a.rows, a.cols, is_bf16);
   a.part_cols = a.cols;
   a.points = mode == 0 ? 1 : a.kept;
-  if (a.parts > 1) {
-    // whole 128-byte lines apart, but for the rows' own alignment
+  if (a.parts > 1 || (stepping && !resident)) {
+    // (whole 128-byte lines apart, but for the rows' own alignment)
     a.part_cols = ((a.cols + a.parts - 1) / a.parts + 63) / 64 * 64;
     a.parts = (a.cols + a.part_cols - 1) / a.part_cols;
     char* at = static_cast<char*>(workspace);
@@ -817,13 +1087,13 @@ hipError_t launch_logits(LogitsArgs a, int mode, bool is_bf16, void* workspace, 
     at += up256(a.rows * a.parts * sizeof(f32x4));
     a.part_lists = reinterpret_cast<unsigned long long*>(at);
     at += up256(a.rows * a.parts * a.top_k * sizeof(u64));
-    a.part_points = a.dz ? reinterpret_cast<float*>(at) : nullptr;
+    a.part_points = stepping ? reinterpret_cast<float*>(at) : nullptr;
   }
   return with(is_bf16, [&](auto b) {
     typedef typename std::conditional<decltype(b)::value, bf16, float>::type T;
     return with(short_rows(a.cols, is_bf16), [&](auto s) {
       constexpr int W = decltype(s)::value ? 1 : WAVES;
-      return with(mode == 0, [&](auto m) { return launch<T, W, decltype(m)::value ? 0 : 1>(a, st); });
+      return with(mode == 0, [&](auto m) { return launch<T, W, decltype(m)::value ? 0 : 1>(a, resident, st); });
     });
   });
 }
