@@ -22,6 +22,7 @@ constexpr int LIST = 256;                                // candidates of a wave
 constexpr int ROOM = LIST + 4 + 64;
 constexpr int GROUPS = 8;                                // groups of a lane's elements whose maxima are kept
 typedef unsigned long long u64;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 template <typename T> constexpr int vec() { return 16 / (int)sizeof(T); }
 
@@ -73,6 +74,25 @@ __device__ __forceinline__ long id_of(const void* ids, long i, bool wide) {
   return wide ? static_cast<const int64_t*>(ids)[i] : (long)static_cast<const int32_t*>(ids)[i];
 }
 
+// ---- over the lanes of a wavefront: the first LANES of them, or groups of so many; the result in all ---------------
+template <int LANES, typename F> __device__ __forceinline__ float over_lanes(float v, F f) {
+  static_assert(LANES == 1 || LANES == 4 || LANES == 8 || LANES == 16 || LANES == 64, "in steps of rows of 16");
+  auto step = [&](unsigned other) { v = f(v, bits_f(other)); };
+  if constexpr (LANES >= 4) { step(lane_move<LANE_XOR1>(f_bits(v))); step(lane_move<LANE_XOR2>(f_bits(v))); }
+  if constexpr (LANES >= 8) step(lane_move<LANE_MIRROR8>(f_bits(v)));
+  if constexpr (LANES >= 16) step(lane_move<LANE_MIRROR16>(f_bits(v)));
+  if constexpr (LANES == 64) {
+    // (rows 1 and 3 against 0 and 2, then the upper 32 lanes against the lower: each of a swap's two results has one side in both places)
+    const auto rows = __builtin_amdgcn_permlane16_swap(f_bits(v), f_bits(v), false, false);
+    v = f(bits_f(rows[0]), bits_f(rows[1]));
+    const auto halves = __builtin_amdgcn_permlane32_swap(f_bits(v), f_bits(v), false, false);
+    v = f(bits_f(halves[0]), bits_f(halves[1]));
+  }
+  return v;
+}
+template <int LANES = 64> __device__ __forceinline__ float all_max(float v) { return over_lanes<LANES>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int LANES = 64> __device__ __forceinline__ float all_sum(float v) { return over_lanes<LANES>(v, [](float a, float b) { return a + b; }); }
+
 // ---- sums of exponentials ----------------------------------------------------------
 // s = sum 2^((x - m) c), t = sum (x - m) c 2^((x - m) c) over the values seen, m one of them, c = log2(e) / tau.  A NaN or
 // +infinity makes s NaN.  Exponents of -160 and less, -infinity among them, have 2^a = 0, and 0 in t.
@@ -97,8 +117,8 @@ __device__ __forceinline__ void merge(Sums& a, Sums b, float c) {
   a.t += b.t;
 }
 __device__ __forceinline__ Sums wave_merge(Sums a, float c) {
-  raise(a, wave_max(a.m), c);
-  return Sums{a.m, wave_sum(a.s), wave_sum(a.t)};
+  raise(a, all_max(a.m), c);
+  return Sums{a.m, all_sum(a.s), all_sum(a.t)};
 }
 
 // A wavefront's sums while it reads.  All lanes refer to one m, which lags behind the maximum: it is raised where a value has an
@@ -111,7 +131,7 @@ template <bool T_SUM> struct Reader {
   __device__ __forceinline__ void start(float scale) { c = scale; m = LOWEST; P = rest = s = t = 0.f; far = true; }
   __device__ __forceinline__ bool low(float most) const { return __any((most - m) * c > 8.f); }
   __device__ __forceinline__ void lift(float most) {
-    const float top = fmaxf(wave_max(most), m), product = top * c;
+    const float top = fmaxf(all_max(most), m), product = top * c;
     const bool beyond = !(fabsf(product) < 0x1p20f);
     const float left = beyond ? 0.f : fmaf(top, c, -product);
     shift(s, t, bounded((m - top) * c - rest + left));
@@ -127,7 +147,7 @@ template <bool T_SUM> struct Reader {
   }
   __device__ __forceinline__ Sums finish() {             // the wavefront's, in all lanes
     shift(s, t, -rest);
-    return Sums{m, wave_sum(s), T_SUM ? wave_sum(t) : 0.f};
+    return Sums{m, all_sum(s), T_SUM ? all_sum(t) : 0.f};
   }
 };
 
@@ -409,12 +429,12 @@ __device__ __forceinline__ void join_waves(const Run<T>& r, int lane, int index,
 // teacher's logit is no number).  Held by one wavefront.
 constexpr int KEPT = 256;
 template <int MODE> struct Points {
-  static constexpr int N = MODE == 0 ? 1 : KEPT / WAVE;
+  static constexpr int N = MODE == 0 ? 1 : KEPT / WAVE, OUTSIDE = -2;
   int id[N];                                             // -1: none
   float w[N], z[N];                                      // z: the student's logits
   float mass;
-  __device__ __forceinline__ void load(const LogitsArgs& a, long row) {
-    const int lane = threadIdx.x & 63;
+  // fetch starts the loads, settle makes the weights of them
+  __device__ __forceinline__ void fetch(const LogitsArgs& a, long row) {
     if constexpr (MODE == 0) {
       const long token = a.tokens ? id_of(a.tokens, row, a.wide_ids) : -1;
       const bool valid = token >= 0 && token < a.cols;
@@ -422,46 +442,56 @@ template <int MODE> struct Points {
       w[0] = 1.f;
       mass = valid ? 1.f : token < 0 ? 0.f : __builtin_nanf("");
     } else {
-      const float none = -__builtin_inff();
-      float y[N], top = none;
+      const int lane = threadIdx.x & 63;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        id[i] = -1;
+        w[i] = 0.f;
+        if (i * WAVE < a.kept && i * WAVE + lane < a.kept) {
+          const long at = row * a.kept + i * WAVE + lane, v = id_of(a.teacher_ids, at, a.wide_ids);
+          id[i] = v < 0 ? -1 : v < a.cols ? (int)v : OUTSIDE;
+          w[i] = a.teacher_bf16 ? to_f(static_cast<const bf16*>(a.teacher)[at]) : static_cast<const float*>(a.teacher)[at];
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void settle(const LogitsArgs& a, long row) {
+    if constexpr (MODE == 1) {
+      float top = -__builtin_inff();
       bool out = false;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int j = lane + i * WAVE;
-        id[i] = -1;
-        y[i] = none;
-        if (j < a.kept) {
-          const long at = row * a.kept + j, v = id_of(a.teacher_ids, at, a.wide_ids);
-          out |= v >= a.cols;
-          if (v >= 0 && v < a.cols) {
-            id[i] = (int)v;
-            y[i] = a.teacher_bf16 ? to_f(static_cast<const bf16*>(a.teacher)[at]) : static_cast<const float*>(a.teacher)[at];
-          }
-        }
-        top = fmaxf(top, y[i]);
+        out |= id[i] == OUTSIDE;
+        if (id[i] == OUTSIDE) id[i] = -1;
+        if (id[i] >= 0) top = fmaxf(top, w[i]);
       }
-      if (a.teacher_lse) {
-        const float l = a.teacher_lse[row];
+      const float l = a.teacher_lse ? a.teacher_lse[row] : 0.f;
+      top = fmaxf(all_max(top), LOWEST);
+      float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = id[i] < 0 ? 0.f : expf(y[i] / a.tau - l);
-      } else {
-        top = fmaxf(wave_max(top), LOWEST);
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          w[i] = id[i] < 0 ? 0.f : expf((y[i] - top) / a.tau);
+      for (int i = 0; i < N; ++i)
+        if (i * WAVE < a.kept) {
+          w[i] = id[i] < 0 ? 0.f : expf(a.teacher_lse ? w[i] / a.tau - l : (w[i] - top) / a.tau);
           s += w[i];
         }
-        s = wave_sum(s);
+      s = all_sum(s);
+      mass = s;
+      if (!a.teacher_lse) {
+        const float one = 1.f / s;
+        float m = 0.f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = s != 0.f ? w[i] / s : 0.f;       // (NaN stays)
+        for (int i = 0; i < N; ++i) {
+          w[i] = s != 0.f ? w[i] * one : 0.f;            // (NaN stays)
+          m += w[i];
+        }
+        mass = all_sum(m);
       }
-      mass = 0.f;
-#pragma unroll
-      for (int i = 0; i < N; ++i) mass += w[i];
-      mass = wave_sum(mass);
       if (__any(out)) mass = __builtin_nanf("");
     }
+  }
+  __device__ __forceinline__ void load(const LogitsArgs& a, long row) {
+    fetch(a, row);
+    settle(a, row);
   }
   // the logits of the ids among the n from `from` on
   template <typename T> __device__ __forceinline__ void gather(const T* row, int from, int n) {
@@ -487,7 +517,7 @@ template <int MODE> __device__ __forceinline__ void put_values(const LogitsArgs&
 #pragma unroll
     for (int i = 0; i < Points<MODE>::N; ++i)
       if (pt.id[i] >= 0 && pt.w[i] != 0.f) l += pt.w[i] * (logf(pt.w[i]) - r.logprob(pt.z[i], a.tau));
-    l = wave_sum(l);
+    l = all_sum(l);
     if (lane == 0 && a.loss) a.loss[row] = pt.mass == 0.f || pt.mass != pt.mass ? pt.mass : l;
   }
 }
@@ -810,7 +840,7 @@ template <typename T, int NW, int RV, bool ENTROPY, int MODE, int OCC>
 __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_step_kernel(const LogitsArgs a) {
   constexpr int N = vec<T>(), team = NW * WAVE, TEAMS = NW == 1 ? WAVES : 1;
   __shared__ float tops[TEAMS * NW];
-  __shared__ f32x4 waves[TEAMS * NW];
+  __shared__ f32x2 waves[TEAMS * NW];
   __shared__ unsigned left_out[MODE == 1 ? TEAMS * team : 1];
   __shared__ int ids[MODE == 1 ? TEAMS * KEPT : 1];
   __shared__ float ws[MODE == 1 ? TEAMS * KEPT : 1];
@@ -829,6 +859,7 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
   };
   u32x4 raw[RV];
   float odd;
+  Points<MODE> pt;
   auto load = [&](const Run<T>& r, int u) {
     const int v = u * team + lane;
     if (u * team < r.vecs) raw[u] = ld_stream(reinterpret_cast<const u32x4*>(r.p + r.vec_at(v < r.vecs ? v : r.vecs - 1)));
@@ -841,6 +872,7 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
 #pragma unroll
     for (int u = 0; u < RV; ++u) load(r, u);
     load_odd(r);
+    if (MODE == 1 && wave == 0) pt.fetch(a, row);
   }
   for (; row < a.rows; row += stride) {
     const Run<T> r(z, row * a.ld, a.cols);
@@ -855,9 +887,12 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
           f(x, u);
         }
     };
-    Points<MODE> pt;
     Marked marked = {0, false};
-    if (MODE == 0 || wave == 0) pt.load(a, row);
+    if (MODE == 0) pt.fetch(a, row);
+    if (MODE == 1 && wave == 0) {
+      pt.settle(a, row);
+      pt.gather(z + row * a.ld, 0, a.cols);
+    }
 #pragma unroll
     for (int u = 0; u < RV; ++u)
       if (u * team < r.vecs && u * team + lane >= r.vecs) raw[u] = u32x4{NOTHING<T>, NOTHING<T>, NOTHING<T>, NOTHING<T>};
@@ -866,12 +901,11 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
 #pragma unroll
       for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
     });
-    top = wave_max(top);
-    if (wave == 0) pt.gather(z + row * a.ld, 0, a.cols);
+    top = all_max(top);
     if constexpr (NW > 1) {
       if (l == 0) tops[wave] = top;
       meet();
-      top = wave_max(tops[l % NW]);
+      top = all_max<NW>(tops[l % NW]);
     }
     top = fmaxf(top, LOWEST);
     // Exponents are x c - P as in Reader; `rest` is the part of each that P leaves out.  Where |P| is too large for that the
@@ -903,24 +937,20 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
       for (int j = 0; j < N; ++j) add(x[j]);
     });
     shift(s, t, -rest);
-    s = wave_sum(s);
-    if constexpr (MODE == 0) t = wave_sum(t);
+    s = all_sum(s);
+    if constexpr (MODE == 0) t = all_sum(t);
     if constexpr (MODE == 1) {
       if (wave == 0) {
         marked = leave_out<T>(r, pt, 0, a.cols, team, left_out + group * team, ids + group * KEPT, ws + group * KEPT);
         if (l == 0) mass[group] = pt.mass;
       }
     }
-    // (the token's logit on this side of the meeting: behind it others may write in its place)
-    if (NW > 1 && l == 0) waves[wave] = f32x4{s, t, MODE == 0 && wave == 0 ? pt.z[0] : 0.f, 0.f};
+    if (NW > 1 && l == 0) waves[wave] = f32x2{s, t};
     meet();
     if constexpr (NW > 1) {
-      const f32x4 w = waves[l % NW];
-      s = wave_sum(l < NW ? w[0] : 0.f);
-      if constexpr (MODE == 0) {
-        t = wave_sum(l < NW ? w[1] : 0.f);
-        pt.z[0] = waves[0][2];
-      }
+      const f32x2 w = waves[l % NW];
+      s = all_sum<NW>(w[0]);
+      if constexpr (MODE == 0) t = all_sum<NW>(w[1]);
     }
     const RowSums sums(Sums{top, s, t}, a.tau);
     unsigned skip = 0;
@@ -933,8 +963,18 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
     Slope slope;
     slope.template set<ENTROPY>(a, row, weight, MODE == 0 ? 1.f : -1.f, sums.entropy);
     slope.from_sums(sums);
-    if (wave == 0) put_values<MODE>(a, row, sums, pt);
     const int token = MODE == 0 && pt.id[0] >= 0 && !slope.zero ? pt.id[0] : -1;
+    if (wave == 0) {
+      // (a loss comes last; a token's log probability from the lane that holds its logit)
+      if (l == 0) {
+        if (a.lse) a.lse[row] = sums.lse;
+        if (MODE == 0 && a.entropy) a.entropy[row] = sums.entropy;
+        if (MODE == 0 && a.logprob && token < 0) a.logprob[row] = pt.mass == 1.f ? (sums.none ? -__builtin_inff() : __builtin_nanf("")) : pt.mass;
+      }
+    }
+    auto at_token = [&](float x) {
+      if (a.logprob) a.logprob[row] = sums.bad ? __builtin_nanf("") : (x - base) / a.tau - sums.log_s;
+    };
     const bool more = row + stride < a.rows;
     const Run<T> next(z, (more ? row + stride : row) * a.ld, a.cols);
     // log2 p = x c - Q - left: Q is P + rest + log2 s rounded
@@ -954,6 +994,7 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
     if (lane < r.odd && !(skip >> ODD_BIT)) {
       const int at = r.odd_at(lane);
       out[at] = from_f<T>(gradient(odd) + (MODE == 0 && at == token ? slope.slope : 0.f));
+      if (MODE == 0 && at == token) at_token(odd);
     }
 #pragma unroll
     for (int u = 0; u < RV; ++u) {
@@ -961,14 +1002,18 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
       if (v < r.vecs) {
         float x[N];
         decode<T>(raw[u], x);
+        const unsigned at = MODE == 0 && token >= 0 ? token - r.vec_at(v) : N;
+        if (at < (unsigned)N) {
+          float own = x[0];
+#pragma unroll
+          for (int j = 1; j < N; ++j) own = (int)at == j ? x[j] : own;
+          at_token(own);
+        }
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] = gradient(x[j]);
-        if constexpr (MODE == 0) {
-          const unsigned at = token - r.vec_at(v);
-          if (at < (unsigned)N && token >= 0) {
+        if (at < (unsigned)N) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) x[j] += (int)at == j ? slope.slope : 0.f;
-          }
+          for (int j = 0; j < N; ++j) x[j] += (int)at == j ? slope.slope : 0.f;
         }
         if (MODE == 0 || !(skip >> u & 1)) put_vector<T>(out + r.vec_at(v), x);
       }
@@ -976,7 +1021,11 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
     }
     if (more) load_odd(next);
     if constexpr (MODE == 1) {
-      if (wave == 0) write_left_out<T>(r, out, slope, pt, 0, a.cols, a.kept, marked, ids + group * KEPT, ws + group * KEPT);
+      if (wave == 0) {
+        put_values<MODE>(a, row, sums, pt);
+        write_left_out<T>(r, out, slope, pt, 0, a.cols, a.kept, marked, ids + group * KEPT, ws + group * KEPT);
+        if (more) pt.fetch(a, row + stride);
+      }
       if constexpr (NW == 1) wave_sync();
     }
   }
@@ -1033,18 +1082,15 @@ template <typename T, int MODE, int NW, int RV, int OCC> hipError_t step_of(cons
     return hipGetLastError();
   });
 }
-#ifndef STEP_NW
-#define STEP_NW 16
-#define STEP_RV 8
-#define STEP_OCC 4
-#endif
 template <typename T, int MODE> hipError_t step(const LogitsArgs& a, hipStream_t st) {
   const int vecs = a.cols / vec<T>();                    // (an odd element less may make one vector less)
   if (vecs <= 4 * WAVE) return step_of<T, MODE, 1, 4, 4>(a, st);
-  if (vecs <= 4 * 4 * WAVE) return step_of<T, MODE, 4, 4, 4>(a, st);
+  if (vecs <= 4 * 4 * WAVE) return step_of<T, MODE, 4, 4, 5>(a, st);
   if (vecs <= 4 * 8 * WAVE) return step_of<T, MODE, 4, 8, 4>(a, st);
-  if (vecs <= 8 * 8 * WAVE) return step_of<T, MODE, 8, 8, 4>(a, st);
-  if (vecs <= STEP_NW * STEP_RV * WAVE) return step_of<T, MODE, STEP_NW, STEP_RV, STEP_OCC>(a, st);
+  if (vecs <= 4 * 16 * WAVE) return step_of<T, MODE, 4, 16, 4>(a, st);
+  if (vecs <= 4 * 26 * WAVE) return step_of<T, MODE, 4, 26, 3>(a, st);
+  if (vecs <= 8 * 16 * WAVE) return step_of<T, MODE, 8, 16, 4>(a, st);
+  if (vecs <= 16 * 13 * WAVE) return step_of<T, MODE, 16, 13, 4>(a, st);
   return step_of<T, MODE, 16, 16, 4>(a, st);
 }
 
