@@ -197,6 +197,7 @@ struct LogitsArgs {
   void* dz; long lddz;                                    // null: values alone
   // set by the launch
   int parts, part_cols, runs, run_cols, points;
+  bool stream;
   f32x4* part_sums; unsigned long long* part_lists; float* part_points;
 };
 constexpr int LOGITS_TOP_MOST = 64, LOGITS_KEPT_MOST = 256;

@@ -655,10 +655,17 @@ struct Slope {
   }
 };
 
-template <typename T> __device__ __forceinline__ void put_vector(T* p, const float (&x)[vec<T>()]) {
+template <typename T> __device__ __forceinline__ void put_vector(T* p, const float (&x)[vec<T>()], bool stream) {
   typedef __attribute__((address_space(1))) u32x4_u* gptr;
   const u32x4 w = encode<T>(x);
-  *(gptr)p = u32x4_u{w[0], w[1], w[2], w[3]};
+  const u32x4_u v = {w[0], w[1], w[2], w[3]};
+  if (stream) {
+    asm volatile("; past the caches");                   // (between two of these, or the compiler makes one ordinary store of both)
+    __builtin_nontemporal_store(v, (gptr)p);
+    asm volatile("; past the caches");
+  } else {
+    *(gptr)p = v;
+  }
 }
 // the gradient of a vector's elements, in place of them; token: its place among them, if it is there
 template <typename T, bool ENTROPY> __device__ __forceinline__ void slope_vector(float (&x)[vec<T>()], const Slope& s, int token) {
@@ -723,7 +730,7 @@ template <typename T> __device__ __forceinline__ void write_left_out(const Run<T
       float x[N];
       decode<T>(ld_global(reinterpret_cast<const u32x4*>(r.p + at)), x);
       slope_vector<T, false>(x, s, -1);
-      put_vector<T>(out + at, x);
+      put_vector<T>(out + at, x, false);
     }
   // .. then the points themselves (a wavefront's stores to an address keep their order).  An id that comes twice is added up in
   // order, by its first.
@@ -776,7 +783,8 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
 #pragma unroll
     for (int u = 0; u < STEP; ++u) {
       const int v = v0 + u * team + lane;
-      raw[u] = ld_global(reinterpret_cast<const u32x4*>(in.p + in.vec_at(v < in.vecs ? v : in.vecs - 1)));
+      const u32x4* at = reinterpret_cast<const u32x4*>(in.p + in.vec_at(v < in.vecs ? v : in.vecs - 1));
+      raw[u] = MODE == 0 ? ld_stream(at) : ld_global(at);
     }
   };
   if (in.vecs) load(0);
@@ -820,7 +828,7 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
         float x[N];
         decode<T>(raw[u], x);
         slope_vector<T, ENTROPY>(x, s, MODE == 0 && token >= 0 ? token - in.vec_at(v) : -1);
-        if (MODE == 0 || !(skip >> (chunk * STEP + u) & 1)) put_vector<T>(out + in.vec_at(v), x);
+        if (MODE == 0 || !(skip >> (chunk * STEP + u) & 1)) put_vector<T>(out + in.vec_at(v), x, MODE == 0 && a.stream);
       }
     }
     v0 += STEP * team;
@@ -972,9 +980,27 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
         if (MODE == 0 && a.logprob && token < 0) a.logprob[row] = pt.mass == 1.f ? (sums.none ? -__builtin_inff() : __builtin_nanf("")) : pt.mass;
       }
     }
-    auto at_token = [&](float x) {
-      if (a.logprob) a.logprob[row] = sums.bad ? __builtin_nanf("") : (x - base) / a.tau - sums.log_s;
-    };
+    // The token's logit, from the lane that holds it, which writes its element once more behind all others
+    float z_token = 0.f;
+    bool owner = false;
+    if (MODE == 0 && token >= 0) {
+      const int from_head = token - r.head, v = from_head / N;
+      if (token < r.head || v >= r.vecs) {
+        owner = lane < r.odd && r.odd_at(lane) == token;
+        z_token = odd;
+      } else {
+        u32x4 held = {0, 0, 0, 0};
+#pragma unroll
+        for (int u = 0; u < RV; ++u)
+          if (u == v / team) held = raw[u];              // (the same u for all lanes)
+        float x[N];
+        decode<T>(held, x);
+        z_token = x[0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) z_token = j == from_head - v * N ? x[j] : z_token;
+        owner = lane == v % team;
+      }
+    }
     const bool more = row + stride < a.rows;
     const Run<T> next(z, (more ? row + stride : row) * a.ld, a.cols);
     // log2 p = x c - Q - left: Q is P + rest + log2 s rounded
@@ -993,31 +1019,23 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
     };
     if (lane < r.odd && !(skip >> ODD_BIT)) {
       const int at = r.odd_at(lane);
-      out[at] = from_f<T>(gradient(odd) + (MODE == 0 && at == token ? slope.slope : 0.f));
-      if (MODE == 0 && at == token) at_token(odd);
+      out[at] = from_f<T>(gradient(odd));
     }
 #pragma unroll
     for (int u = 0; u < RV; ++u) {
-      const int v = u * team + lane;
-      if (v < r.vecs) {
+      if (u * team + wave * WAVE < r.vecs) {             // (the same for a whole wavefront)
+        const int v = u * team + lane;
         float x[N];
         decode<T>(raw[u], x);
-        const unsigned at = MODE == 0 && token >= 0 ? token - r.vec_at(v) : N;
-        if (at < (unsigned)N) {
-          float own = x[0];
-#pragma unroll
-          for (int j = 1; j < N; ++j) own = (int)at == j ? x[j] : own;
-          at_token(own);
-        }
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] = gradient(x[j]);
-        if (at < (unsigned)N) {
-#pragma unroll
-          for (int j = 0; j < N; ++j) x[j] += (int)at == j ? slope.slope : 0.f;
-        }
-        if (MODE == 0 || !(skip >> u & 1)) put_vector<T>(out + r.vec_at(v), x);
+        if (v < r.vecs && (MODE == 0 || !(skip >> u & 1))) put_vector<T>(out + r.vec_at(v), x, a.stream);
       }
       if (more) load(next, u);
+    }
+    if (owner) {
+      out[token] = from_f<T>(gradient(z_token) + slope.slope);
+      if (a.logprob) a.logprob[row] = sums.bad ? __builtin_nanf("") : (z_token - base) / a.tau - sums.log_s;
     }
     if (more) load_odd(next);
     if constexpr (MODE == 1) {
@@ -1082,14 +1100,17 @@ template <typename T, int MODE, int NW, int RV, int OCC> hipError_t step_of(cons
     return hipGetLastError();
   });
 }
+// The fewer wavefronts hold a row, the more rows a CU works on, whose loads, sums and stores overlap (8192 x 50304 bf16: 350 us
+// with 4 wavefronts, 358 with 8, 416 with 16); a row alone is done soonest by many (1 x 50304: 12.2 and 9.5 us with 4 and 16).
 template <typename T, int MODE> hipError_t step(const LogitsArgs& a, hipStream_t st) {
   const int vecs = a.cols / vec<T>();                    // (an odd element less may make one vector less)
+  const bool few = a.rows <= 2 * compute_units();
   if (vecs <= 4 * WAVE) return step_of<T, MODE, 1, 4, 4>(a, st);
   if (vecs <= 4 * 4 * WAVE) return step_of<T, MODE, 4, 4, 5>(a, st);
-  if (vecs <= 4 * 8 * WAVE) return step_of<T, MODE, 4, 8, 4>(a, st);
-  if (vecs <= 4 * 16 * WAVE) return step_of<T, MODE, 4, 16, 4>(a, st);
-  if (vecs <= 4 * 26 * WAVE) return step_of<T, MODE, 4, 26, 3>(a, st);
-  if (vecs <= 8 * 16 * WAVE) return step_of<T, MODE, 8, 16, 4>(a, st);
+  if (vecs <= 4 * 8 * WAVE && !few) return step_of<T, MODE, 4, 8, 4>(a, st);
+  if (vecs <= 4 * 16 * WAVE && !few) return step_of<T, MODE, 4, 16, 4>(a, st);
+  if (vecs <= 4 * 26 * WAVE && !few) return step_of<T, MODE, 4, 26, 3>(a, st);
+  if (vecs <= 16 * 8 * WAVE) return step_of<T, MODE, 16, 8, 4>(a, st);
   if (vecs <= 16 * 13 * WAVE) return step_of<T, MODE, 16, 13, 4>(a, st);
   return step_of<T, MODE, 16, 16, 4>(a, st);
 }
@@ -1124,6 +1145,8 @@ hipError_t launch_logits(LogitsArgs a, int mode, bool is_bf16, void* workspace, 
   a.parts = a.lse_in || resident ? 1 : parts_of(a.rows, a.cols, is_bf16);
   a.part_cols = a.cols;
   a.points = mode == 0 ? 1 : a.kept;
+  // Gradients that no cache could hold are written past them (measured: 4096 x 50304 with 32 kept 187 -> 172 us)
+  a.stream = elems * size > 256.0 * (1 << 20);
   if (a.parts > 1 || (stepping && !resident)) {
     // (whole 128-byte lines apart, but for the rows' own alignment)
     a.part_cols = ((a.cols + a.parts - 1) / a.parts + 63) / 64 * 64;
