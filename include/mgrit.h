@@ -436,7 +436,7 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
  *   p = softmax(z / temperature),  lse = ln sum exp(z / temperature),  ln p_i = z_i / temperature - lse,
  *   entropy H = - sum p_i ln p_i
  * Ids are 32- or 64-bit integers (id_dtype), contiguous.  Values are fp32, contiguous, and computed in fp32; dlogits has the logits'
- * type, rounded once, and may be the logits themselves (same stride), which it then replaces.
+ * type, rounded once, and may be the logits themselves (same stride), which it then replaces; it must not lie across them otherwise.
  *   A logit of -infinity is a masked one: p = 0.  A finite one whose quotient by the temperature passes fp32's range counts as infinite.
  *   A row of -infinity alone has no distribution: lse and every log probability -infinity, entropy 0, gradient 0.
  *   A row with a NaN or +infinity has NaN for all its values and its gradient, and -1 for its alternatives' ids.
@@ -452,8 +452,8 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
  *   g_logprob          device [rows];  g_entropy  device [rows], or NULL for 0
  * _step does both in one call that reads the logits once where a row fits, for cotangents that are known beforehand (a mean
  * of cross entropies: g_logprob = -1 / count); logprob and entropy may be NULL, lse may be NULL.
- * Workspace of _forward and _step: 256-byte aligned, mgrit_token_logprobs_workspace_bytes (host only; 0, also on invalid arguments:
- * none is needed and it may be NULL; _step: top_k 0). */
+ * Workspace of _forward (step 0) and _step (step 1): 256-byte aligned, mgrit_token_logprobs_workspace_bytes (host only; 0, also on
+ * invalid arguments: none is needed and it may be NULL). */
 #define MGRIT_TOP_MOST 64
 enum { MGRIT_IDS_I32 = 0, MGRIT_IDS_I64 = 1 };
 typedef struct mgrit_logits_desc {
@@ -463,7 +463,7 @@ typedef struct mgrit_logits_desc {
   int32_t id_dtype;              /* MGRIT_IDS_* */
   float   temperature;           /* 1e-4 to 1e4 */
 } mgrit_logits_desc;
-size_t mgrit_token_logprobs_workspace_bytes(const mgrit_logits_desc* desc, int32_t top_k);
+size_t mgrit_token_logprobs_workspace_bytes(const mgrit_logits_desc* desc, int32_t top_k, int step);
 int mgrit_token_logprobs_forward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const void* tokens,
                                  float* logprob, float* entropy, float* lse, int32_t top_k, void* top_ids, float* top_logprobs,
                                  void* workspace, size_t workspace_bytes, void* stream);
@@ -491,7 +491,7 @@ typedef struct mgrit_teacher {
   const void*  logits;           /* device [rows, kept] */
   const float* lse;              /* device [rows] at the same temperature, or NULL */
 } mgrit_teacher;
-size_t mgrit_distill_workspace_bytes(const mgrit_logits_desc* desc, int32_t kept);
+size_t mgrit_distill_workspace_bytes(const mgrit_logits_desc* desc, int32_t kept, int step);
 int mgrit_distill_forward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const mgrit_teacher* teacher,
                           float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 int mgrit_distill_backward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const mgrit_teacher* teacher,

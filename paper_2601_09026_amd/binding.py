@@ -136,7 +136,7 @@ def lib() -> C.CDLL:
             getattr(L, name).argtypes = [ld, vp, i64, *args]
             getattr(L, name).restype = C.c_int
         for name in ("mgrit_token_logprobs_workspace_bytes", "mgrit_distill_workspace_bytes"):
-            getattr(L, name).argtypes = [ld, i32]
+            getattr(L, name).argtypes = [ld, i32, C.c_int]
             getattr(L, name).restype = size
         L.mgrit_layer_norm_forward.argtypes = [nd, vp, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp]
         L.mgrit_layer_norm_forward.restype = C.c_int
@@ -1118,6 +1118,15 @@ def _out(given: Optional[torch.Tensor], shape, name: str, device: int, like: tor
     return given, _floats(given, shape, name, device)
 
 
+def _row_values(logprob, entropy, lse, lead, device: int, like: torch.Tensor, other):
+    """The three values per row: the caller's, or new ones (one allocation for all: 1 us less)."""
+    if logprob is None and entropy is None and lse is None:
+        logprob, entropy, lse = _new((3, *lead), torch.float32, like.device, other).unbind(0)
+        return logprob, logprob.data_ptr(), entropy, entropy.data_ptr(), lse, lse.data_ptr()
+    return (*_out(logprob, lead, "logprob", device, like, other), *_out(entropy, lead, "entropy", device, like, other),
+            *_out(lse, lead, "lse", device, like, other))
+
+
 def _dlogits(given: Optional[torch.Tensor], logits: torch.Tensor, cols: int, device: int, other):
     """(tensor, stride) of the logits' gradient."""
     if given is None:
@@ -1132,8 +1141,8 @@ def _logits_desc(logits: torch.Tensor, rows: int, cols: int, ids: torch.dtype, t
     return LogitsDesc(rows, cols, _DTYPES[logits.dtype], _ID_DTYPES[ids], temperature)
 
 
-def mgrit_token_logprobs_workspace_bytes(rows: int, cols: int, dtype: torch.dtype, top_k: int = 0) -> int:
-    return int(lib().mgrit_token_logprobs_workspace_bytes(LogitsDesc(rows, _c_int32(cols), _DTYPES[dtype], 0, 1.0), top_k))
+def mgrit_token_logprobs_workspace_bytes(rows: int, cols: int, dtype: torch.dtype, top_k: int = 0, step: bool = False) -> int:
+    return int(lib().mgrit_token_logprobs_workspace_bytes(LogitsDesc(rows, _c_int32(cols), _DTYPES[dtype], 0, 1.0), top_k, int(step)))
 
 
 def mgrit_token_logprobs_forward(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0, temperature: float = 1.0,
@@ -1151,14 +1160,14 @@ def mgrit_token_logprobs_forward(logits: torch.Tensor, tokens: Optional[torch.Te
     tokens_at = logprob_at = ids_at = top_at = None
     if tokens is not None:
         tokens_at = _ids(tokens, lead, "tokens", device)
-        logprob, logprob_at = _out(logprob, lead, "logprob", device, logits, other)
+        logprob, logprob_at, entropy, entropy_at, lse, lse_at = _row_values(logprob, entropy, lse, lead, device, logits, other)
         id_dtype = tokens.dtype
     else:
         if logprob is not None:
             raise ValueError("logprob: expected tokens as well")
         id_dtype = torch.int64 if top_ids is None else top_ids.dtype
-    entropy, entropy_at = _out(entropy, lead, "entropy", device, logits, other)
-    lse, lse_at = _out(lse, lead, "lse", device, logits, other)
+        entropy, entropy_at = _out(entropy, lead, "entropy", device, logits, other)
+        lse, lse_at = _out(lse, lead, "lse", device, logits, other)
     if top_k:
         if not 0 < top_k <= TOP_MOST:
             raise ValueError(f"top_k: expected 0 to {TOP_MOST}, got {top_k}")
@@ -1172,7 +1181,7 @@ def mgrit_token_logprobs_forward(logits: torch.Tensor, tokens: Optional[torch.Te
     elif top_ids is not None or top_logprobs is not None:
         raise ValueError("top_ids, top_logprobs: expected a top_k")
     L, desc = lib(), _logits_desc(logits, rows, cols, id_dtype, temperature)
-    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_token_logprobs_workspace_bytes(desc, top_k), logits.device, other)
+    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_token_logprobs_workspace_bytes(desc, top_k, 0), logits.device, other)
     st = L.mgrit_token_logprobs_forward(desc, logits.data_ptr(), stride, tokens_at, logprob_at, entropy_at, lse_at, top_k, ids_at, top_at,
                                         ws_at, ws_bytes, handle)
     if st != MGRIT_OK:
@@ -1220,12 +1229,10 @@ def mgrit_token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, g_logp
     handle, other = _on(stream, device)
     tokens_at, g_at = _ids(tokens, lead, "tokens", device), _floats(g_logprob, lead, "g_logprob", device)
     h_at = None if g_entropy is None else _floats(g_entropy, lead, "g_entropy", device)
-    logprob, logprob_at = _out(logprob, lead, "logprob", device, logits, other)
-    entropy, entropy_at = _out(entropy, lead, "entropy", device, logits, other)
-    lse, lse_at = _out(lse, lead, "lse", device, logits, other)
+    logprob, logprob_at, entropy, entropy_at, lse, lse_at = _row_values(logprob, entropy, lse, lead, device, logits, other)
     dlogits, dstride = _dlogits(dlogits, logits, cols, device, other)
     L, desc = lib(), _logits_desc(logits, rows, cols, tokens.dtype, temperature)
-    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_token_logprobs_workspace_bytes(desc, 0), logits.device, other)
+    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_token_logprobs_workspace_bytes(desc, 0, 1), logits.device, other)
     st = L.mgrit_token_logprobs_step(desc, logits.data_ptr(), stride, tokens_at, g_at, h_at, logprob_at, entropy_at, lse_at,
                                      dlogits.data_ptr(), dstride, ws_at, ws_bytes, handle)
     if st != MGRIT_OK:
@@ -1235,8 +1242,8 @@ def mgrit_token_logprobs_step(logits: torch.Tensor, tokens: torch.Tensor, g_logp
     return TokenLogprobs(logprob, entropy, lse), dlogits
 
 
-def mgrit_distill_workspace_bytes(rows: int, cols: int, dtype: torch.dtype, kept: int) -> int:
-    return int(lib().mgrit_distill_workspace_bytes(LogitsDesc(rows, _c_int32(cols), _DTYPES[dtype], 0, 1.0), _c_int32(kept)))
+def mgrit_distill_workspace_bytes(rows: int, cols: int, dtype: torch.dtype, kept: int, step: bool = False) -> int:
+    return int(lib().mgrit_distill_workspace_bytes(LogitsDesc(rows, _c_int32(cols), _DTYPES[dtype], 0, 1.0), _c_int32(kept), int(step)))
 
 
 def _teacher(logits: torch.Tensor, ids: torch.Tensor, values: torch.Tensor, lse: Optional[torch.Tensor], device: int) -> Teacher:
@@ -1268,7 +1275,7 @@ def mgrit_distill_forward(logits: torch.Tensor, teacher_ids: torch.Tensor, teach
     loss, loss_at = _out(loss, lead, "loss", device, logits, other)
     lse, lse_at = _out(lse, lead, "lse", device, logits, other)
     L, desc = lib(), _logits_desc(logits, rows, cols, teacher_ids.dtype, temperature)
-    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_distill_workspace_bytes(desc, teacher.kept), logits.device, other)
+    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_distill_workspace_bytes(desc, teacher.kept, 0), logits.device, other)
     st = L.mgrit_distill_forward(desc, logits.data_ptr(), stride, teacher, loss_at, lse_at, ws_at, ws_bytes, handle)
     if st != MGRIT_OK:
         raise MgritError(st, "mgrit_distill_forward")
@@ -1314,7 +1321,7 @@ def mgrit_distill_step(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_
     lse, lse_at = _out(lse, lead, "lse", device, logits, other)
     dlogits, dstride = _dlogits(dlogits, logits, cols, device, other)
     L, desc = lib(), _logits_desc(logits, rows, cols, teacher_ids.dtype, temperature)
-    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_distill_workspace_bytes(desc, teacher.kept), logits.device, other)
+    ws, ws_at, ws_bytes = _workspace(workspace, L.mgrit_distill_workspace_bytes(desc, teacher.kept, 1), logits.device, other)
     st = L.mgrit_distill_step(desc, logits.data_ptr(), stride, teacher, g_at, loss_at, lse_at, dlogits.data_ptr(), dstride, ws_at, ws_bytes,
                               handle)
     if st != MGRIT_OK:

@@ -200,8 +200,7 @@ struct LogitsArgs {
   bool stream;
   f32x4* part_sums; unsigned long long* part_lists; float* part_points;
 };
-constexpr int LOGITS_TOP_MOST = 64, LOGITS_KEPT_MOST = 256;
-size_t logits_workspace_bytes(long rows, int cols, bool is_bf16, int top_k, int points);
+size_t logits_workspace_bytes(long rows, int cols, bool is_bf16, int top_k, int points, bool step);
 hipError_t launch_logits(LogitsArgs a, int mode, bool is_bf16, void* workspace, hipStream_t st);   // mode 0: log probabilities, 1: distillation
 
 // ---- attention.hip -----------------------------------------------------------

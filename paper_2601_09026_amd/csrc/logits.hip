@@ -39,10 +39,10 @@ template <typename T> struct Run {
   }
   __device__ __forceinline__ int odd_at(int i) const { return i < head ? i : i + vecs * vec<T>(); }
   __device__ __forceinline__ int vec_at(int v) const { return head + v * vec<T>(); }
-  // Chunks of STEP vectors per lane of W wavefronts; 2^fold of them are a group, at most GROUPS a run
-  template <int W> __device__ __forceinline__ int chunks() const { return vecs ? (vecs - 1) / (STEP * W * WAVE) + 1 : 1; }
-  template <int W> __device__ __forceinline__ int fold() const { return chunks<W>() <= GROUPS ? 0 : 32 - __builtin_clz((chunks<W>() - 1) / GROUPS); }
-  template <int W> __device__ __forceinline__ int groups() const { return ((chunks<W>() - 1) >> fold<W>()) + 1; }
+  // Chunks of STEP vectors per lane of a block; 2^fold of them are a group, at most GROUPS a run
+  __device__ __forceinline__ int chunks() const { return vecs ? (vecs - 1) / (STEP * THREADS) + 1 : 1; }
+  __device__ __forceinline__ int fold() const { return chunks() <= GROUPS ? 0 : 32 - __builtin_clz((chunks() - 1) / GROUPS); }
+  __device__ __forceinline__ int groups() const { return ((chunks() - 1) >> fold()) + 1; }
 };
 
 template <typename T> __device__ __forceinline__ void decode(u32x4 r, float (&x)[vec<T>()]);
@@ -215,6 +215,7 @@ struct Top {
       if (__popcll(__ballot(mine >= (low | bit))) >= want) low |= bit;
     return low;
   }
+  static __device__ __forceinline__ float bar_of(unsigned low) { return low > 0x007fffffu ? value_of((u64)low << 32) : LOWEST; }    // (masked elements: fill())
   // sorts the list, the k first stay
   __device__ __forceinline__ void settle() {
     const int lane = threadIdx.x & 63;
@@ -246,23 +247,67 @@ struct Top {
     n += __popcll(who);
     if (n > LIST - WAVE) settle();
   }
-  // the rest of the list is empty
+  // the elements of the lane's vectors that reach the bar: those of vector u where inside(u), index(u) the first's
+  template <typename T, int COUNT, typename F, typename G> __device__ __forceinline__ void take_high(const u32x4 (&raw)[COUNT], float bar, F inside, G index) {
+    constexpr int N = vec<T>();
+    static_assert(COUNT * N <= 32, "a bit each");
+    unsigned high = 0;
+#pragma unroll
+    for (int u = COUNT - 1; u >= 0; --u) {
+      const bool in = inside(u);
+      float x[N];
+      decode<T>(raw[u], x);
+#pragma unroll
+      for (int j = N - 1; j >= 0; --j) high = high << 1 | (unsigned)(in && x[j] >= bar);
+    }
+    while (__any(high != 0)) {
+      const int e = high ? __builtin_ctz(high) : 0, u = e / N, j = e % N;
+      unsigned w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[i] = raw[0][i];
+#pragma unroll
+        for (int o = 1; o < COUNT; ++o) w[i] = u == o ? raw[o][i] : w[i];
+      }
+      const int d = sizeof(T) == 2 ? j >> 1 : j;
+      const unsigned lo = d & 1 ? w[1] : w[0], hi = d & 1 ? w[3] : w[2], word = d & 2 ? hi : lo;
+      const float x = bits_f(sizeof(T) == 4 ? word : j & 1 ? word & 0xffff0000u : word << 16);
+      take(high != 0, candidate(x, index(u) + j));
+      high &= high - 1;
+    }
+  }
+  // sorted; the rest of the list is empty
   __device__ __forceinline__ void finish() {
     settle();
     const int lane = threadIdx.x & 63;
     if (lane >= n && lane < k) list[lane] = 0;
     wave_sync();
   }
+  // A list of fewer than k that holds all elements but the masked ones: of those, the first of the `count` from `from` on
+  __device__ __forceinline__ void fill(int from, int count) {
+    const int lane = threadIdx.x & 63;
+    int have = n;
+    for (int i0 = 0; have < k && i0 < count; i0 += WAVE) {
+      bool masked = i0 + lane < count;
+      for (int j = 0; j < n; ++j) masked = masked && index_of(list[j]) != from + i0 + lane;
+      const u64 who = __ballot(masked);
+      const int at = have + __popcll(who & ((1ull << lane) - 1));
+      if (masked && at < k) list[at] = candidate(-__builtin_inff(), from + i0 + lane);
+      have += __popcll(who);
+    }
+    wave_sync();
+  }
 };
 
-// ---- a row's sums (and its largest elements), by W wavefronts ---------------------------
+// ---- a row's sums (and its largest elements), by a block --------------------------------
 template <typename T> constexpr unsigned NOTHING = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;          // -infinity
 
-// The team's wavefronts go through the run's chunks of STEP vectors per lane.
-template <typename T, int W, bool T_SUM, bool TOP>
+// The block goes through the run's chunks of STEP vectors per lane.  What comes back is each wavefront's own.
+template <typename T, bool T_SUM, bool TOP>
 __device__ __forceinline__ Sums read_run(const Run<T>& r, int lane, float c, Top& top) {
-  constexpr int N = vec<T>(), team = W * WAVE;
+  constexpr int N = vec<T>(), team = THREADS;
   const float none = -__builtin_inff();
+  const int fold = TOP ? r.fold() : 0;
   Reader<T_SUM> sums;
   sums.start(c);
   const bool odd = lane < r.odd;                         // (odd < 2 N: lanes of the first wavefront)
@@ -332,8 +377,8 @@ __device__ __forceinline__ Sums read_run(const Run<T>& r, int lane, float c, Top
     }
     if constexpr (TOP) {
       group = fmaxf(group, all);
-      if (((chunk + 1) & ((1 << r.template fold<W>()) - 1)) == 0 || v0 + STEP * team >= r.vecs) {
-        top.groups[(chunk >> r.template fold<W>()) * THREADS] = group;
+      if (((chunk + 1) & ((1 << fold) - 1)) == 0 || v0 + STEP * team >= r.vecs) {
+        top.groups[(chunk >> fold) * THREADS] = group;
         top.best = fmaxf(top.best, group);
         group = none;
       }
@@ -344,10 +389,10 @@ __device__ __forceinline__ Sums read_run(const Run<T>& r, int lane, float c, Top
 }
 
 // The candidates among a lane's elements: those of its groups that reach the bar are read again
-template <typename T, int W> __device__ __forceinline__ void pick(const Run<T>& r, int lane, int index, unsigned low, Top& top) {
-  constexpr int N = vec<T>(), team = W * WAVE;
-  const float bar = low > 0x007fffffu ? value_of((u64)low << 32) : -__builtin_inff();
-  const int fold = r.template fold<W>(), groups = r.template groups<W>();
+template <typename T> __device__ __forceinline__ void pick(const Run<T>& r, int lane, int index, unsigned low, Top& top) {
+  constexpr int team = THREADS;
+  const float bar = Top::bar_of(low);
+  const int fold = r.fold(), groups = r.groups();
   top.take(lane < r.odd && top.first >= bar, candidate(top.first, index + r.odd_at(lane)));
   unsigned hit = 0;
   for (int g = 0; g < groups; ++g) hit |= top.groups[g * THREADS] >= bar ? 1u << g : 0u;
@@ -362,63 +407,36 @@ template <typename T, int W> __device__ __forceinline__ void pick(const Run<T>& 
         const int v = v0 + u * team;
         raw[u] = ld_global(reinterpret_cast<const u32x4*>(r.p + r.vec_at(hit && v < r.vecs ? v : 0)));
       }
-      unsigned high = 0;                                 // elements that reach it, a bit each
-#pragma unroll
-      for (int u = STEP - 1; u >= 0; --u) {
-        const bool inside = hit && v0 + u * team < r.vecs;
-        float x[N];
-        decode<T>(raw[u], x);
-#pragma unroll
-        for (int j = N - 1; j >= 0; --j) high = high << 1 | (unsigned)(inside && x[j] >= bar);
-      }
-      while (__any(high != 0)) {
-        const int e = high ? __builtin_ctz(high) : 0, u = e / N, j = e % N;
-        unsigned w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[i] = raw[0][i];
-#pragma unroll
-          for (int o = 1; o < STEP; ++o) w[i] = u == o ? raw[o][i] : w[i];
-        }
-        const int d = sizeof(T) == 2 ? j >> 1 : j;
-        const unsigned lo = d & 1 ? w[1] : w[0], hi = d & 1 ? w[3] : w[2], word = d & 2 ? hi : lo;
-        const float x = bits_f(sizeof(T) == 4 ? word : j & 1 ? word & 0xffff0000u : word << 16);
-        top.take(high != 0, candidate(x, index + r.vec_at(v0 + u * team) + j));
-        high &= high - 1;
-      }
+      top.template take_high<T>(raw, bar, [&](int u) { return hit && v0 + u * team < r.vecs; }, [&](int u) { return index + r.vec_at(v0 + u * team); });
     }
     hit &= hit - 1;
   }
   top.finish();
 }
 
-// What a team's wavefronts found: the sums in all of them, the list in the first.
-template <typename T, int W, bool TOP>
-__device__ __forceinline__ void join_waves(const Run<T>& r, int lane, int index, Sums& sums, Top& top, f32x4* waves, u64* lists, float c) {
+// What a block's wavefronts found: the sums in all of them, the list in the first.
+template <typename T, bool TOP>
+__device__ __forceinline__ void join_waves(const Run<T>& r, int index, Sums& sums, Top& top, f32x4* waves, u64* lists, float c) {
+  const int wave = threadIdx.x / WAVE, lane = threadIdx.x & 63;
   unsigned low = 0;
-  if constexpr (TOP) low = top.reached((top.k + W - 1) / W);
-  if constexpr (W > 1) {
-    const int wave = threadIdx.x / WAVE;
-    if ((threadIdx.x & 63) == 0) waves[wave] = f32x4{sums.m, sums.s, sums.t, bits_f(low)};
-    __syncthreads();
-    Sums all = {waves[0][0], waves[0][1], waves[0][2]};
-    low = f_bits(waves[0][3]);
+  if constexpr (TOP) low = top.reached((top.k + WAVES - 1) / WAVES);
+  if (lane == 0) waves[wave] = f32x4{sums.m, sums.s, sums.t, bits_f(low)};
+  __syncthreads();
+  sums = Sums{waves[0][0], waves[0][1], waves[0][2]};
+  low = f_bits(waves[0][3]);
 #pragma unroll
-    for (int w = 1; w < W; ++w) {
-      merge(all, Sums{waves[w][0], waves[w][1], waves[w][2]}, c);
-      const unsigned other = f_bits(waves[w][3]);        // (k / W of every wavefront's lanes reach the least of these)
-      low = other < low ? other : low;
-    }
-    sums = all;
+  for (int w = 1; w < WAVES; ++w) {
+    merge(sums, Sums{waves[w][0], waves[w][1], waves[w][2]}, c);
+    const unsigned other = f_bits(waves[w][3]);          // (a quarter of the k lanes in every wavefront reach the least of these)
+    low = other < low ? other : low;
   }
   if constexpr (TOP) {
-    pick<T, W>(r, lane, index, low, top);
-    if constexpr (W > 1) {
-      __syncthreads();
-      if (threadIdx.x < WAVE) {
-        for (int w = 1; w < W; ++w) top.take(lane < top.k, lane < top.k ? lists[w * ROOM + lane] : 0);
-        top.finish();
-      }
+    pick<T>(r, threadIdx.x, index, low, top);
+    __syncthreads();
+    if (wave == 0) {
+      for (int w = 1; w < WAVES; ++w) top.take(lane < top.k, lane < top.k ? lists[w * ROOM + lane] : 0);
+      top.finish();
+      if (top.n < top.k) top.fill(index, r.vecs * vec<T>() + r.odd);
     }
   }
 }
@@ -533,53 +551,49 @@ __device__ __forceinline__ void put_alternatives(const LogitsArgs& a, long row, 
 }
 
 // ---- values of a row --------------------------------------------------------------------
-// Teams of W wavefronts walk (row, part) pairs; with several parts a row's sums, lists and points go to the workspace.
-template <typename T, int W, bool TOP, int MODE>
+// A block per row, or per part of it; with several parts a row's sums, lists and points go to the workspace.
+template <typename T, bool TOP, int MODE>
 __global__ void __launch_bounds__(THREADS, 6) logits_values_kernel(const LogitsArgs a) {
   __shared__ u64 lists[TOP ? WAVES * ROOM : 1];
   __shared__ f32x4 waves[WAVES];
   __shared__ float groups[TOP ? GROUPS * THREADS : 1];
-  constexpr int TEAMS = WAVES / W;
-  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % (W * WAVE);
+  const int wave = threadIdx.x / WAVE, lane = threadIdx.x & 63;
   const float c = LOG2E / a.tau;
-  const long tasks = a.rows * a.parts;
-  const long task = block_index() * TEAMS + wave / W;
-  if (task >= tasks) return;                             // (a team of a whole block together; one of a wavefront meets no barrier)
-  {
-    const long row = task / a.parts;
-    const int part = (int)(task - row * a.parts), from = part * a.part_cols;
-    const int n = a.cols - from < a.part_cols ? a.cols - from : a.part_cols;
-    const T* z = static_cast<const T*>(a.z) + row * a.ld;
-    Top top;
-    if constexpr (TOP) top.start(lists, groups, a.top_k);
-    const Run<T> in(z, from, n);
-    Sums sums = read_run<T, W, MODE == 0, TOP>(in, lane, c, top);
-    join_waves<T, W, TOP>(in, lane, from, sums, top, waves, lists, c);
-    if (wave % W == 0) {
-      Points<MODE> pt;
-      if (part == 0 && (!a.part_sums || a.part_points)) {
-        pt.load(a, row);
-        pt.gather(z, 0, a.cols);
-      }
-      if (!a.part_sums) {
-        const RowSums r(sums, a.tau);
-        put_values<MODE>(a, row, r, pt);
-        if constexpr (TOP) put_alternatives(a, row, r, top.list);
-      } else {
-        if (lane == 0) a.part_sums[task] = f32x4{sums.m, sums.s, sums.t, 0.f};
-        if constexpr (TOP)
-          if (lane < a.top_k) a.part_lists[task * a.top_k + lane] = top.list[lane];
-        if (part == 0 && a.part_points) {
+  const long task = block_index();
+  if (task >= a.rows * a.parts) return;
+  const long row = task / a.parts;
+  const int part = (int)(task - row * a.parts), from = part * a.part_cols;
+  const int n = a.cols - from < a.part_cols ? a.cols - from : a.part_cols;
+  const T* z = static_cast<const T*>(a.z) + row * a.ld;
+  const bool asked = wave == 0 && part == 0 && (!a.part_sums || a.part_points);
+  Points<MODE> pt;
+  if (asked) {
+    pt.load(a, row);
+    pt.gather(z, 0, a.cols);
+  }
+  Top top;
+  if constexpr (TOP) top.start(lists, groups, a.top_k);
+  const Run<T> in(z, from, n);
+  Sums sums = read_run<T, MODE == 0, TOP>(in, threadIdx.x, c, top);
+  join_waves<T, TOP>(in, from, sums, top, waves, lists, c);
+  if (wave != 0) return;
+  if (!a.part_sums) {
+    const RowSums r(sums, a.tau);
+    put_values<MODE>(a, row, r, pt);
+    if constexpr (TOP) put_alternatives(a, row, r, top.list);
+    return;
+  }
+  if (lane == 0) a.part_sums[task] = f32x4{sums.m, sums.s, sums.t, 0.f};
+  if constexpr (TOP)
+    if (lane < a.top_k) a.part_lists[task * a.top_k + lane] = top.list[lane];
+  if (asked) {
 #pragma unroll
-          for (int i = 0; i < Points<MODE>::N; ++i)
-            if (i * WAVE + lane < a.points) a.part_points[row * a.points + i * WAVE + lane] = pt.z[i];
-        }
-      }
-    }
+    for (int i = 0; i < Points<MODE>::N; ++i)
+      if (i * WAVE + lane < a.points) a.part_points[row * a.points + i * WAVE + lane] = pt.z[i];
   }
 }
 
-// A row's sums from those of its parts (by a wavefront; MOST_PARTS <= 64)
+// A row's sums from those of its parts, one per lane
 __device__ __forceinline__ Sums joined(const LogitsArgs& a, long row, float c) {
   const int lane = threadIdx.x & 63;
   Sums own = {LOWEST, 0.f, 0.f};
@@ -596,28 +610,36 @@ __global__ void __launch_bounds__(THREADS) logits_join_kernel(const LogitsArgs a
   __shared__ u64 lists[TOP ? WAVES * ROOM : 1];
   const int wave = threadIdx.x / WAVE, lane = threadIdx.x & 63;
   const long row = block_index() * WAVES + wave;
-  if (row < a.rows) {
-    const RowSums r(joined(a, row, LOG2E / a.tau), a.tau);
-    Points<MODE> pt;
-    pt.load(a, row);
-    pt.gather(static_cast<const T*>(a.z) + row * a.ld, 0, a.cols);
-    put_values<MODE>(a, row, r, pt);
-    if constexpr (TOP) {
-      Top top;
-      top.start(lists, nullptr, a.top_k);
-      const int all = a.parts * a.top_k;
-      const u64* from = a.part_lists + row * all;
-      // each of the parts has (k / parts, rounded up) candidates that reach the least of their last
-      u64 low = ~0ull;
-      if (lane < a.parts) low = from[lane * a.top_k + (a.top_k + a.parts - 1) / a.parts - 1];
+  if (row >= a.rows) return;
+  // (what is loaded comes first: each load's way there and back is as long as the rest)
+  constexpr int FIRST = 4;
+  const int all = a.parts * a.top_k;
+  u64 low = ~0ull, keys[FIRST];
+  if constexpr (TOP) {
+    const u64* from = a.part_lists + row * all;
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) { const u64 other = __shfl_xor(low, o, 64); low = other < low ? other : low; }
-      top.floor = low ? low - 1 : 0;
-      for (int i = 0; i < all; i += WAVE) top.take(i + lane < all, i + lane < all ? from[i + lane] : 0);
-      top.finish();
-      put_alternatives(a, row, r, top.list);
-    }
+    for (int i = 0; i < FIRST; ++i) keys[i] = i * WAVE + lane < all ? from[i * WAVE + lane] : 0;
+    // each of the parts has (k / parts, rounded up) candidates that reach the least of their last
+    if (lane < a.parts) low = from[lane * a.top_k + (a.top_k + a.parts - 1) / a.parts - 1];
   }
+  Points<MODE> pt;
+  pt.load(a, row);
+  pt.gather(static_cast<const T*>(a.z) + row * a.ld, 0, a.cols);
+  const RowSums r(joined(a, row, LOG2E / a.tau), a.tau);
+  if constexpr (TOP) {
+    Top top;
+    top.start(lists, nullptr, a.top_k);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) { const u64 other = __shfl_xor(low, o, 64); low = other < low ? other : low; }
+    top.floor = low ? uniform(low) - 1 : 0;
+#pragma unroll
+    for (int i = 0; i < FIRST; ++i) top.take(true, keys[i]);
+    const u64* from = a.part_lists + row * all;
+    for (int i = FIRST * WAVE; i < all; i += WAVE) top.take(i + lane < all, i + lane < all ? from[i + lane] : 0);
+    top.finish();
+    put_alternatives(a, row, r, top.list);
+  }
+  put_values<MODE>(a, row, r, pt);
 }
 
 // ---- gradients of a row -------------------------------------------------------------------
@@ -844,14 +866,18 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
 
 // ---- values and gradients of rows that fit the registers of NW wavefronts -------------------------
 // RV vectors per lane.  A row is read once; the next row's loads are issued as its registers are written.
-template <typename T, int NW, int RV, bool ENTROPY, int MODE, int OCC>
+// GRAD false: the values alone, of short rows (NW = 1), TOP with alternatives.
+template <typename T, int NW, int RV, bool ENTROPY, int MODE, int OCC, bool GRAD, bool TOP>
 __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_step_kernel(const LogitsArgs a) {
+  static_assert(NW == 1 || (GRAD && !TOP), "longer rows have kernels of their own for values");
+  __shared__ u64 lists[TOP ? WAVES * ROOM : 1];
+  Top best;
   constexpr int N = vec<T>(), team = NW * WAVE, TEAMS = NW == 1 ? WAVES : 1;
   __shared__ float tops[TEAMS * NW];
   __shared__ f32x2 waves[TEAMS * NW];
-  __shared__ unsigned left_out[MODE == 1 ? TEAMS * team : 1];
-  __shared__ int ids[MODE == 1 ? TEAMS * KEPT : 1];
-  __shared__ float ws[MODE == 1 ? TEAMS * KEPT : 1];
+  __shared__ unsigned left_out[MODE == 1 && GRAD ? TEAMS * team : 1];
+  __shared__ int ids[MODE == 1 && GRAD ? TEAMS * KEPT : 1];
+  __shared__ float ws[MODE == 1 && GRAD ? TEAMS * KEPT : 1];
   __shared__ float mass[TEAMS];
   const int group = NW == 1 ? threadIdx.x / WAVE : 0, lane = threadIdx.x % team, wave = lane / WAVE, l = threadIdx.x & 63;
   const float c = LOG2E / a.tau, none = -__builtin_inff();
@@ -873,7 +899,7 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
     if (u * team < r.vecs) raw[u] = ld_stream(reinterpret_cast<const u32x4*>(r.p + r.vec_at(v < r.vecs ? v : r.vecs - 1)));
   };
   auto load_odd = [&](const Run<T>& r) { odd = lane < r.odd ? to_f(r.p[r.odd_at(lane)]) : none; };
-  if constexpr (MODE == 1) left_out[group * team + lane] = 0;
+  if constexpr (MODE == 1 && GRAD) left_out[group * team + lane] = 0;
   long row = (long)blockIdx.x * TEAMS + group;
   if (row < a.rows) {
     const Run<T> r(z, row * a.ld, a.cols);
@@ -909,6 +935,15 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
 #pragma unroll
       for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
     });
+    if constexpr (TOP) {
+      best.start(lists, nullptr, a.top_k);
+      best.best = top;
+      const float bar = Top::bar_of(best.reached(a.top_k));
+      best.take(lane < r.odd && odd >= bar, candidate(odd, r.odd_at(lane)));
+      best.template take_high<T>(raw, bar, [&](int u) { return u * team + lane < r.vecs; }, [&](int u) { return r.vec_at(u * team + lane); });
+      best.finish();
+      if (best.n < best.k) best.fill(0, a.cols);
+    }
     top = all_max(top);
     if constexpr (NW > 1) {
       if (l == 0) tops[wave] = top;
@@ -948,7 +983,7 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
     s = all_sum(s);
     if constexpr (MODE == 0) t = all_sum(t);
     if constexpr (MODE == 1) {
-      if (wave == 0) {
+      if (GRAD && wave == 0) {
         marked = leave_out<T>(r, pt, 0, a.cols, team, left_out + group * team, ids + group * KEPT, ws + group * KEPT);
         if (l == 0) mass[group] = pt.mass;
       }
@@ -963,13 +998,14 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
     const RowSums sums(Sums{top, s, t}, a.tau);
     unsigned skip = 0;
     float weight = pt.mass;
-    if constexpr (MODE == 1) {
+    if constexpr (MODE == 1 && GRAD) {
       weight = mass[group];
       skip = left_out[group * team + lane];
       left_out[group * team + lane] = 0;                 // (marked again only behind the next row's first meeting)
     }
     Slope slope;
-    slope.template set<ENTROPY>(a, row, weight, MODE == 0 ? 1.f : -1.f, sums.entropy);
+    slope.zero = false;
+    if constexpr (GRAD) slope.template set<ENTROPY>(a, row, weight, MODE == 0 ? 1.f : -1.f, sums.entropy);
     slope.from_sums(sums);
     const int token = MODE == 0 && pt.id[0] >= 0 && !slope.zero ? pt.id[0] : -1;
     if (wave == 0) {
@@ -1003,6 +1039,17 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
     }
     const bool more = row + stride < a.rows;
     const Run<T> next(z, (more ? row + stride : row) * a.ld, a.cols);
+    if constexpr (!GRAD) {
+      if (owner && a.logprob) a.logprob[row] = sums.bad ? __builtin_nanf("") : (z_token - base) / a.tau - sums.log_s;
+      if (MODE == 1) put_values<MODE>(a, row, sums, pt);
+      if constexpr (TOP) put_alternatives(a, row, sums, best.list);
+#pragma unroll
+      for (int u = 0; u < RV; ++u)
+        if (more) load(next, u);
+      if (more) load_odd(next);
+      if (MODE == 1 && more) pt.fetch(a, row + stride);
+      continue;
+    }
     // log2 p = x c - Q - left: Q is P + rest + log2 s rounded
     const float tail = rest + slope.off * LOG2E;
     float Q = P + tail;
@@ -1051,8 +1098,8 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
 
 // ---- launches ---------------------------------------------------------------------------
 constexpr long MOST_BLOCKS = 1 << 22;                    // along x (a launch has at most 2^32 threads there)
-constexpr int MOST_PARTS = 16;
-static_assert(MOST_PARTS <= WAVE, "a lane per part");
+constexpr int MOST_PARTS = WAVE;                         // a lane per part in the join
+
 template <typename F> hipError_t with(bool x, F&& f) { return x ? f(std::true_type()) : f(std::false_type()); }
 dim3 blocks_for(long tasks, int teams) {
   const long b = (tasks + teams - 1) / teams;
@@ -1060,12 +1107,18 @@ dim3 blocks_for(long tasks, int teams) {
 }
 // short rows: one wavefront each
 bool short_rows(int cols, bool is_bf16) { return cols <= (is_bf16 ? 2048 : 1024); }
-// Few rows: a row's elements are shared out over several blocks
+// Few rows: a row's elements are shared out over several blocks, with a join behind them, from 64 KB on (1 x 16000 bf16, 20
+// alternatives: 8.3 us whole, 11.7 in three parts; 1 x 50257: 12 in 12 parts, 20 in one), into no less than 8 KB, and
+// so that there are no more than two blocks per CU (300 x 50257: 18.5 us whole, 26.6 in six parts); 128 KB a part
+// in any case (300 x 200000: 51 us whole, 41 in three parts).
 int parts_of(long rows, int cols, bool is_bf16) {
-  if (short_rows(cols, is_bf16) || rows >= 512) return 1;
-  const long most = cols / 4096, wanted = 512 / (rows < 1 ? 1 : rows);
-  const long parts = wanted < most ? wanted : most;
-  return (int)(parts < 1 ? 1 : parts > MOST_PARTS ? MOST_PARTS : parts);
+  const long bytes = (long)cols * (is_bf16 ? 2 : 4);
+  if (bytes < 65536 || rows >= 512 || rows < 1) return 1;
+  long parts = 512 / rows < bytes / 8192 ? 512 / rows : bytes / 8192;
+  if (parts > 16) parts = 16;
+  const long least = 2048 / rows < bytes / 131072 ? 2048 / rows : bytes / 131072;
+  if (parts < least) parts = least;
+  return (int)(parts < MOST_PARTS ? parts : MOST_PARTS);
 }
 // rows that a step keeps in registers
 bool fits(int cols, bool is_bf16) { return cols <= (is_bf16 ? 131072 : 65536); }
@@ -1074,10 +1127,10 @@ size_t parts_bytes(long rows, int parts, int top_k, int points) {
   return up256(rows * parts * sizeof(f32x4)) + up256(rows * parts * top_k * sizeof(u64)) + up256((size_t)rows * points * sizeof(float));
 }
 
-template <typename T, int W, int MODE> hipError_t values(const LogitsArgs& a, hipStream_t st) {
+template <typename T, int MODE> hipError_t values(const LogitsArgs& a, hipStream_t st) {
   return with(a.top_k > 0 && MODE == 0, [&](auto top) -> hipError_t {
     constexpr bool TOP = decltype(top)::value && MODE == 0;
-    logits_values_kernel<T, W, TOP, MODE><<<blocks_for(a.rows * a.parts, WAVES / W), THREADS, 0, st>>>(a);
+    logits_values_kernel<T, TOP, MODE><<<blocks_for(a.rows * a.parts, 1), THREADS, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.part_sums || a.dz) return e;
     logits_join_kernel<T, TOP, MODE><<<blocks_for(a.rows, WAVES), THREADS, 0, st>>>(a);
@@ -1095,8 +1148,15 @@ template <typename T, int MODE, int NW, int RV, int OCC> hipError_t step_of(cons
   // as many blocks as run at once: each walks over its rows
   const long most = (long)compute_units() * (4 * OCC * WAVE / threads), blocks = (a.rows + teams - 1) / teams;
   const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+  if constexpr (NW == 1) {
+    if (!a.dz)
+      return with(MODE == 0 && a.top_k > 0, [&](auto top) -> hipError_t {
+        logits_step_kernel<T, NW, RV, false, MODE, OCC, false, decltype(top)::value && MODE == 0><<<grid, threads, 0, st>>>(a);
+        return hipGetLastError();
+      });
+  }
   return with(MODE == 0 && a.h, [&](auto entropy) -> hipError_t {
-    logits_step_kernel<T, NW, RV, decltype(entropy)::value && MODE == 0, MODE, OCC><<<grid, threads, 0, st>>>(a);
+    logits_step_kernel<T, NW, RV, decltype(entropy)::value && MODE == 0, MODE, OCC, true, false><<<grid, threads, 0, st>>>(a);
     return hipGetLastError();
   });
 }
@@ -1105,7 +1165,8 @@ template <typename T, int MODE, int NW, int RV, int OCC> hipError_t step_of(cons
 template <typename T, int MODE> hipError_t step(const LogitsArgs& a, hipStream_t st) {
   const int vecs = a.cols / vec<T>();                    // (an odd element less may make one vector less)
   const bool few = a.rows <= 2 * compute_units();
-  if (vecs <= 4 * WAVE) return step_of<T, MODE, 1, 4, 4>(a, st);
+  if (vecs <= WAVE) return step_of<T, MODE, 1, 1, 6>(a, st);
+  if (vecs <= 4 * WAVE) return step_of<T, MODE, 1, 4, 5>(a, st);
   if (vecs <= 4 * 4 * WAVE) return step_of<T, MODE, 4, 4, 5>(a, st);
   if (vecs <= 4 * 8 * WAVE && !few) return step_of<T, MODE, 4, 8, 4>(a, st);
   if (vecs <= 4 * 16 * WAVE && !few) return step_of<T, MODE, 4, 16, 4>(a, st);
@@ -1117,8 +1178,8 @@ template <typename T, int MODE> hipError_t step(const LogitsArgs& a, hipStream_t
 
 template <typename T, int W, int MODE> hipError_t launch(LogitsArgs a, bool resident, hipStream_t st) {
   constexpr int TILE = THREADS * STEP * vec<T>();
-  if (!a.dz) return values<T, W, MODE>(a, st);
-  if (resident) return step<T, MODE>(a, st);
+  if (resident || (W == 1 && !a.dz)) return step<T, MODE>(a, st);
+  if (!a.dz) return values<T, MODE>(a, st);
   a.runs = 1;
   a.run_cols = a.cols;
   if (W > 1) {
@@ -1126,15 +1187,19 @@ template <typename T, int W, int MODE> hipError_t launch(LogitsArgs a, bool resi
     a.runs = (a.cols + TILE - 1) / TILE;
   }
   if (a.lse_in) return gradient<T, W, MODE, GIVEN>(a, st);
-  const hipError_t e = values<T, W, MODE>(a, st);
-  return e != hipSuccess ? e : gradient<T, W, MODE, PARTS>(a, st);
+  if constexpr (W > 1) {                                 // (short rows fit)
+    const hipError_t e = values<T, MODE>(a, st);
+    return e != hipSuccess ? e : gradient<T, W, MODE, PARTS>(a, st);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
 
-size_t logits_workspace_bytes(long rows, int cols, bool is_bf16, int top_k, int points) {
+size_t logits_workspace_bytes(long rows, int cols, bool is_bf16, int top_k, int points, bool step) {
+  if (rows == 0 || (step && fits(cols, is_bf16))) return 0;
   const int parts = parts_of(rows, cols, is_bf16);
-  return parts > 1 || !fits(cols, is_bf16) ? parts_bytes(rows, parts, top_k, points) : 0;
+  return parts > 1 || step ? parts_bytes(rows, parts, top_k, points) : 0;
 }
 
 hipError_t launch_logits(LogitsArgs a, int mode, bool is_bf16, void* workspace, hipStream_t st) {

@@ -82,10 +82,18 @@ int check_teacher(const mgrit_logits_desc* d, const mgrit_teacher* t) {
   STCHK(check_ids(d, t->ids));
   return d->rows && (!t->logits || !element_aligned(t->logits, t->dtype) || !aligned(t->lse, 4)) ? MGRIT_INVALID_ARG : MGRIT_OK;
 }
-// gradients beside the logits, or in their place
+// gradients beside the logits, or in their place: nowhere across them
 int check_dlogits(const mgrit_logits_desc* d, const void* logits, int64_t stride, const void* dlogits, int64_t dstride) {
   STCHK(check_rows(d->rows, d->cols, dlogits, dstride, d->dtype));
-  return d->rows && logits == dlogits && stride != dstride ? MGRIT_INVALID_ARG : MGRIT_OK;
+  if (d->rows == 0) return MGRIT_OK;
+  const int64_t size = d->dtype == MGRIT_DTYPE_BF16 ? 2 : 4, apart = static_cast<const char*>(dlogits) - static_cast<const char*>(logits);
+  const int64_t z_bytes = ((d->rows - 1) * stride + d->cols) * size, dz_bytes = ((d->rows - 1) * dstride + d->cols) * size;
+  if (apart >= z_bytes || -apart >= dz_bytes) return MGRIT_OK;
+  if (d->rows > 1 && stride != dstride) return MGRIT_INVALID_ARG;
+  if (apart == 0) return MGRIT_OK;
+  // slices of the same wider rows
+  const int64_t at = (apart / size % stride + stride) % stride;
+  return apart % size == 0 && d->rows > 1 && at >= d->cols && at <= stride - d->cols ? MGRIT_OK : MGRIT_INVALID_ARG;
 }
 LogitsArgs logits_args(const mgrit_logits_desc* d, const void* logits, int64_t stride) {
   LogitsArgs a = {};
@@ -199,9 +207,9 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
   return enqueued(launch_q8_grad(a, dy_dtype == MGRIT_DTYPE_BF16, static_cast<float*>(workspace), static_cast<hipStream_t>(stream)));
 }
 
-size_t mgrit_token_logprobs_workspace_bytes(const mgrit_logits_desc* desc, int32_t top_k) {
+size_t mgrit_token_logprobs_workspace_bytes(const mgrit_logits_desc* desc, int32_t top_k, int step) {
   if (check_logits(desc) != MGRIT_OK || check_top(desc, top_k) != MGRIT_OK) return 0;
-  return logits_workspace_bytes(desc->rows, desc->cols, desc->dtype == MGRIT_DTYPE_BF16, top_k, 1);
+  return logits_workspace_bytes(desc->rows, desc->cols, desc->dtype == MGRIT_DTYPE_BF16, step ? 0 : top_k, 1, step != 0);
 }
 
 int mgrit_token_logprobs_forward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const void* tokens, float* logprob,
@@ -219,7 +227,7 @@ int mgrit_token_logprobs_forward(const mgrit_logits_desc* desc, const void* logi
     STCHK(check_floats(desc, top_logprobs));
     if (desc->rows && (top_ids == top_logprobs || top_ids == tokens || top_logprobs == logprob || top_logprobs == entropy || top_logprobs == lse)) return MGRIT_INVALID_ARG;
   }
-  STCHK(check_workspace(mgrit_token_logprobs_workspace_bytes(desc, top_k), workspace, workspace_bytes));
+  STCHK(check_workspace(mgrit_token_logprobs_workspace_bytes(desc, top_k, 0), workspace, workspace_bytes));
   LogitsArgs a = logits_args(desc, logits, stride);
   a.tokens = tokens; a.logprob = logprob; a.entropy = entropy; a.lse = lse; a.top_k = top_k; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
   return enqueue_logits(desc, a, 0, workspace, stream);
@@ -253,15 +261,15 @@ int mgrit_token_logprobs_step(const mgrit_logits_desc* desc, const void* logits,
   if (!aligned(g_entropy, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4)) return MGRIT_INVALID_ARG;
   if ((logprob && (logprob == entropy || logprob == lse)) || (entropy && entropy == lse)) return MGRIT_INVALID_ARG;
   STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
-  STCHK(check_workspace(mgrit_token_logprobs_workspace_bytes(desc, 0), workspace, workspace_bytes));
+  STCHK(check_workspace(mgrit_token_logprobs_workspace_bytes(desc, 0, 1), workspace, workspace_bytes));
   LogitsArgs a = logits_args(desc, logits, stride);
   a.tokens = tokens; a.logprob = logprob; a.entropy = entropy; a.lse = lse; a.g = g_logprob; a.h = g_entropy; a.dz = dlogits; a.lddz = dlogits_stride;
   return enqueue_logits(desc, a, 0, workspace, stream);
 }
 
-size_t mgrit_distill_workspace_bytes(const mgrit_logits_desc* desc, int32_t kept) {
+size_t mgrit_distill_workspace_bytes(const mgrit_logits_desc* desc, int32_t kept, int step) {
   if (check_logits(desc) != MGRIT_OK || check_kept(kept) != MGRIT_OK) return 0;
-  return logits_workspace_bytes(desc->rows, desc->cols, desc->dtype == MGRIT_DTYPE_BF16, 0, kept);
+  return logits_workspace_bytes(desc->rows, desc->cols, desc->dtype == MGRIT_DTYPE_BF16, 0, kept, step != 0);
 }
 
 int mgrit_distill_forward(const mgrit_logits_desc* desc, const void* logits, int64_t stride, const mgrit_teacher* teacher, float* loss,
@@ -271,7 +279,7 @@ int mgrit_distill_forward(const mgrit_logits_desc* desc, const void* logits, int
   STCHK(check_teacher(desc, teacher));
   STCHK(check_floats(desc, loss));
   if (!aligned(lse, 4) || (desc->rows && loss == lse)) return MGRIT_INVALID_ARG;
-  STCHK(check_workspace(mgrit_distill_workspace_bytes(desc, teacher->kept), workspace, workspace_bytes));
+  STCHK(check_workspace(mgrit_distill_workspace_bytes(desc, teacher->kept, 0), workspace, workspace_bytes));
   LogitsArgs a = logits_args(desc, logits, stride);
   add_teacher(a, teacher);
   a.loss = loss; a.lse = lse;
@@ -300,7 +308,7 @@ int mgrit_distill_step(const mgrit_logits_desc* desc, const void* logits, int64_
   STCHK(check_floats(desc, loss));
   if (!aligned(g_loss, 4) || !aligned(lse, 4) || (desc->rows && loss == lse)) return MGRIT_INVALID_ARG;
   STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
-  STCHK(check_workspace(mgrit_distill_workspace_bytes(desc, teacher->kept), workspace, workspace_bytes));
+  STCHK(check_workspace(mgrit_distill_workspace_bytes(desc, teacher->kept, 1), workspace, workspace_bytes));
   LogitsArgs a = logits_args(desc, logits, stride);
   add_teacher(a, teacher);
   a.loss = loss; a.lse = lse; a.g = g_loss; a.dz = dlogits; a.lddz = dlogits_stride;

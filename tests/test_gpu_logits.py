@@ -558,6 +558,102 @@ def test_given_results_and_leading_dimensions():
     assert only.logprob is None and torch.equal(only.top_ids, ref[3])
 
 
+def test_gradients_in_the_logits_own_rows():
+    """Logits and gradient as slices of the same wider rows, and one behind the other."""
+    say("slices of the same rows")
+    for rows, cols, dtype in ((5, 1000, BF16), (3, 3001, F32), (2, 50257, BF16)):
+        z, t, g, h, ids, y = operands(rows, cols, dtype)
+        big = torch.full((rows, 2 * cols + 8), NAN, dtype=dtype, device="cuda")
+        left, right = big[:, :cols], big[:, cols + 8:]
+        left.copy_(z)
+        lse = mb.mgrit_token_logprobs_forward(left, t).lse
+        mb.mgrit_token_logprobs_backward(left, t, lse, g, dlogits=right)
+        assert torch.equal(right, mb.mgrit_token_logprobs_backward(left, t, lse, g)) and torch.isnan(big[:, cols:cols + 8]).all()
+        mb.mgrit_distill_step(left, ids, y, g, dlogits=right)
+        assert torch.equal(right, mb.mgrit_distill_step(left, ids, y, g)[2]) and torch.equal(left, z)
+        right.copy_(z)
+        mb.mgrit_distill_backward(right, ids, y, lse, g, dlogits=left)
+        assert torch.equal(left, mb.mgrit_distill_backward(right, ids, y, lse, g)) and torch.equal(right, z)
+        pair = torch.stack([z, z])
+        mb.mgrit_token_logprobs_step(pair[0], t, g, dlogits=pair[1])
+        assert torch.equal(pair[1], mb.mgrit_token_logprobs_step(pair[0], t, g)[1])
+        with pytest.raises(mb.MgritError):
+            mb.mgrit_token_logprobs_backward(left, t, lse, g, dlogits=big[:, 1:cols + 1])
+
+
+@pytest.mark.parametrize("cols,dtype", [(200001, BF16), (131073, BF16), (65537, F32), (262145, F32)])
+def test_steps_of_rows_that_no_block_holds(cols, dtype):
+    """The rows' sums in a launch of their own, the gradient in another; in place as well."""
+    say("wide steps", cols, dtype)
+    for rows in (1, 3, 520):
+        if rows > 3 and dtype is F32 and cols > 200000:
+            continue
+        some = min(rows, 3)
+        z, tokens = logits(rows, some, cols, dtype), some_tokens(rows + 1, some, cols)
+        g, h, ids, y = floats(1, some), floats(2, some, spread=0.3), lists(3, some, cols, 30), floats(4, some, 30)
+        g[torch.from_numpy(tokens < 0).cuda()] = 0.0
+        times = rows // some
+        many, t = z.repeat(times, 1), ids_of(np.tile(tokens, times))
+        b, gs, hs = Bounds(n64(z), 1.0), n64(g), n64(h)
+        weights = np.zeros(z.shape)
+        weights[np.arange(some), np.clip(tokens, 0, None)] = tokens >= 0
+        ref = ol.logprobs_gradient(n64(z), tokens, gs, hs)
+        bound = b.gradient(ref, dtype, False, np.abs(gs), (tokens >= 0).astype(float), weights, hs, b.entropy)
+        lp, _, _ = ol.logprobs(n64(z), tokens)
+        q = ol.teacher(ids, n64(y), 1.0, None, cols)
+        rel, e_loss = distill_bounds(b, ids, q, n64(y), 1.0, False)
+        loss_ref, _ = ol.distill(n64(z), ids, n64(y))
+        d_ref = ol.distill_gradient(n64(z), ids, n64(y), gs)
+        weights, wrel = np.zeros(z.shape), np.zeros(z.shape)
+        for r in range(some):
+            for j in np.flatnonzero(q[r] > 0):
+                weights[r, ids[r, j]] += q[r, j]
+                wrel[r, ids[r, j]] += q[r, j] * (rel[r, j] + 40 * U)
+        d_bound = b.gradient(d_ref, dtype, False, np.abs(gs), q.sum(1), weights)
+        d_bound = d_bound + 1.02 * np.abs(gs)[:, None] * (b.p * ((q * rel).sum(1) + 12 * U * q.sum(1))[:, None] + wrel)
+        for inplace in (False, True):
+            own = many.clone()
+            r, d = mb.mgrit_token_logprobs_step(own, t, g.repeat(times), h.repeat(times), dlogits=own if inplace else None)
+            for i in {0, times - 1}:
+                at = slice(i * some, (i + 1) * some)
+                close(d[at], ref, bound, "gradient")
+                close(r.lse[at], b.lse, b.lse_bound(), "lse")
+                close(r.logprob[at], lp, b.lp_bound(np.clip(tokens, 0, None)[:, None])[:, 0], "logprob")
+            own = many.clone()
+            loss, lse, d = mb.mgrit_distill_step(own, ids_of(ids).repeat(times, 1), y.repeat(times, 1), g.repeat(times), dlogits=own if inplace else None)
+            for i in {0, times - 1}:
+                at = slice(i * some, (i + 1) * some)
+                close(d[at], d_ref, d_bound, "distillation's gradient")
+                close(loss[at], loss_ref, e_loss, "loss")
+                close(lse[at], b.lse, b.lse_bound(), "lse")
+
+
+@pytest.mark.parametrize("cols", [9000, 20000, 30000, 40000, 60000, 100000, 130000])
+def test_steps_of_every_block(cols):
+    """Rows in the registers of 4, 8 or 16 wavefronts, few and many of them, also where the last vectors are full or nearly so."""
+    say("steps by block", cols)
+    for dtype in (BF16, F32):
+        if dtype is F32 and cols > 65536:
+            continue
+        for rows, c in ((2, cols), (520, cols), (2, cols // 512 * 512 + 7), (515, cols // 512 * 512)):
+            z, tokens = logits(cols, 2, c, dtype), np.array([c - 1, 5])
+            g = floats(1, 2)
+            times = (rows + 1) // 2
+            many, t = z.repeat(times, 1)[:rows], ids_of(np.tile(tokens, times)[:rows])
+            b, gs = Bounds(n64(z), 1.0), n64(g)
+            weights = np.zeros(z.shape)
+            weights[np.arange(2), tokens] = 1.0
+            ref = ol.logprobs_gradient(n64(z), tokens, gs)
+            bound = b.gradient(ref, dtype, False, np.abs(gs), np.ones(2), weights)
+            r, d = mb.mgrit_token_logprobs_step(many, t, g.repeat(times)[:rows])
+            lp, _, _ = ol.logprobs(n64(z), tokens)
+            for i in (0, rows // 2 - 1):
+                close(d[2 * i:2 * i + 2], ref, bound, "gradient")
+                close(r.logprob[2 * i:2 * i + 2], lp, b.lp_bound(tokens[:, None])[:, 0], "logprob")
+            if c % 8 == 0:                                 # (every row has the same place in its vectors)
+                assert torch.equal(d[0::2], d[:1].expand((rows + 1) // 2, -1)) and torch.equal(d[1::2], d[1:2].expand(rows // 2, -1))
+
+
 def test_no_rows():
     say("no rows")
     for dtype in (F32, BF16):

@@ -63,7 +63,7 @@ def test_descriptions_and_logits(call):
         assert call(dz=P, ldd=48) == INVALID                                           # in place at another place
     L = mb.lib()
     null = C.POINTER(mb.LogitsDesc)()
-    assert L.mgrit_token_logprobs_workspace_bytes(null, 0) == 0 and L.mgrit_distill_workspace_bytes(null, 1) == 0
+    assert L.mgrit_token_logprobs_workspace_bytes(null, 0, 0) == 0 and L.mgrit_distill_workspace_bytes(null, 1, 1) == 0
 
 
 def test_forward_refusals():
@@ -105,24 +105,45 @@ def test_distill_refusals():
 
 
 def test_workspaces():
-    one = desc(rows=1, cols=50257, dtype=1)
-    need = mb.mgrit_token_logprobs_workspace_bytes(1, 50257, torch.bfloat16, 20)
+    bf16, f32 = torch.bfloat16, torch.float32
+    one, wide = desc(rows=1, cols=50257, dtype=1), desc(rows=4, cols=200001, dtype=1)
     top = dict(k=20, ids=6 * P, top=7 * P)
-    assert need > 0
+    need = mb.mgrit_token_logprobs_workspace_bytes(1, 50257, bf16, 20)
+    assert need > mb.mgrit_token_logprobs_workspace_bytes(1, 50257, bf16) > 0
     assert forward(one, ld=50257, ws=8 * P, n=need - 1, **top) == SMALL
     assert forward(one, ld=50257, ws=None, n=need, **top) == INVALID and forward(one, ld=50257, ws=8 * P + 128, n=need, **top) == INVALID
-    need = mb.mgrit_token_logprobs_workspace_bytes(1, 50257, torch.bfloat16)
-    assert need > 0 and step(one, ld=50257, ldd=50257, ws=8 * P, n=need - 1) == SMALL and step(one, ld=50257, ldd=50257) == INVALID
-    need = mb.mgrit_distill_workspace_bytes(1, 50257, torch.bfloat16, 3)
-    assert need > 0 and d_forward(one, ld=50257, ws=8 * P, n=need - 1) == SMALL and d_step(one, ld=50257, ldd=50257) == INVALID
+    need = mb.mgrit_distill_workspace_bytes(1, 50257, bf16, 3)
+    assert need > 0 and d_forward(one, ld=50257, ws=8 * P, n=need - 1) == SMALL and d_forward(one, ld=50257) == INVALID
+    # a step needs one for rows that no block holds
+    assert mb.mgrit_token_logprobs_workspace_bytes(4, 131072, bf16, step=True) == 0 == mb.mgrit_distill_workspace_bytes(9000, 65536, f32, 3, step=True)
+    need = mb.mgrit_token_logprobs_workspace_bytes(4, 200001, bf16, step=True)
+    assert need > 0 and step(wide, ld=200001, ldd=200001, ws=8 * P, n=need - 1) == SMALL and step(wide, ld=200001, ldd=200001) == INVALID
+    need = mb.mgrit_distill_workspace_bytes(4, 200001, bf16, 3, step=True)
+    assert need > 0 and d_step(wide, ld=200001, ldd=200001, ws=8 * P, n=need - 1) == SMALL and d_step(wide, ld=200001, ldd=200001) == INVALID
+    assert mb.mgrit_token_logprobs_workspace_bytes(9000, 65537, f32, step=True) > 0
     L = mb.lib()
     for kw, _ in BAD_DESCS:
-        assert L.mgrit_token_logprobs_workspace_bytes(desc(**kw), 0) == 0 and L.mgrit_distill_workspace_bytes(desc(**kw), 3) == 0
-    assert L.mgrit_token_logprobs_workspace_bytes(one, 65) == 0 and L.mgrit_distill_workspace_bytes(one, 257) == 0
-    assert mb.mgrit_token_logprobs_workspace_bytes(4096, 50257, torch.bfloat16, 20) == 0            # many rows need none
-    assert mb.mgrit_token_logprobs_workspace_bytes(0, 50257, torch.bfloat16, 20) == 0
+        for s in (0, 1):
+            assert L.mgrit_token_logprobs_workspace_bytes(desc(**kw), 0, s) == 0 and L.mgrit_distill_workspace_bytes(desc(**kw), 3, s) == 0
+    assert L.mgrit_token_logprobs_workspace_bytes(one, 65, 0) == 0 and L.mgrit_distill_workspace_bytes(one, 257, 0) == 0
+    assert mb.mgrit_token_logprobs_workspace_bytes(4096, 50257, bf16, 20) == 0                      # many rows need none
+    assert mb.mgrit_token_logprobs_workspace_bytes(0, 50257, bf16, 20) == 0 == mb.mgrit_token_logprobs_workspace_bytes(0, 200001, bf16, step=True)
     with pytest.raises(ValueError, match="2\\^31 - 1"):
-        mb.mgrit_token_logprobs_workspace_bytes(4, (1 << 32) + 40, torch.float32)
+        mb.mgrit_token_logprobs_workspace_bytes(4, (1 << 32) + 40, f32)
+
+
+@pytest.mark.parametrize("offset,ldd", [(39, 100), (61, 100), (1, 100), (-39, 100), (139, 100), (339, 100), (40, 101), (0, 101), (-300, 111)])
+def test_gradients_that_lie_across_the_logits(offset, ldd):
+    """4 rows of 40 fp32 elements at a distance of 100 (what is in order runs on the GPU)."""
+    assert backward(z=8 * P, ld=100, dz=8 * P + 4 * offset, ldd=ldd) == INVALID
+    assert step(z=8 * P, ld=100, dz=8 * P + 4 * offset, ldd=ldd) == INVALID
+    assert d_backward(z=8 * P, ld=100, dz=8 * P + 4 * offset, ldd=ldd) == INVALID and d_step(z=8 * P, ld=100, dz=8 * P + 4 * offset, ldd=ldd) == INVALID
+
+
+def test_gradients_that_lie_across_a_single_row():
+    one = desc(rows=1)
+    assert backward(one, z=8 * P, dz=8 * P + 4 * 39) == INVALID and backward(one, z=8 * P, dz=8 * P - 4 * 39) == INVALID
+    assert backward(desc(dtype=1), z=8 * P, ld=100, dz=8 * P + 2 * 39, ldd=100) == INVALID and backward(desc(dtype=1), z=8 * P, ld=100, dz=8 * P + 2 * 61, ldd=100) == INVALID
 
 
 def test_binding_refuses_what_the_library_cannot_see():
