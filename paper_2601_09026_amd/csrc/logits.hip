@@ -248,7 +248,7 @@ struct Top {
     if (n > LIST - WAVE) settle();
   }
   // the elements of the lane's vectors that reach the bar: those of vector u where inside(u), index(u) the first's
-  template <typename T, int COUNT, typename F, typename G> __device__ __forceinline__ void take_high(const u32x4 (&raw)[COUNT], float bar, F inside, G index) {
+  template <typename T, int COUNT, typename F, typename G> __device__ __forceinline__ void take_high(const u32x4* raw, float bar, F inside, G index) {
     constexpr int N = vec<T>();
     static_assert(COUNT * N <= 32, "a bit each");
     unsigned high = 0;
@@ -407,7 +407,7 @@ template <typename T> __device__ __forceinline__ void pick(const Run<T>& r, int 
         const int v = v0 + u * team;
         raw[u] = ld_global(reinterpret_cast<const u32x4*>(r.p + r.vec_at(hit && v < r.vecs ? v : 0)));
       }
-      top.template take_high<T>(raw, bar, [&](int u) { return hit && v0 + u * team < r.vecs; }, [&](int u) { return index + r.vec_at(v0 + u * team); });
+      top.template take_high<T, STEP>(raw, bar, [&](int u) { return hit && v0 + u * team < r.vecs; }, [&](int u) { return index + r.vec_at(v0 + u * team); });
     }
     hit &= hit - 1;
   }
@@ -775,7 +775,8 @@ template <typename T> __device__ __forceinline__ void write_left_out(const Run<T
 }
 
 // FROM: where a row's sums come from.  GIVEN: its log-sum-exp (and entropy) are arguments; PARTS: they lie in the workspace, and the
-// rows' values are written as well.  A block (W = 4) writes a run of a row, a wavefront (W = 1) a whole short one.  dz may be z
+// rows' values are written as well.  A block (W = 4) writes a run of a row, a wavefront (W = 1) a whole short one, STEP
+// vectors per lane.  dz may be z
 // itself: what is needed of other runs lies in the workspace.
 enum { GIVEN = 0, PARTS = 1 };
 template <typename T, int W, bool ENTROPY, int MODE, int FROM>
@@ -801,15 +802,14 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
     else wave_sync();
   };
   u32x4 raw[STEP];
-  auto load = [&](int v0) {
+  if (in.vecs) {
 #pragma unroll
     for (int u = 0; u < STEP; ++u) {
-      const int v = v0 + u * team + lane;
+      const int v = u * team + lane;
       const u32x4* at = reinterpret_cast<const u32x4*>(in.p + in.vec_at(v < in.vecs ? v : in.vecs - 1));
       raw[u] = MODE == 0 ? ld_stream(at) : ld_global(at);
     }
-  };
-  if (in.vecs) load(0);
+  }
   Points<MODE> pt;
   Marked marked = {0, false};
   unsigned skip = 0;
@@ -842,19 +842,15 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
     }
   }
   const int token = MODE == 0 && pt.id[0] >= 0 && !s.zero ? pt.id[0] - from : -1;
-  for (int v0 = 0, chunk = 0; v0 < in.vecs; ++chunk) {
 #pragma unroll
-    for (int u = 0; u < STEP; ++u) {
-      const int v = v0 + u * team + lane;
-      if (v < in.vecs) {
-        float x[N];
-        decode<T>(raw[u], x);
-        slope_vector<T, ENTROPY>(x, s, MODE == 0 && token >= 0 ? token - in.vec_at(v) : -1);
-        if (MODE == 0 || !(skip >> (chunk * STEP + u) & 1)) put_vector<T>(out + in.vec_at(v), x, MODE == 0 && a.stream);
-      }
+  for (int u = 0; u < STEP; ++u) {
+    const int v = u * team + lane;
+    if (v < in.vecs) {
+      float x[N];
+      decode<T>(raw[u], x);
+      slope_vector<T, ENTROPY>(x, s, MODE == 0 && token >= 0 ? token - in.vec_at(v) : -1);
+      if (MODE == 0 || !(skip >> u & 1)) put_vector<T>(out + in.vec_at(v), x, MODE == 0 && a.stream);
     }
-    v0 += STEP * team;
-    if (v0 < in.vecs) load(v0);
   }
   if (lane < in.odd && !(skip >> ODD_BIT)) {
     const int at = in.odd_at(lane);
@@ -870,9 +866,8 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
 template <typename T, int NW, int RV, bool ENTROPY, int MODE, int OCC, bool GRAD, bool TOP>
 __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_step_kernel(const LogitsArgs a) {
   static_assert(NW == 1 || (GRAD && !TOP), "longer rows have kernels of their own for values");
-  __shared__ u64 lists[TOP ? WAVES * ROOM : 1];
-  Top best;
   constexpr int N = vec<T>(), team = NW * WAVE, TEAMS = NW == 1 ? WAVES : 1;
+  __shared__ u64 lists[TOP ? WAVES * ROOM : 1];
   __shared__ float tops[TEAMS * NW];
   __shared__ f32x2 waves[TEAMS * NW];
   __shared__ unsigned left_out[MODE == 1 && GRAD ? TEAMS * team : 1];
@@ -935,12 +930,17 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
 #pragma unroll
       for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
     });
+    Top best;
     if constexpr (TOP) {
       best.start(lists, nullptr, a.top_k);
       best.best = top;
       const float bar = Top::bar_of(best.reached(a.top_k));
       best.take(lane < r.odd && odd >= bar, candidate(odd, r.odd_at(lane)));
-      best.template take_high<T>(raw, bar, [&](int u) { return u * team + lane < r.vecs; }, [&](int u) { return r.vec_at(u * team + lane); });
+      constexpr int PART = RV < 4 ? RV : 4;
+#pragma unroll
+      for (int u0 = 0; u0 < RV; u0 += PART)
+        if (u0 * team < r.vecs)
+          best.template take_high<T, PART>(raw + u0, bar, [&](int u) { return (u0 + u) * team + lane < r.vecs; }, [&](int u) { return r.vec_at((u0 + u) * team + lane); });
       best.finish();
       if (best.n < best.k) best.fill(0, a.cols);
     }
@@ -951,9 +951,30 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
       top = all_max<NW>(tops[l % NW]);
     }
     top = fmaxf(top, LOWEST);
+    // The token's logit, from the lane that holds it
+    float z_token = 0.f;
+    bool owner = false;
+    if (MODE == 0 && pt.id[0] >= 0) {
+      const int from_head = pt.id[0] - r.head, v = from_head / N;
+      if (pt.id[0] < r.head || v >= r.vecs) {
+        owner = lane < r.odd && r.odd_at(lane) == pt.id[0];
+        z_token = odd;
+      } else {
+        u32x4 held = {0, 0, 0, 0};
+#pragma unroll
+        for (int u = 0; u < RV; ++u)
+          if (u == v / team) held = raw[u];              // (the same u for all lanes)
+        float x[N];
+        decode<T>(held, x);
+        z_token = x[0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) z_token = j == from_head - v * N ? x[j] : z_token;
+        owner = lane == v % team;
+      }
+    }
     // Exponents are x c - P as in Reader; `rest` is the part of each that P leaves out.  Where |P| is too large for that the
     // row's values become their differences to the maximum, which then is 0: those that matter are exact.
-    float base = top, P = top * c;
+    float base = top, P = top * c, x_token = z_token;
     if (!(fabsf(P) < 0x1p20f)) {
 #pragma unroll
       for (int u = 0; u < RV; ++u)
@@ -965,6 +986,7 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
           raw[u] = encode<T>(x);
         }
       odd -= top;
+      x_token -= top;
       base = P = 0.f;
     }
     const float rest = fmaf(base, c, -P);
@@ -1007,40 +1029,15 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
     slope.zero = false;
     if constexpr (GRAD) slope.template set<ENTROPY>(a, row, weight, MODE == 0 ? 1.f : -1.f, sums.entropy);
     slope.from_sums(sums);
-    const int token = MODE == 0 && pt.id[0] >= 0 && !slope.zero ? pt.id[0] : -1;
-    if (wave == 0) {
-      // (a loss comes last; a token's log probability from the lane that holds its logit)
-      if (l == 0) {
-        if (a.lse) a.lse[row] = sums.lse;
-        if (MODE == 0 && a.entropy) a.entropy[row] = sums.entropy;
-        if (MODE == 0 && a.logprob && token < 0) a.logprob[row] = pt.mass == 1.f ? (sums.none ? -__builtin_inff() : __builtin_nanf("")) : pt.mass;
-      }
+    if (wave == 0 && l == 0) {                           // (a loss comes last)
+      if (a.lse) a.lse[row] = sums.lse;
+      if (MODE == 0 && a.entropy) a.entropy[row] = sums.entropy;
+      if (MODE == 0 && a.logprob && pt.id[0] < 0) a.logprob[row] = pt.mass;
     }
-    // The token's logit, from the lane that holds it, which writes its element once more behind all others
-    float z_token = 0.f;
-    bool owner = false;
-    if (MODE == 0 && token >= 0) {
-      const int from_head = token - r.head, v = from_head / N;
-      if (token < r.head || v >= r.vecs) {
-        owner = lane < r.odd && r.odd_at(lane) == token;
-        z_token = odd;
-      } else {
-        u32x4 held = {0, 0, 0, 0};
-#pragma unroll
-        for (int u = 0; u < RV; ++u)
-          if (u == v / team) held = raw[u];              // (the same u for all lanes)
-        float x[N];
-        decode<T>(held, x);
-        z_token = x[0];
-#pragma unroll
-        for (int j = 1; j < N; ++j) z_token = j == from_head - v * N ? x[j] : z_token;
-        owner = lane == v % team;
-      }
-    }
+    if (owner && a.logprob) a.logprob[row] = sums.logprob(z_token, a.tau);
     const bool more = row + stride < a.rows;
     const Run<T> next(z, (more ? row + stride : row) * a.ld, a.cols);
     if constexpr (!GRAD) {
-      if (owner && a.logprob) a.logprob[row] = sums.bad ? __builtin_nanf("") : (z_token - base) / a.tau - sums.log_s;
       if (MODE == 1) put_values<MODE>(a, row, sums, pt);
       if constexpr (TOP) put_alternatives(a, row, sums, best.list);
 #pragma unroll
@@ -1080,10 +1077,7 @@ __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_ste
       }
       if (more) load(next, u);
     }
-    if (owner) {
-      out[token] = from_f<T>(gradient(z_token) + slope.slope);
-      if (a.logprob) a.logprob[row] = sums.bad ? __builtin_nanf("") : (z_token - base) / a.tau - sums.log_s;
-    }
+    if (owner && !slope.zero) out[pt.id[0]] = from_f<T>(gradient(x_token) + slope.slope);    // (once more, behind its vector)
     if (more) load_odd(next);
     if constexpr (MODE == 1) {
       if (wave == 0) {
@@ -1105,8 +1099,8 @@ dim3 blocks_for(long tasks, int teams) {
   const long b = (tasks + teams - 1) / teams;
   return b <= MOST_BLOCKS ? dim3((unsigned)b) : dim3((unsigned)MOST_BLOCKS, (unsigned)((b + MOST_BLOCKS - 1) / MOST_BLOCKS));
 }
-// short rows: one wavefront each
-bool short_rows(int cols, bool is_bf16) { return cols <= (is_bf16 ? 2048 : 1024); }
+// short rows: one wavefront each, which holds them
+bool short_rows(int cols, bool is_bf16) { return cols <= (is_bf16 ? 4096 : 2048); }
 // Few rows: a row's elements are shared out over several blocks, with a join behind them, from 64 KB on (1 x 16000 bf16, 20
 // alternatives: 8.3 us whole, 11.7 in three parts; 1 x 50257: 12 in 12 parts, 20 in one), into no less than 8 KB, and
 // so that there are no more than two blocks per CU (300 x 50257: 18.5 us whole, 26.6 in six parts); 128 KB a part
@@ -1167,6 +1161,7 @@ template <typename T, int MODE> hipError_t step(const LogitsArgs& a, hipStream_t
   const bool few = a.rows <= 2 * compute_units();
   if (vecs <= WAVE) return step_of<T, MODE, 1, 1, 6>(a, st);
   if (vecs <= 4 * WAVE) return step_of<T, MODE, 1, 4, 5>(a, st);
+  if (vecs <= 8 * WAVE && (!few || !a.dz)) return step_of<T, MODE, 1, 8, MODE == 0 ? 5 : 4>(a, st);
   if (vecs <= 4 * 4 * WAVE) return step_of<T, MODE, 4, 4, 5>(a, st);
   if (vecs <= 4 * 8 * WAVE && !few) return step_of<T, MODE, 4, 8, 4>(a, st);
   if (vecs <= 4 * 16 * WAVE && !few) return step_of<T, MODE, 4, 16, 4>(a, st);
@@ -1176,22 +1171,20 @@ template <typename T, int MODE> hipError_t step(const LogitsArgs& a, hipStream_t
   return step_of<T, MODE, 16, 16, 4>(a, st);
 }
 
-template <typename T, int W, int MODE> hipError_t launch(LogitsArgs a, bool resident, hipStream_t st) {
-  constexpr int TILE = THREADS * STEP * vec<T>();
-  if (resident || (W == 1 && !a.dz)) return step<T, MODE>(a, st);
+template <typename T, int MODE> hipError_t launch(LogitsArgs a, bool resident, hipStream_t st) {
+  constexpr int LANE_TILE = STEP * vec<T>();             // elements that a lane loads together
+  if (resident) return step<T, MODE>(a, st);
   if (!a.dz) return values<T, MODE>(a, st);
-  a.runs = 1;
-  a.run_cols = a.cols;
-  if (W > 1) {
-    a.run_cols = TILE;
-    a.runs = (a.cols + TILE - 1) / TILE;
+  if (a.lse_in && a.cols <= WAVE * LANE_TILE) {
+    a.runs = 1;
+    a.run_cols = a.cols;
+    return gradient<T, 1, MODE, GIVEN>(a, st);
   }
-  if (a.lse_in) return gradient<T, W, MODE, GIVEN>(a, st);
-  if constexpr (W > 1) {                                 // (short rows fit)
-    const hipError_t e = values<T, MODE>(a, st);
-    return e != hipSuccess ? e : gradient<T, W, MODE, PARTS>(a, st);
-  }
-  return hipErrorInvalidValue;
+  a.run_cols = THREADS * LANE_TILE;
+  a.runs = (a.cols + a.run_cols - 1) / a.run_cols;
+  if (a.lse_in) return gradient<T, WAVES, MODE, GIVEN>(a, st);
+  const hipError_t e = values<T, MODE>(a, st);
+  return e != hipSuccess ? e : gradient<T, WAVES, MODE, PARTS>(a, st);
 }
 
 }  // namespace
@@ -1206,7 +1199,7 @@ hipError_t launch_logits(LogitsArgs a, int mode, bool is_bf16, void* workspace, 
   if (a.rows == 0) return hipSuccess;
   const double elems = (double)a.rows * a.cols, size = is_bf16 ? 2 : 4;
   ProfScope ps(a.lse_in ? PC_LOGITS_GRAD : a.dz ? PC_LOGITS_STEP : PC_LOGITS, elems * (a.dz && !a.lse_in ? 10 : 6), elems * size * (a.dz ? 2 : 1), st);
-  const bool stepping = a.dz && !a.lse_in, resident = stepping && fits(a.cols, is_bf16);
+  const bool stepping = a.dz && !a.lse_in, resident = stepping ? fits(a.cols, is_bf16) : !a.lse_in && short_rows(a.cols, is_bf16);
   a.parts = a.lse_in || resident ? 1 : parts_of(a.rows, a.cols, is_bf16);
   a.part_cols = a.cols;
   a.points = mode == 0 ? 1 : a.kept;
@@ -1225,10 +1218,7 @@ hipError_t launch_logits(LogitsArgs a, int mode, bool is_bf16, void* workspace, 
   }
   return with(is_bf16, [&](auto b) {
     typedef typename std::conditional<decltype(b)::value, bf16, float>::type T;
-    return with(short_rows(a.cols, is_bf16), [&](auto s) {
-      constexpr int W = decltype(s)::value ? 1 : WAVES;
-      return with(mode == 0, [&](auto m) { return launch<T, W, decltype(m)::value ? 0 : 1>(a, resident, st); });
-    });
+    return with(mode == 0, [&](auto m) { return launch<T, decltype(m)::value ? 0 : 1>(a, resident, st); });
   });
 }
 

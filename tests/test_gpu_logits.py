@@ -283,6 +283,52 @@ def test_values_of_the_types_range(cols):
             assert np.isfinite(lse[ok]).all() and np.isfinite(H[ok]).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [40, 1000, 3000, 9000, 50257, 200001])
+def test_sharp_and_shifted_rows(cols, dtype):
+    """Rows whose quotients by the temperature are far beyond their differences': values and gradients as of any other."""
+    say("sharp rows", cols, dtype)
+    rows = 6
+    for tau, offset, spread in ((1e-4, 100.0, 2.0), (1.0, 3e5, 200.0), (1e-4, -3e5, 0.05), (0.01, 0.0, 1e5), (1e4, 1e8, 1e5), (1.0, -3e30, 1e24)):
+        z = (floats(cols, rows, cols) * spread + offset).to(dtype)
+        z[:, 2] = z[:, 1]
+        z[1, 3] = z[1].max()
+        z[2, ::2] = -INF
+        tokens = np.array([0, 3, 1, cols - 1, 2, -1])
+        tokens[3] = int(z[3].float().argmax())
+        b, g = Bounds(n64(z), tau), floats(1, rows)
+        times = 1 if cols > 60000 else 90
+        many, t = z.repeat(times, 1), ids_of(np.tile(tokens, times))
+        lp, H, lse = ol.logprobs(n64(z), tokens, tau)
+        ref = ol.logprobs_gradient(n64(z), tokens, np.where(tokens >= 0, n64(g), 0.0), None, tau)
+        weights = np.zeros(z.shape)
+        weights[np.arange(rows), np.clip(tokens, 0, None)] = tokens >= 0
+        bound = b.gradient(ref, dtype, False, np.abs(n64(g)) * (tokens >= 0) / tau, (tokens >= 0).astype(float), weights)
+        lp_bound = b.lp_bound(np.clip(tokens, 0, None)[:, None])[:, 0]
+        for zz, tt in ((z, ids_of(tokens)), (many, t)):
+            n = len(zz) // rows
+            r = mb.mgrit_token_logprobs_forward(zz, tt, top_k=2, temperature=tau)
+            s, d = mb.mgrit_token_logprobs_step(zz, tt, g.repeat(n), temperature=tau)
+            for x in (r, s):
+                for i in (0, n - 1):
+                    at = slice(i * rows, (i + 1) * rows)
+                    close(x.logprob[at], lp, lp_bound, "logprob")
+                    close(x.lse[at], lse, b.lse_bound(), "lse")
+                    close(x.entropy[at], H, b.entropy_bound(), "entropy")
+            close(d[:rows], ref, bound, "gradient")
+            close(d[-rows:], ref, bound, "gradient")
+            assert np.array_equal(r.top_ids[:rows].cpu().numpy(), ol.largest(n64(z), 2))
+        ids, y = np.stack([tokens.clip(0), np.ones(rows, int)], 1), floats(5, rows, 2) * tau
+        q = ol.teacher(ids, n64(y), tau, None, cols)
+        rel, e_loss = distill_bounds(b, ids, q, n64(y), tau, False)
+        loss_ref, _ = ol.distill(n64(z), ids, n64(y), tau)
+        for zz in (z, many):
+            n = len(zz) // rows
+            args = (zz, ids_of(ids).repeat(n, 1), y.repeat(n, 1))
+            for loss in (mb.mgrit_distill_forward(*args, temperature=tau)[0], mb.mgrit_distill_step(*args, temperature=tau)[0]):
+                close(loss[:rows], loss_ref, e_loss, "loss")
+
+
 # ------------------------------------------------------------------ gradients of log probabilities
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("cols", WIDTHS + [50257])
