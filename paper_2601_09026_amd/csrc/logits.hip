@@ -3,7 +3,16 @@
 //   p = softmax(z / tau),  lse = log sum exp(z / tau),  H = lse - sum p z / tau
 //   log p_i = z_i / tau - lse,  dz_i = 1 / tau (g ([i = token] - p_i) - h p_i (log p_i + H))
 //   L = sum_j q_j (log q_j - log p_id(j)),  dz_i = g / tau (Q p_i - sum_{j: id(j) = i} q_j),  Q = sum q
-// A row is read in 16-byte vectors from its first 16-byte address on, the elements before and behind them one by one.
+// A row is read in 16-byte vectors from its first 16-byte address on, the elements before and behind them one by one; all
+// arithmetic is fp32, sums in a tree over a lane's vectors, lanes and wavefronts, the gradient is rounded once.
+//
+// What bounds it: moving the logits, and in bf16 next to that the vector unit: an element of the values takes 8 vector
+// instructions of a lane (counted at 2048 x 131072 fp32, loop and sums included), and in bf16 twice as many elements come
+// with the same bytes.  Hence the exponents of one instruction (Reader) and sums of which nothing is rescaled as a rule.
+// Values, fp32, 2048 x 131072: 158 us, 6.8 TB/s; bf16, 4096 x 50257: 70 us, 5.9 TB/s, 81 with 5 alternatives.  Backward,
+// 4096 x 50257 bf16 with entropies: 140 us, 5.9 TB/s (a large copy reaches 5.7).  Both in one call, 8192 x 50304 bf16: 312 us, 5.3
+// TB/s over one reading and one writing; the two calls one after the other take 133 and 275.  One row of 50257 with 20
+// alternatives: 12 us in two launches.
 #include <math.h>
 
 #include <type_traits>
@@ -551,7 +560,9 @@ __device__ __forceinline__ void put_alternatives(const LogitsArgs& a, long row, 
 }
 
 // ---- values of a row --------------------------------------------------------------------
-// A block per row, or per part of it; with several parts a row's sums, lists and points go to the workspace.
+// A block per row, or per part of it; with several parts a row's sums, lists and points go to the workspace.  A task to a block and
+// no loop over them.  The alternatives were the most of it: with a list that every element is held against, 4096 x 50304 bf16
+// took 142 us with 5 and 396 with 64 (89 without any); with the second look at the few groups that matter 78 and 98 (68 without any).
 template <typename T, bool TOP, int MODE>
 __global__ void __launch_bounds__(THREADS, 6) logits_values_kernel(const LogitsArgs a) {
   __shared__ u64 lists[TOP ? WAVES * ROOM : 1];
@@ -774,6 +785,8 @@ template <typename T> __device__ __forceinline__ void write_left_out(const Run<T
   }
 }
 
+// Bound by its bytes: 4096 x 50257 bf16 with one token a row 141 us, 5.8 TB/s.  A teacher's list costs what every run's
+// wavefronts spend on looking through it: 146 us with 1 id a row, 151 with 16, 156 with 64, 192 with 200.
 // FROM: where a row's sums come from.  GIVEN: its log-sum-exp (and entropy) are arguments; PARTS: they lie in the workspace, and the
 // rows' values are written as well.  A block (W = 4) writes a run of a row, a wavefront (W = 1) a whole short one, STEP
 // vectors per lane.  dz may be z
@@ -861,7 +874,9 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
 }
 
 // ---- values and gradients of rows that fit the registers of NW wavefronts -------------------------
-// RV vectors per lane.  A row is read once; the next row's loads are issued as its registers are written.
+// RV vectors per lane.  A row is read once; the next row's loads are issued as its registers are written.  With the row's
+// sums in the workspace and the row read again, 8192 x 50304 bf16 takes 394 us, here 319; that is the way of larger rows
+// (1024 x 200000 bf16: 215 us), and of few long ones (fits()).
 // GRAD false: the values alone, of short rows (NW = 1), TOP with alternatives.
 template <typename T, int NW, int RV, bool ENTROPY, int MODE, int OCC, bool GRAD, bool TOP>
 __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_step_kernel(const LogitsArgs a) {
@@ -1101,10 +1116,10 @@ dim3 blocks_for(long tasks, int teams) {
 }
 // short rows: one wavefront each, which holds them
 bool short_rows(int cols, bool is_bf16) { return cols <= (is_bf16 ? 4096 : 2048); }
-// Few rows: a row's elements are shared out over several blocks, with a join behind them, from 64 KB on (1 x 16000 bf16, 20
-// alternatives: 8.3 us whole, 11.7 in three parts; 1 x 50257: 12 in 12 parts, 20 in one), into no less than 8 KB, and
-// so that there are no more than two blocks per CU (300 x 50257: 18.5 us whole, 26.6 in six parts); 128 KB a part
-// in any case (300 x 200000: 51 us whole, 41 in three parts).
+// Few rows: a row's elements are shared out over several blocks, with a join behind them, from 64 KB on, into no less than
+// 8 KB, at most two blocks per CU; 128 KB a part in any case.  In parts and whole: 1 x 50257 bf16 5.7 and 7.7 us, with 20
+// alternatives 11.7 and 11.8; 16 x 131072 fp32 7.3 and 27.5, with 20 17.4 and 35.7; 300 x 200000 bf16 with 20 39.5 and 50.4; the join costs
+// where a part is short and there are alternatives: 16 x 32003 fp32 with 20 14.6 and 12.4, 256 x 50257 bf16 with 20 19.0 and 16.9.
 int parts_of(long rows, int cols, bool is_bf16) {
   const long bytes = (long)cols * (is_bf16 ? 2 : 4);
   if (bytes < 65536 || rows >= 512 || rows < 1) return 1;
@@ -1114,8 +1129,14 @@ int parts_of(long rows, int cols, bool is_bf16) {
   if (parts < least) parts = least;
   return (int)(parts < MOST_PARTS ? parts : MOST_PARTS);
 }
-// rows that a step keeps in registers
-bool fits(int cols, bool is_bf16) { return cols <= (is_bf16 ? 131072 : 65536); }
+// Rows that a step keeps in registers.  Few long ones keep too few CUs at work so and go through the workspace, in parts (in
+// registers and in parts: 1 x 131072 bf16 19.3 and 7.7 us, 32 rows 21.4 and 10.4, 77 rows 24.9 and 19.2, 200 rows 30.4 and 37.2; 32 x
+// 65536 fp32 14.7 and 9.4).  Up to 128 KB a row the two are about even for few rows (32 x 50304 bf16 10.8 and 9.5, distillation 10.5 and
+// 12.0) and one launch is less than two.
+bool fits(long rows, int cols, bool is_bf16) {
+  const long bytes = (long)cols * (is_bf16 ? 2 : 4);
+  return bytes <= 262144 && (bytes <= 131072 || rows > 64);
+}
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 size_t parts_bytes(long rows, int parts, int top_k, int points) {
   return up256(rows * parts * sizeof(f32x4)) + up256(rows * parts * top_k * sizeof(u64)) + up256((size_t)rows * points * sizeof(float));
@@ -1154,8 +1175,10 @@ template <typename T, int MODE, int NW, int RV, int OCC> hipError_t step_of(cons
     return hipGetLastError();
   });
 }
-// The fewer wavefronts hold a row, the more rows a CU works on, whose loads, sums and stores overlap (8192 x 50304 bf16: 350 us
-// with 4 wavefronts, 358 with 8, 416 with 16); a row alone is done soonest by many (1 x 50304: 12.2 and 9.5 us with 4 and 16).
+// The fewer wavefronts hold a row, the more rows a CU works on, whose loads, sums and stores overlap; few rows are done
+// soonest by many (step, bf16, with few as the rule has it and the other way: 1 x 50304 9.7 and 13.6 us, 200 rows 14.8 and 18.0, 500 rows
+// 26.4 and 26.6, 600 rows 31.4 and 36.8, 1000 rows 38 and 49; 500 x 3000 5.4 and 6.6).  Wavefronts per SIMD, by a sweep: what
+// the registers of RV vectors leave room for (16384 x 3000, distillation, 4 and 5: 54 and 71 us).
 template <typename T, int MODE> hipError_t step(const LogitsArgs& a, hipStream_t st) {
   const int vecs = a.cols / vec<T>();                    // (an odd element less may make one vector less)
   const bool few = a.rows <= 2 * compute_units();
@@ -1175,6 +1198,8 @@ template <typename T, int MODE> hipError_t launch(LogitsArgs a, bool resident, h
   constexpr int LANE_TILE = STEP * vec<T>();             // elements that a lane loads together
   if (resident) return step<T, MODE>(a, st);
   if (!a.dz) return values<T, MODE>(a, st);
+  // A row of one tile to a wavefront, else a block to a run (so and with blocks: 16384 x 2000 bf16 25.8 and 33.6 us, 16384 x 1000
+  // 15.6 and 27.9, 16384 x 64 8.1 and 17.5; 64 x 1000 fp32 3.6 and 3.2).
   if (a.lse_in && a.cols <= WAVE * LANE_TILE) {
     a.runs = 1;
     a.run_cols = a.cols;
@@ -1190,7 +1215,7 @@ template <typename T, int MODE> hipError_t launch(LogitsArgs a, bool resident, h
 }  // namespace
 
 size_t logits_workspace_bytes(long rows, int cols, bool is_bf16, int top_k, int points, bool step) {
-  if (rows == 0 || (step && fits(cols, is_bf16))) return 0;
+  if (rows == 0 || (step && fits(rows, cols, is_bf16))) return 0;
   const int parts = parts_of(rows, cols, is_bf16);
   return parts > 1 || step ? parts_bytes(rows, parts, top_k, points) : 0;
 }
@@ -1199,11 +1224,13 @@ hipError_t launch_logits(LogitsArgs a, int mode, bool is_bf16, void* workspace, 
   if (a.rows == 0) return hipSuccess;
   const double elems = (double)a.rows * a.cols, size = is_bf16 ? 2 : 4;
   ProfScope ps(a.lse_in ? PC_LOGITS_GRAD : a.dz ? PC_LOGITS_STEP : PC_LOGITS, elems * (a.dz && !a.lse_in ? 10 : 6), elems * size * (a.dz ? 2 : 1), st);
-  const bool stepping = a.dz && !a.lse_in, resident = stepping ? fits(a.cols, is_bf16) : !a.lse_in && short_rows(a.cols, is_bf16);
+  const bool stepping = a.dz && !a.lse_in, resident = stepping ? fits(a.rows, a.cols, is_bf16) : !a.lse_in && short_rows(a.cols, is_bf16);
   a.parts = a.lse_in || resident ? 1 : parts_of(a.rows, a.cols, is_bf16);
   a.part_cols = a.cols;
   a.points = mode == 0 ? 1 : a.kept;
-  // Gradients that no cache could hold are written past them (measured: 4096 x 50304 with 32 kept 187 -> 172 us)
+  // Gradients that no cache could hold are written past them: past and into them 8192 x 50304 bf16 274 and 300 us backward, 314
+  // and 326 in a step, 4096 x 50304 137 and 148.  Smaller ones stay for who reads them next, at the same cost (2048 x 50304:
+  // 69.5 and 68.1 us, a step 78.3 and 73.9; 1024 x 50304: 36.9 and 38.6, 37.4 and 40.8).
   a.stream = elems * size > 256.0 * (1 << 20);
   if (a.parts > 1 || (stepping && !resident)) {
     // (whole 128-byte lines apart, but for the rows' own alignment)

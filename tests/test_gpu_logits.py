@@ -627,6 +627,47 @@ def test_gradients_in_the_logits_own_rows():
             mb.mgrit_token_logprobs_backward(left, t, lse, g, dlogits=big[:, 1:cols + 1])
 
 
+def check_steps(rows, some, cols, dtype):
+    """Both steps of `rows` rows, `some` different ones over and over, into new memory and in place, against 64 bits."""
+    z, tokens = logits(rows, some, cols, dtype), some_tokens(rows + 1, some, cols)
+    g, h, ids, y = floats(1, some), floats(2, some, spread=0.3), lists(3, some, cols, 30), floats(4, some, 30)
+    g[torch.from_numpy(tokens < 0).cuda()] = 0.0
+    times = rows // some
+    many, t = z.repeat(times, 1), ids_of(np.tile(tokens, times))
+    b, gs, hs = Bounds(n64(z), 1.0), n64(g), n64(h)
+    weights = np.zeros(z.shape)
+    weights[np.arange(some), np.clip(tokens, 0, None)] = tokens >= 0
+    ref = ol.logprobs_gradient(n64(z), tokens, gs, hs)
+    bound = b.gradient(ref, dtype, False, np.abs(gs), (tokens >= 0).astype(float), weights, hs, b.entropy)
+    lp, _, _ = ol.logprobs(n64(z), tokens)
+    q = ol.teacher(ids, n64(y), 1.0, None, cols)
+    rel, e_loss = distill_bounds(b, ids, q, n64(y), 1.0, False)
+    loss_ref, _ = ol.distill(n64(z), ids, n64(y))
+    d_ref = ol.distill_gradient(n64(z), ids, n64(y), gs)
+    weights, wrel = np.zeros(z.shape), np.zeros(z.shape)
+    for r in range(some):
+        for j in np.flatnonzero(q[r] > 0):
+            weights[r, ids[r, j]] += q[r, j]
+            wrel[r, ids[r, j]] += q[r, j] * (rel[r, j] + 40 * U)
+    d_bound = b.gradient(d_ref, dtype, False, np.abs(gs), q.sum(1), weights)
+    d_bound = d_bound + 1.02 * np.abs(gs)[:, None] * (b.p * ((q * rel).sum(1) + 12 * U * q.sum(1))[:, None] + wrel)
+    for inplace in (False, True):
+        own = many.clone()
+        r, d = mb.mgrit_token_logprobs_step(own, t, g.repeat(times), h.repeat(times), dlogits=own if inplace else None)
+        for i in {0, times - 1}:
+            at = slice(i * some, (i + 1) * some)
+            close(d[at], ref, bound, "gradient")
+            close(r.lse[at], b.lse, b.lse_bound(), "lse")
+            close(r.logprob[at], lp, b.lp_bound(np.clip(tokens, 0, None)[:, None])[:, 0], "logprob")
+        own = many.clone()
+        loss, lse, d = mb.mgrit_distill_step(own, ids_of(ids).repeat(times, 1), y.repeat(times, 1), g.repeat(times), dlogits=own if inplace else None)
+        for i in {0, times - 1}:
+            at = slice(i * some, (i + 1) * some)
+            close(d[at], d_ref, d_bound, "distillation's gradient")
+            close(loss[at], loss_ref, e_loss, "loss")
+            close(lse[at], b.lse, b.lse_bound(), "lse")
+
+
 @pytest.mark.parametrize("cols,dtype", [(200001, BF16), (131073, BF16), (65537, F32), (262145, F32)])
 def test_steps_of_rows_that_no_block_holds(cols, dtype):
     """The rows' sums in a launch of their own, the gradient in another; in place as well."""
@@ -634,44 +675,15 @@ def test_steps_of_rows_that_no_block_holds(cols, dtype):
     for rows in (1, 3, 520):
         if rows > 3 and dtype is F32 and cols > 200000:
             continue
-        some = min(rows, 3)
-        z, tokens = logits(rows, some, cols, dtype), some_tokens(rows + 1, some, cols)
-        g, h, ids, y = floats(1, some), floats(2, some, spread=0.3), lists(3, some, cols, 30), floats(4, some, 30)
-        g[torch.from_numpy(tokens < 0).cuda()] = 0.0
-        times = rows // some
-        many, t = z.repeat(times, 1), ids_of(np.tile(tokens, times))
-        b, gs, hs = Bounds(n64(z), 1.0), n64(g), n64(h)
-        weights = np.zeros(z.shape)
-        weights[np.arange(some), np.clip(tokens, 0, None)] = tokens >= 0
-        ref = ol.logprobs_gradient(n64(z), tokens, gs, hs)
-        bound = b.gradient(ref, dtype, False, np.abs(gs), (tokens >= 0).astype(float), weights, hs, b.entropy)
-        lp, _, _ = ol.logprobs(n64(z), tokens)
-        q = ol.teacher(ids, n64(y), 1.0, None, cols)
-        rel, e_loss = distill_bounds(b, ids, q, n64(y), 1.0, False)
-        loss_ref, _ = ol.distill(n64(z), ids, n64(y))
-        d_ref = ol.distill_gradient(n64(z), ids, n64(y), gs)
-        weights, wrel = np.zeros(z.shape), np.zeros(z.shape)
-        for r in range(some):
-            for j in np.flatnonzero(q[r] > 0):
-                weights[r, ids[r, j]] += q[r, j]
-                wrel[r, ids[r, j]] += q[r, j] * (rel[r, j] + 40 * U)
-        d_bound = b.gradient(d_ref, dtype, False, np.abs(gs), q.sum(1), weights)
-        d_bound = d_bound + 1.02 * np.abs(gs)[:, None] * (b.p * ((q * rel).sum(1) + 12 * U * q.sum(1))[:, None] + wrel)
-        for inplace in (False, True):
-            own = many.clone()
-            r, d = mb.mgrit_token_logprobs_step(own, t, g.repeat(times), h.repeat(times), dlogits=own if inplace else None)
-            for i in {0, times - 1}:
-                at = slice(i * some, (i + 1) * some)
-                close(d[at], ref, bound, "gradient")
-                close(r.lse[at], b.lse, b.lse_bound(), "lse")
-                close(r.logprob[at], lp, b.lp_bound(np.clip(tokens, 0, None)[:, None])[:, 0], "logprob")
-            own = many.clone()
-            loss, lse, d = mb.mgrit_distill_step(own, ids_of(ids).repeat(times, 1), y.repeat(times, 1), g.repeat(times), dlogits=own if inplace else None)
-            for i in {0, times - 1}:
-                at = slice(i * some, (i + 1) * some)
-                close(d[at], d_ref, d_bound, "distillation's gradient")
-                close(loss[at], loss_ref, e_loss, "loss")
-                close(lse[at], b.lse, b.lse_bound(), "lse")
+        check_steps(rows, min(rows, 3), cols, dtype)
+
+
+@pytest.mark.parametrize("rows", [1, 64, 65])
+@pytest.mark.parametrize("cols,dtype", [(65536, BF16), (65551, BF16), (131072, BF16), (32768, F32), (32771, F32), (65536, F32)])
+def test_steps_of_few_long_rows(cols, dtype, rows):
+    """Both sides of where few long rows leave the registers for parts."""
+    say("few long rows", rows, cols, dtype)
+    check_steps(rows, 5 if rows == 65 else min(rows, 4), cols, dtype)
 
 
 @pytest.mark.parametrize("cols", [9000, 20000, 30000, 40000, 60000, 100000, 130000])

@@ -114,8 +114,10 @@ def test_workspaces():
     assert forward(one, ld=50257, ws=None, n=need, **top) == INVALID and forward(one, ld=50257, ws=8 * P + 128, n=need, **top) == INVALID
     need = mb.mgrit_distill_workspace_bytes(1, 50257, bf16, 3)
     assert need > 0 and d_forward(one, ld=50257, ws=8 * P, n=need - 1) == SMALL and d_forward(one, ld=50257) == INVALID
-    # a step needs one for rows that no block holds
-    assert mb.mgrit_token_logprobs_workspace_bytes(4, 131072, bf16, step=True) == 0 == mb.mgrit_distill_workspace_bytes(9000, 65536, f32, 3, step=True)
+    # a step needs one for rows that no block holds, and for few long ones
+    assert mb.mgrit_token_logprobs_workspace_bytes(65, 131072, bf16, step=True) == 0 == mb.mgrit_distill_workspace_bytes(9000, 65536, f32, 3, step=True)
+    assert mb.mgrit_token_logprobs_workspace_bytes(64, 131072, bf16, step=True) > 0 < mb.mgrit_distill_workspace_bytes(1, 65536, f32, 3, step=True)
+    assert mb.mgrit_token_logprobs_workspace_bytes(1, 65536, bf16, step=True) == 0 == mb.mgrit_distill_workspace_bytes(1, 32768, f32, 3, step=True)
     need = mb.mgrit_token_logprobs_workspace_bytes(4, 200001, bf16, step=True)
     assert need > 0 and step(wide, ld=200001, ldd=200001, ws=8 * P, n=need - 1) == SMALL and step(wide, ld=200001, ldd=200001) == INVALID
     need = mb.mgrit_distill_workspace_bytes(4, 200001, bf16, 3, step=True)
