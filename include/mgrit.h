@@ -451,9 +451,10 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
  * Backward:  dlogits_i = (g_logprob ([i = token] - p_i) - g_entropy p_i (ln p_i + H)) / temperature
  *   g_logprob          device [rows];  g_entropy  device [rows], or NULL for 0
  * _step does both in one call that reads the logits once where a row fits, for cotangents that are known beforehand (a mean
- * of cross entropies: g_logprob = -1 / count); logprob and entropy may be NULL, lse may be NULL.
+ * of cross entropies: g_logprob = -1 / count); logprob and entropy may be NULL, lse may be NULL.  What it writes per row must not
+ * lie on the cotangents (or a teacher's lse) that it reads.
  * Workspace of _forward (step 0) and _step (step 1): 256-byte aligned, mgrit_token_logprobs_workspace_bytes (host only; 0, also on
- * invalid arguments: none is needed and it may be NULL). */
+ * invalid arguments: none is needed and it may be NULL).  It is for the call's own rows: fewer rows can need more. */
 #define MGRIT_TOP_MOST 64
 enum { MGRIT_IDS_I32 = 0, MGRIT_IDS_I64 = 1 };
 typedef struct mgrit_logits_desc {

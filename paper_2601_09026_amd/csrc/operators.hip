@@ -82,6 +82,17 @@ int check_teacher(const mgrit_logits_desc* d, const mgrit_teacher* t) {
   STCHK(check_ids(d, t->ids));
   return d->rows && (!t->logits || !element_aligned(t->logits, t->dtype) || !aligned(t->lse, 4)) ? MGRIT_INVALID_ARG : MGRIT_OK;
 }
+// two arrays of one value per row that do not meet
+bool apart(const mgrit_logits_desc* d, const float* p, const float* q) {
+  const int64_t bytes = reinterpret_cast<intptr_t>(p) - reinterpret_cast<intptr_t>(q);
+  return !p || !q || (bytes < 0 ? -bytes : bytes) >= d->rows * 4;
+}
+// A step's values, one of a row, are written while others still read what the row is given: none lies on that, or on another.
+int check_step(const mgrit_logits_desc* d, const float* const (&out)[3], const float* g, const float* h) {
+  for (int i = 0; i < 3; ++i)
+    if (!apart(d, out[i], g) || !apart(d, out[i], h) || !apart(d, out[i], out[(i + 1) % 3])) return MGRIT_INVALID_ARG;
+  return MGRIT_OK;
+}
 // gradients beside the logits, or in their place: nowhere across them
 int check_dlogits(const mgrit_logits_desc* d, const void* logits, int64_t stride, const void* dlogits, int64_t dstride) {
   STCHK(check_rows(d->rows, d->cols, dlogits, dstride, d->dtype));
@@ -259,7 +270,7 @@ int mgrit_token_logprobs_step(const mgrit_logits_desc* desc, const void* logits,
   STCHK(check_ids(desc, tokens));
   STCHK(check_floats(desc, g_logprob));
   if (!aligned(g_entropy, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4)) return MGRIT_INVALID_ARG;
-  if ((logprob && (logprob == entropy || logprob == lse)) || (entropy && entropy == lse)) return MGRIT_INVALID_ARG;
+  STCHK(check_step(desc, {logprob, entropy, lse}, g_logprob, g_entropy));
   STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
   STCHK(check_workspace(mgrit_token_logprobs_workspace_bytes(desc, 0, 1), workspace, workspace_bytes));
   LogitsArgs a = logits_args(desc, logits, stride);
@@ -306,7 +317,8 @@ int mgrit_distill_step(const mgrit_logits_desc* desc, const void* logits, int64_
   STCHK(check_rows(desc->rows, desc->cols, logits, stride, desc->dtype));
   STCHK(check_teacher(desc, teacher));
   STCHK(check_floats(desc, loss));
-  if (!aligned(g_loss, 4) || !aligned(lse, 4) || (desc->rows && loss == lse)) return MGRIT_INVALID_ARG;
+  if (!aligned(g_loss, 4) || !aligned(lse, 4)) return MGRIT_INVALID_ARG;
+  STCHK(check_step(desc, {loss, lse, nullptr}, g_loss, teacher->lse));
   STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
   STCHK(check_workspace(mgrit_distill_workspace_bytes(desc, teacher->kept, 1), workspace, workspace_bytes));
   LogitsArgs a = logits_args(desc, logits, stride);

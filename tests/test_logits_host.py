@@ -158,3 +158,16 @@ def test_binding_refuses_what_the_library_cannot_see():
             f()
     with pytest.raises(ValueError, match="expected a tensor"):
         mb.mgrit_token_logprobs_forward([1.0])
+
+
+def test_steps_do_not_write_what_they_read():
+    """A row's values are written while other wavefronts of the row still read its cotangents and its teacher."""
+    for at in (-12, -4, 0, 4, 12):                         # 4 rows: 16 bytes each
+        for out in ("lp", "H", "lse"):
+            assert step(**{out: 30 * P + at}, g=30 * P) == INVALID
+            assert step(**{out: 30 * P + at}, h=30 * P) == INVALID
+        for out in ("loss", "lse"):
+            assert d_step(**{out: 30 * P + at}, g=30 * P) == INVALID
+            assert d_step(**{out: 30 * P + at}, t=teacher(lse=30 * P)) == INVALID
+        assert step(lp=30 * P + at, H=30 * P) == INVALID and step(lse=30 * P + at, H=30 * P) == INVALID and step(lse=30 * P + at, lp=30 * P) == INVALID
+        assert d_step(lse=30 * P + at, loss=30 * P) == INVALID
