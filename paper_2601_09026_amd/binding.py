@@ -918,7 +918,7 @@ def _vector(given: Optional[torch.Tensor], n: int, name: str, device: int, like:
 
 
 def _c_int32(n: int) -> int:
-    if n > MOST_COLS:
+    if not -MOST_COLS <= n <= MOST_COLS:
         raise ValueError(f"expected a length of at most 2^31 - 1, got {n}")
     return n
 
@@ -1142,7 +1142,7 @@ def _logits_desc(logits: torch.Tensor, rows: int, cols: int, ids: torch.dtype, t
 
 
 def mgrit_token_logprobs_workspace_bytes(rows: int, cols: int, dtype: torch.dtype, top_k: int = 0, step: bool = False) -> int:
-    return int(lib().mgrit_token_logprobs_workspace_bytes(LogitsDesc(rows, _c_int32(cols), _DTYPES[dtype], 0, 1.0), top_k, int(step)))
+    return int(lib().mgrit_token_logprobs_workspace_bytes(LogitsDesc(rows, _c_int32(cols), _DTYPES[dtype], 0, 1.0), _c_int32(top_k), int(step)))
 
 
 def mgrit_token_logprobs_forward(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0, temperature: float = 1.0,

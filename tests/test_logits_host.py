@@ -171,3 +171,10 @@ def test_steps_do_not_write_what_they_read():
             assert d_step(**{out: 30 * P + at}, t=teacher(lse=30 * P)) == INVALID
         assert step(lp=30 * P + at, H=30 * P) == INVALID and step(lse=30 * P + at, H=30 * P) == INVALID and step(lse=30 * P + at, lp=30 * P) == INVALID
         assert d_step(lse=30 * P + at, loss=30 * P) == INVALID
+
+
+def test_workspace_query_of_no_count():
+    f32 = torch.float32
+    for k in ((1 << 32) + 5, -(1 << 32) + 5):
+        with pytest.raises(ValueError, match="2\\^31 - 1"):
+            mb.mgrit_token_logprobs_workspace_bytes(1, 50257, f32, k)
