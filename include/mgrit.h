@@ -480,8 +480,9 @@ int mgrit_token_logprobs_step(const mgrit_logits_desc* desc, const void* logits,
  *       probabilities under the whole teacher, which need not sum to 1)
  *   loss = sum_j q_j (ln q_j - ln p_id(j)),  dlogits_i = g_loss / temperature (p_i sum_j q_j - sum_{j: id(j) = i} q_j)
  * p: the student's, as above.  Ids below 0 fill up shorter lists; a row without any id, or with q = 0 throughout, has loss and
- * gradient 0; an id of cols and more, or a value that is NaN or +infinity, gives NaN for both.  An id may come twice: its
- * shares add up.  top_ids and top_logprobs of a teacher's rows at temperature 1 are such a list.
+ * gradient 0; an id of cols and more, a value that is NaN or +infinity, or, by a teacher's lse, q that are no numbers or whose
+ * sum passes fp32's range, give NaN for both.  An id may come twice: its shares add up.  top_ids and top_logprobs of a teacher's rows
+ * at temperature 1 are such a list.
  *   g_loss             device [rows], or NULL for 1;  lse  device [rows] out, may be NULL; the backward pass takes it
  * Everything else as above. */
 #define MGRIT_KEPT_MOST 256

@@ -61,7 +61,8 @@ def logprobs_gradient(z, tokens, g, h=None, tau=1.0, lse=None, entropy=None):
 
 
 def teacher(ids, values, tau=1.0, lse=None, cols=None):
-    """q [rows, kept], 0 where there is no id; all NaN in rows with an id out of range or a value that is no number."""
+    """q [rows, kept], 0 where there is no id; all NaN in rows with an id out of range, a value that is no number, or shares whose sum
+    is beyond 32 bits' range."""
     ids, y = np.asarray(ids), np.asarray(values, np.float64) / tau
     q = np.zeros(y.shape)
     for r in range(len(y)):
@@ -69,7 +70,10 @@ def teacher(ids, values, tau=1.0, lse=None, cols=None):
         if (ids[r] >= cols).any() or np.isnan(y[r][live]).any() or (y[r][live] == np.inf).any():
             q[r] = np.nan
         elif lse is not None:
-            q[r][live] = np.exp(y[r][live] - lse[r])
+            with np.errstate(invalid="ignore", over="ignore"):
+                q[r][live] = np.exp(y[r][live] - lse[r])
+            if not q[r].sum() <= np.finfo(np.float32).max:
+                q[r] = np.nan
         elif live.any() and y[r][live].max() > -np.inf:
             e = np.exp(y[r][live] - y[r][live].max())
             q[r][live] = e / e.sum()

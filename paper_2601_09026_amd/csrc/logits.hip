@@ -453,7 +453,7 @@ __device__ __forceinline__ void join_waves(const Run<T>& r, int index, Sums& sum
 // ---- what a row is measured by ----------------------------------------------------------
 // Ids with weights w that sum to `mass`.  Log probabilities (MODE 0): the token, w = 1, in the first lane.  Distillation
 // (MODE 1): the teacher's kept ids with w = q, id j in lane j % 64.  mass 0: the row has none; NaN: one is out of range (or a
-// teacher's logit is no number).  Held by one wavefront.
+// teacher's logit is no number, or the sum passes fp32's range).  Held by one wavefront.
 constexpr int KEPT = 256;
 template <int MODE> struct Points {
   static constexpr int N = MODE == 0 ? 1 : KEPT / WAVE, OUTSIDE = -2;
@@ -513,7 +513,7 @@ template <int MODE> struct Points {
         }
         mass = all_sum(m);
       }
-      if (__any(out)) mass = __builtin_nanf("");
+      if (__any(out) || !(mass < __builtin_inff())) mass = __builtin_nanf("");         // (infinite: by a teacher's log-sum-exp alone)
     }
   }
   __device__ __forceinline__ void load(const LogitsArgs& a, long row) {

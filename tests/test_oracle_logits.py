@@ -77,3 +77,17 @@ def test_rows_without_a_distribution():
     ids = np.array([[-1, -1], [0, 1], [0, 1], [1, 4], [0, 1]])
     loss, _ = ol.distill(z, ids, np.array([[0.0, 0], [0, 0], [0, 0], [0, 0], [-np.inf, 0]]))
     assert loss[0] == 0 and loss[1] == np.inf and np.isnan(loss[2]) and np.isnan(loss[3]) and np.isclose(loss[4], np.log(3))
+
+
+def test_teachers_beyond_the_range():
+    """With a log-sum-exp a share may be any number: those that 32 bits do not hold, alone or summed up, are none."""
+    inf, nan = np.inf, np.nan
+    ids = np.array([[0, 1]] * 8 + [[0, -1]])
+    y = np.array([[0.0, 0], [inf, 0], [200, 0], [88.5, 88.5], [0, 0], [0, 0], [0, 0], [-inf, -inf], [0, inf]])
+    lse = np.array([0.5, 0, 0, 0, -inf, inf, nan, 0, 0.5])
+    q = ol.teacher(ids, y, 1.0, lse, 4)
+    assert np.isnan(q).all(1).tolist() == [False, True, True, True, True, False, True, False, False]
+    assert np.allclose(q[0], np.exp(-0.5)) and (q[5] == 0).all() and (q[7] == 0).all() and np.allclose(q[8], [np.exp(-0.5), 0])
+    loss, _ = ol.distill(np.zeros((9, 4)), ids, y, 1.0, lse)
+    d = ol.distill_gradient(np.zeros((9, 4)), ids, y, None, 1.0, lse)
+    assert (np.isnan(loss) == np.isnan(q).any(1)).all() and (np.isnan(d).all(1) == np.isnan(q).any(1)).all() and (d[5] == 0).all()
