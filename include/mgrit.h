@@ -450,6 +450,8 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
  *                      largest logits in descending order, equal ones by their id, and their log probabilities
  * Backward:  dlogits_i = (g_logprob ([i = token] - p_i) - g_entropy p_i (ln p_i + H)) / temperature
  *   g_logprob          device [rows];  g_entropy  device [rows], or NULL for 0
+ *   ln p_i is taken as z_i / temperature - lse for the lse given.  Its 32 bits are all that is left of a row's sum: half a step of
+ *   lse is an error of every ln p of the row, 0.03 where the quotients are about 10^6.  _step does not have it.
  * _step does both in one call that reads the logits once where a row fits, for cotangents that are known beforehand (a mean
  * of cross entropies: g_logprob = -1 / count); logprob and entropy may be NULL, lse may be NULL.  What it writes per row must not
  * lie on the cotangents (or a teacher's lse) that it reads.

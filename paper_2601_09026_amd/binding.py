@@ -1196,7 +1196,8 @@ def mgrit_token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, ls
                                   temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None,
                                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The logits' gradient for cotangents g_logprob (and g_entropy) of mgrit_token_logprobs_forward's values; lse and
-    entropy as it returned them.  dlogits may be the logits themselves, which it then replaces."""
+    entropy as it returned them (where logits / temperature are beyond 10^4 or so their 32 bits show in p; _step does without
+    them).  dlogits may be the logits themselves, which it then replaces."""
     device = _device_of(logits, "logits")
     rows, cols, stride = _check_rows(logits, "logits", device)
     lead = logits.shape[:-1]

@@ -671,9 +671,13 @@ struct Slope {
     }
     zero = !ENTROPY && mass == 0.f;
   }
-  __device__ __forceinline__ void from_lse(float lse) {
-    top = 0.f;
-    off = lse;
+  // A given lse, through the logit that has it for a quotient by tau: only differences to that are rounded, not the quotients, which
+  // may be far larger.  off is what it, rounded, leaves of lse; left: 1 / tau - inv_tau.  (Figures past 2^100 leave nothing to tell apart.)
+  __device__ __forceinline__ void from_lse(float lse, float tau) {
+    top = lse * tau;
+    const float left = fmaf(-tau, inv_tau, 1.f) * inv_tau;
+    off = fmaf(-top, left, fmaf(-top, inv_tau, lse));
+    if (!(fabsf(lse) < 0x1p100f)) { top = 0.f; off = lse; }
     zero |= lse == -__builtin_inff();
   }
   __device__ __forceinline__ void from_sums(const RowSums& r) {
@@ -843,7 +847,7 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
   Slope s;
   if constexpr (FROM == GIVEN) {
     s.template set<ENTROPY>(a, row, pt.mass, MODE == 0 ? 1.f : -1.f, ENTROPY ? a.entropy_in[row] : 0.f);
-    s.from_lse(a.lse_in[row]);
+    s.from_lse(a.lse_in[row], a.tau);
   } else {
     const RowSums r(joined(a, row, c), a.tau);
     s.template set<ENTROPY>(a, row, pt.mass, MODE == 0 ? 1.f : -1.f, r.entropy);

@@ -63,3 +63,81 @@ def test_teachers_with_a_log_sum_exp(cols, values):
                 if given:                                  # (the log-sum-exp is the call's own here: half a step of it, and its error)
                     bound = bound + 1.02 * b.p * (slope * mass * (b.lse_bound() + U * np.abs(b.lse)))[:, None]
                 close(x[fine], d_ref[fine], bound[fine], "gradient")
+
+
+# ------------------------------------------------------------------ statistics far from zero
+def given_bound(z, tau, lse, ref, dtype, slope, mass, weights, h=None, entropy=None):
+    """The gradient from a given log-sum-exp in 32 bits, an argument that is exact here.  ln p = z / tau - lse: a difference to lse tau,
+    its product with a rounded constant and one more difference, to what lse tau left out (at most 4 u |lse|): with the
+    exponential's own (5 |ln p| + 2 |what was left out| + 4) u, and of the second order 16 u^2 |lse|.  No rounding of the quotients.
+    A p below 2^-126 counts as 0: with its factor of at most |h| / tau (88 + H) an error of its own."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        lp = np.asarray(z, np.float64) / tau - lse[:, None]
+        p = np.exp(lp)
+    lp = np.where(p > 0, np.abs(lp), 0.0)
+    rel = U * (5 * lp + 4 + 8 * U * np.abs(lse)[:, None] + 16 * U * np.abs(lse)[:, None])
+    e = p * (slope * mass)[:, None] * (rel + 8 * U) + slope[:, None] * weights * 16 * U
+    if h is not None:
+        b = (np.abs(h) / tau)[:, None]
+        e += p * b * ((lp + np.abs(entropy)[:, None]) * (rel + 10 * U) + rel) + 2.0 ** -126 * b * (88 + np.abs(entropy)[:, None])
+    return p, 1.01 * e + HALF_STEP[dtype] * (np.abs(ref) + 1.01 * e) + 2.0 ** -120 * ((slope * mass)[:, None] + 1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [40, 1000, 3000, 9000, 50257])
+def test_backward_of_sharp_and_shifted_rows(cols, dtype):
+    """Temperatures that are no powers of two, quotients up to 4e6: the gradient is that of the log-sum-exp given, to the last bits."""
+    say("backward of sharp rows", cols, dtype)
+    rows = 6
+    for tau, offset, spread in ((1e-4, 100.0, 2.0), (0.7, 3e5, 200.0), (3.0, 3e5, 3.0), (0.01, -3e3, 0.5), (1e4, 1e8, 1e5), (0.3, 0.0, 3.0), (1.0, 3e5, 200.0)):
+        tau = float(np.float32(tau))                       # (an argument of 32 bits: half a step of it is 0.03 of a quotient of 1e6)
+        z = (floats(cols, rows, cols) * spread + offset).to(dtype)
+        z[:, 2] = z[:, 1]
+        z[1, 3] = z[1].max()
+        z[2, ::2] = -INF
+        tokens = np.array([0, 3, 1, cols - 1, 2, -1])
+        tokens[3] = int(z[3].float().argmax())
+        g, h = floats(1, rows), floats(2, rows, spread=0.3)
+        _, H, lse = ol.logprobs(n64(z), tokens, tau)
+        lse32, H32 = (torch.from_numpy(x.astype(np.float32)).cuda() for x in (lse, H))
+        live = (tokens >= 0).astype(float)
+        weights = np.zeros(z.shape)
+        weights[np.arange(rows), np.clip(tokens, 0, None)] = live
+        gs = n64(g) * live
+        for kw in (dict(), dict(g_entropy=h, entropy=H32)):
+            hs = n64(h) if kw else None
+            ref = ol.logprobs_gradient(n64(z), tokens, gs, hs, tau, n64(lse32), n64(H32))
+            _, bound = given_bound(n64(z), tau, n64(lse32), ref, dtype, np.abs(gs) / tau, live, weights, hs, n64(H32))
+            for times in (1, 90):
+                t = ids_of(np.tile(tokens, times))
+                d = mb.mgrit_token_logprobs_backward(z.repeat(times, 1), t, lse32.repeat(times), g.repeat(times), temperature=tau,
+                                                     **{k: v.repeat(times) for k, v in kw.items()})
+                close(d[:rows], ref, bound, "gradient")
+                close(d[-rows:], ref, bound, "gradient")
+        ids, y = np.stack([tokens.clip(0), np.ones(rows, int)], 1), floats(5, rows, 2) * tau
+        q = ol.teacher(ids, n64(y), tau, None, cols)
+        rel, _ = distill_bounds(Bounds(n64(z), tau), ids, q, n64(y), tau, False)
+        ref = ol.distill_gradient(n64(z), ids, n64(y), n64(g), tau, None, n64(lse32))
+        weights, wrel, slope = np.zeros(z.shape), np.zeros(z.shape), np.abs(n64(g)) / tau
+        for r in range(rows):
+            for j in range(2):
+                weights[r, ids[r, j]] += q[r, j]
+                wrel[r, ids[r, j]] += q[r, j] * (rel[r, j] + 2 * U)
+        p, bound = given_bound(n64(z), tau, n64(lse32), ref, dtype, slope, q.sum(1), weights)
+        bound = bound + 1.02 * slope[:, None] * (p * ((q * rel).sum(1) + 12 * U)[:, None] + wrel)
+        close(mb.mgrit_distill_backward(z, ids_of(ids), y, lse32, g, temperature=tau), ref, bound, "distillation's gradient")
+
+
+def test_backward_of_a_log_sum_exp_at_the_range():
+    """Rows of one logit near the type's ends, or none: p is 1 or 0, no NaN comes of a quotient that has left the range."""
+    say("lse at the range")
+    for tau in (1.0, 0.5, 2.0):
+        z = torch.full((5, 300), -INF, device="cuda")
+        for r, x in enumerate((1e38, -1e38, 1e-40, 0.0)):
+            z[r, 7] = x
+        t, g = torch.tensor([7, 7, 3, -1, 7], device="cuda"), torch.ones(5, device="cuda")
+        lse = mb.mgrit_token_logprobs_forward(z, t, temperature=tau).lse
+        d = mb.mgrit_token_logprobs_backward(z, t, lse, g, temperature=tau)
+        ref = torch.zeros_like(z)
+        ref[2, 3], ref[2, 7] = 1.0 / tau, -1.0 / tau
+        assert torch.equal(d, ref)
