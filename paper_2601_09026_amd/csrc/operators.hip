@@ -230,7 +230,7 @@ int mgrit_token_logprobs_forward(const mgrit_logits_desc* desc, const void* logi
   STCHK(check_top(desc, top_k));
   STCHK(check_rows(desc->rows, desc->cols, logits, stride, desc->dtype));
   if (logprob || tokens) STCHK(check_ids(desc, tokens));
-  if (!logprob && !entropy && !lse && !top_k) return MGRIT_INVALID_ARG;
+  if (desc->rows && !logprob && !entropy && !lse && !top_k) return MGRIT_INVALID_ARG;
   if (!aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4)) return MGRIT_INVALID_ARG;
   if ((logprob && (logprob == entropy || logprob == lse)) || (entropy && entropy == lse)) return MGRIT_INVALID_ARG;
   if (top_k) {

@@ -65,6 +65,24 @@ def test_teachers_with_a_log_sum_exp(cols, values):
                 close(x[fine], d_ref[fine], bound[fine], "gradient")
 
 
+# ------------------------------------------------------------------ no rows
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lead", [(0,), (0, 3), (2, 0)])
+def test_an_empty_batch(lead, dtype):
+    """Every call of no rows, alternatives or none asked for."""
+    say("empty batch", lead, dtype)
+    z, t, g = torch.empty((*lead, 70), dtype=dtype, device="cuda"), torch.empty(lead, dtype=I64, device="cuda"), torch.empty(lead, device="cuda")
+    ids, y = torch.empty((*lead, 3), dtype=I32, device="cuda"), torch.empty((*lead, 3), dtype=dtype, device="cuda")
+    for tokens in (t, None):
+        for k in (0, 4):
+            r = mb.mgrit_token_logprobs_forward(z, tokens, top_k=k)
+            assert r.entropy.shape == r.lse.shape == lead and (r.logprob is None) == (tokens is None) and (r.top_ids is None) == (k == 0)
+    assert mb.mgrit_token_logprobs_backward(z, t, g, g, entropy=g, g_entropy=g).shape == z.shape
+    assert mb.mgrit_token_logprobs_step(z, t, g, g)[1].shape == z.shape
+    assert mb.mgrit_distill_forward(z, ids, y)[0].shape == lead and mb.mgrit_distill_forward(z, ids, y, teacher_lse=g)[1].shape == lead
+    assert mb.mgrit_distill_backward(z, ids, y, g).shape == z.shape and mb.mgrit_distill_step(z, ids, y, g)[2].shape == z.shape
+
+
 # ------------------------------------------------------------------ statistics far from zero
 def given_bound(z, tau, lse, ref, dtype, slope, mass, weights, h=None, entropy=None):
     """The gradient from a given log-sum-exp in 32 bits, an argument that is exact here.  ln p = z / tau - lse: a difference to lse tau,

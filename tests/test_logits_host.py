@@ -178,3 +178,18 @@ def test_workspace_query_of_no_count():
     for k in ((1 << 32) + 5, -(1 << 32) + 5):
         with pytest.raises(ValueError, match="2\\^31 - 1"):
             mb.mgrit_token_logprobs_workspace_bytes(1, 50257, f32, k)
+
+
+def test_no_rows_without_arrays():
+    """A batch without rows has arrays without memory: nothing is asked for then, and nothing refused."""
+    none = desc(rows=0)
+    for tokens in (None, 2 * P):
+        for k in (0, 3):
+            assert forward(none, z=None, tokens=tokens, lp=None, H=None, lse=None, k=k) == OK
+    for lse in (None, 22 * P):
+        empty = teacher(ids=None, logits=None, lse=lse)
+        assert d_forward(none, z=None, t=empty, loss=None, lse=None) == OK and d_backward(none, z=None, t=empty, lse=None, g=None, dz=None) == OK
+        assert d_step(none, z=None, t=empty, g=None, loss=None, lse=None, dz=None) == OK
+    assert step(none, z=None, tokens=None, g=None, lp=None, H=None, lse=None, dz=None) == OK
+    assert forward(desc(rows=-1), z=None, tokens=None, lp=None, H=None, lse=None) == INVALID
+    assert forward(tokens=None, lp=None, H=None, lse=None) == INVALID
