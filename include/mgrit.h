@@ -453,8 +453,9 @@ int mgrit_q8_weight_grad(int64_t rows, int32_t out_features, int32_t in_features
  *   ln p_i is taken as z_i / temperature - lse for the lse given.  Its 32 bits are all that is left of a row's sum: half a step of
  *   lse is an error of every ln p of the row, 0.03 where the quotients are about 10^6.  _step does not have it.
  * _step does both in one call that reads the logits once where a row fits, for cotangents that are known beforehand (a mean
- * of cross entropies: g_logprob = -1 / count); logprob and entropy may be NULL, lse may be NULL.  What it writes per row must not
- * lie on the cotangents (or a teacher's lse) that it reads.
+ * of cross entropies: g_logprob = -1 / count); logprob and entropy may be NULL, lse may be NULL.
+ * What a call writes, its workspace too, must lie neither on what it reads nor on what else it writes (MGRIT_INVALID_ARG), dlogits on the
+ * logits apart.  Only a forward pass may write a value per row over an argument of 32 bits per row, entry upon entry.
  * Workspace of _forward (step 0) and _step (step 1): 256-byte aligned, mgrit_token_logprobs_workspace_bytes (host only; 0, also on
  * invalid arguments: none is needed and it may be NULL).  It is for the call's own rows: fewer rows can need more. */
 #define MGRIT_TOP_MOST 64

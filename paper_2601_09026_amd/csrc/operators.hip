@@ -82,22 +82,53 @@ int check_teacher(const mgrit_logits_desc* d, const mgrit_teacher* t) {
   STCHK(check_ids(d, t->ids));
   return d->rows && (!t->logits || !element_aligned(t->logits, t->dtype) || !aligned(t->lse, 4)) ? MGRIT_INVALID_ARG : MGRIT_OK;
 }
-// two arrays of one value per row that do not meet
-bool apart(const mgrit_logits_desc* d, const float* p, const float* q) {
-  const int64_t bytes = reinterpret_cast<intptr_t>(p) - reinterpret_cast<intptr_t>(q);
-  return !p || !q || (bytes < 0 ? -bytes : bytes) >= d->rows * 4;
+// What a call reads and writes: arrays of `row` bytes per row of logits, `stride` bytes apart.  While a result is written other blocks still
+// read and write, so none lies on another or on an argument.  But a forward pass reads what it needs of a row before it writes the row's
+// values: those may take the place of an argument, entry upon entry.  The logits' gradient against the logits: check_dlogits.
+class Arrays {
+  struct Span { const char* at; int64_t row, stride, rows; bool written; };
+  Span all[16];
+  int n = 0;
+  int64_t rows;
+  bool fine = true;
+  static bool meet(const Span& a, const Span& b) {       // one of them without gaps between its rows
+    const Span &s = a.row == a.stride ? b : a, &flat = a.row == a.stride ? a : b;
+    const int64_t off = flat.at - s.at, bytes = flat.row * flat.rows;
+    if (off >= (s.rows - 1) * s.stride + s.row || off + bytes <= 0) return false;
+    return off < 0 || off % s.stride < s.row || off % s.stride + bytes > s.stride;
+  }
+  void add(const void* p, int64_t row, int64_t stride, int64_t count, bool written, bool upon) {
+    if (!p || !row || !count) return;
+    const Span s = {static_cast<const char*>(p), row, stride, count, written};
+    for (int i = 0; written && i < n; ++i)
+      fine = fine && (!meet(s, all[i]) || (upon && !all[i].written && all[i].at == s.at && all[i].row == row && all[i].stride == stride));
+    all[n++] = s;
+  }
+ public:
+  explicit Arrays(const mgrit_logits_desc* d) : rows(d->rows) {}
+  Arrays& reads(const void* p, int64_t row) { add(p, row, row, rows, false, false); return *this; }
+  Arrays& reads_rows(const void* p, int64_t row, int64_t stride) { add(p, row, stride, rows, false, false); return *this; }
+  Arrays& writes(const void* p, int64_t row, bool upon = false) { add(p, row, row, rows, true, upon); return *this; }
+  Arrays& writes_rows(const void* p, int64_t row, int64_t stride) { add(p, row, stride, rows, true, false); return *this; }     // (first of the results, logits after it)
+  Arrays& writes_once(const void* p, int64_t bytes) { add(p, bytes, bytes, rows ? 1 : 0, true, false); return *this; }
+  int check() const { return fine ? MGRIT_OK : MGRIT_INVALID_ARG; }
+};
+int64_t elem_bytes(int dtype) { return dtype == MGRIT_DTYPE_BF16 ? 2 : 4; }
+int64_t id_bytes(const mgrit_logits_desc* d) { return d->id_dtype == MGRIT_IDS_I64 ? 8 : 4; }
+Arrays& read_logits(Arrays& a, const mgrit_logits_desc* d, const void* logits, int64_t stride) {
+  return a.reads_rows(logits, d->cols * elem_bytes(d->dtype), stride * elem_bytes(d->dtype));
 }
-// A step's values, one of a row, are written while others still read what the row is given: none lies on that, or on another.
-int check_step(const mgrit_logits_desc* d, const float* const (&out)[3], const float* g, const float* h) {
-  for (int i = 0; i < 3; ++i)
-    if (!apart(d, out[i], g) || !apart(d, out[i], h) || !apart(d, out[i], out[(i + 1) % 3])) return MGRIT_INVALID_ARG;
-  return MGRIT_OK;
+Arrays& write_dlogits(Arrays& a, const mgrit_logits_desc* d, const void* dlogits, int64_t stride) {
+  return a.writes_rows(dlogits, d->cols * elem_bytes(d->dtype), stride * elem_bytes(d->dtype));
+}
+Arrays& read_teacher(Arrays& a, const mgrit_logits_desc* d, const mgrit_teacher* t) {
+  return a.reads(t->ids, t->kept * id_bytes(d)).reads(t->logits, t->kept * elem_bytes(t->dtype)).reads(t->lse, 4);
 }
 // gradients beside the logits, or in their place: nowhere across them
 int check_dlogits(const mgrit_logits_desc* d, const void* logits, int64_t stride, const void* dlogits, int64_t dstride) {
   STCHK(check_rows(d->rows, d->cols, dlogits, dstride, d->dtype));
   if (d->rows == 0) return MGRIT_OK;
-  const int64_t size = d->dtype == MGRIT_DTYPE_BF16 ? 2 : 4, apart = static_cast<const char*>(dlogits) - static_cast<const char*>(logits);
+  const int64_t size = elem_bytes(d->dtype), apart = static_cast<const char*>(dlogits) - static_cast<const char*>(logits);
   const int64_t z_bytes = ((d->rows - 1) * stride + d->cols) * size, dz_bytes = ((d->rows - 1) * dstride + d->cols) * size;
   if (apart >= z_bytes || -apart >= dz_bytes) return MGRIT_OK;
   if (d->rows > 1 && stride != dstride) return MGRIT_INVALID_ARG;
@@ -232,13 +263,16 @@ int mgrit_token_logprobs_forward(const mgrit_logits_desc* desc, const void* logi
   if (logprob || tokens) STCHK(check_ids(desc, tokens));
   if (desc->rows && !logprob && !entropy && !lse && !top_k) return MGRIT_INVALID_ARG;
   if (!aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4)) return MGRIT_INVALID_ARG;
-  if ((logprob && (logprob == entropy || logprob == lse)) || (entropy && entropy == lse)) return MGRIT_INVALID_ARG;
   if (top_k) {
     STCHK(check_ids(desc, top_ids));
     STCHK(check_floats(desc, top_logprobs));
-    if (desc->rows && (top_ids == top_logprobs || top_ids == tokens || top_logprobs == logprob || top_logprobs == entropy || top_logprobs == lse)) return MGRIT_INVALID_ARG;
   }
-  STCHK(check_workspace(mgrit_token_logprobs_workspace_bytes(desc, top_k, 0), workspace, workspace_bytes));
+  const size_t need = mgrit_token_logprobs_workspace_bytes(desc, top_k, 0);
+  STCHK(check_workspace(need, workspace, workspace_bytes));
+  Arrays arrays(desc);
+  read_logits(arrays, desc, logits, stride).reads(tokens, id_bytes(desc)).writes(logprob, 4, true).writes(entropy, 4, true).writes(lse, 4, true);
+  arrays.writes(top_k ? top_ids : nullptr, top_k * id_bytes(desc)).writes(top_k ? top_logprobs : nullptr, top_k * 4, true);
+  STCHK(arrays.writes_once(workspace, need).check());
   LogitsArgs a = logits_args(desc, logits, stride);
   a.tokens = tokens; a.logprob = logprob; a.entropy = entropy; a.lse = lse; a.top_k = top_k; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
   return enqueue_logits(desc, a, 0, workspace, stream);
@@ -257,6 +291,9 @@ int mgrit_token_logprobs_backward(const mgrit_logits_desc* desc, const void* log
     STCHK(check_floats(desc, g_entropy));
   }
   STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
+  Arrays arrays(desc);
+  arrays.reads(tokens, id_bytes(desc)).reads(lse, 4).reads(g_logprob, 4).reads(g_entropy ? entropy : nullptr, 4).reads(g_entropy, 4);
+  STCHK(write_dlogits(arrays, desc, dlogits, dlogits_stride).check());
   LogitsArgs a = logits_args(desc, logits, stride);
   a.tokens = tokens; a.lse_in = lse; a.entropy_in = entropy; a.g = g_logprob; a.h = g_entropy; a.dz = dlogits; a.lddz = dlogits_stride;
   return enqueue_logits(desc, a, 0, nullptr, stream);
@@ -270,9 +307,13 @@ int mgrit_token_logprobs_step(const mgrit_logits_desc* desc, const void* logits,
   STCHK(check_ids(desc, tokens));
   STCHK(check_floats(desc, g_logprob));
   if (!aligned(g_entropy, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4)) return MGRIT_INVALID_ARG;
-  STCHK(check_step(desc, {logprob, entropy, lse}, g_logprob, g_entropy));
   STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
-  STCHK(check_workspace(mgrit_token_logprobs_workspace_bytes(desc, 0, 1), workspace, workspace_bytes));
+  const size_t need = mgrit_token_logprobs_workspace_bytes(desc, 0, 1);
+  STCHK(check_workspace(need, workspace, workspace_bytes));
+  Arrays arrays(desc);
+  arrays.reads(tokens, id_bytes(desc)).reads(g_logprob, 4).reads(g_entropy, 4);
+  read_logits(write_dlogits(arrays, desc, dlogits, dlogits_stride), desc, logits, stride).writes(logprob, 4).writes(entropy, 4).writes(lse, 4);
+  STCHK(arrays.writes_once(workspace, need).check());
   LogitsArgs a = logits_args(desc, logits, stride);
   a.tokens = tokens; a.logprob = logprob; a.entropy = entropy; a.lse = lse; a.g = g_logprob; a.h = g_entropy; a.dz = dlogits; a.lddz = dlogits_stride;
   return enqueue_logits(desc, a, 0, workspace, stream);
@@ -289,8 +330,12 @@ int mgrit_distill_forward(const mgrit_logits_desc* desc, const void* logits, int
   STCHK(check_rows(desc->rows, desc->cols, logits, stride, desc->dtype));
   STCHK(check_teacher(desc, teacher));
   STCHK(check_floats(desc, loss));
-  if (!aligned(lse, 4) || (desc->rows && loss == lse)) return MGRIT_INVALID_ARG;
-  STCHK(check_workspace(mgrit_distill_workspace_bytes(desc, teacher->kept, 0), workspace, workspace_bytes));
+  if (!aligned(lse, 4)) return MGRIT_INVALID_ARG;
+  const size_t need = mgrit_distill_workspace_bytes(desc, teacher->kept, 0);
+  STCHK(check_workspace(need, workspace, workspace_bytes));
+  Arrays arrays(desc);
+  read_teacher(read_logits(arrays, desc, logits, stride), desc, teacher).writes(loss, 4, true).writes(lse, 4, true);
+  STCHK(arrays.writes_once(workspace, need).check());
   LogitsArgs a = logits_args(desc, logits, stride);
   add_teacher(a, teacher);
   a.loss = loss; a.lse = lse;
@@ -305,6 +350,9 @@ int mgrit_distill_backward(const mgrit_logits_desc* desc, const void* logits, in
   STCHK(check_floats(desc, lse));
   if (!aligned(g_loss, 4)) return MGRIT_INVALID_ARG;
   STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
+  Arrays arrays(desc);
+  read_teacher(arrays, desc, teacher).reads(lse, 4).reads(g_loss, 4);
+  STCHK(write_dlogits(arrays, desc, dlogits, dlogits_stride).check());
   LogitsArgs a = logits_args(desc, logits, stride);
   add_teacher(a, teacher);
   a.lse_in = lse; a.g = g_loss; a.dz = dlogits; a.lddz = dlogits_stride;
@@ -318,9 +366,13 @@ int mgrit_distill_step(const mgrit_logits_desc* desc, const void* logits, int64_
   STCHK(check_teacher(desc, teacher));
   STCHK(check_floats(desc, loss));
   if (!aligned(g_loss, 4) || !aligned(lse, 4)) return MGRIT_INVALID_ARG;
-  STCHK(check_step(desc, {loss, lse, nullptr}, g_loss, teacher->lse));
   STCHK(check_dlogits(desc, logits, stride, dlogits, dlogits_stride));
-  STCHK(check_workspace(mgrit_distill_workspace_bytes(desc, teacher->kept, 1), workspace, workspace_bytes));
+  const size_t need = mgrit_distill_workspace_bytes(desc, teacher->kept, 1);
+  STCHK(check_workspace(need, workspace, workspace_bytes));
+  Arrays arrays(desc);
+  read_teacher(arrays, desc, teacher).reads(g_loss, 4);
+  read_logits(write_dlogits(arrays, desc, dlogits, dlogits_stride), desc, logits, stride).writes(loss, 4).writes(lse, 4);
+  STCHK(arrays.writes_once(workspace, need).check());
   LogitsArgs a = logits_args(desc, logits, stride);
   add_teacher(a, teacher);
   a.loss = loss; a.lse = lse; a.g = g_loss; a.dz = dlogits; a.lddz = dlogits_stride;

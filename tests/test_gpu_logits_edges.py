@@ -83,6 +83,64 @@ def test_an_empty_batch(lead, dtype):
     assert mb.mgrit_distill_backward(z, ids, y, g).shape == z.shape and mb.mgrit_distill_step(z, ids, y, g)[2].shape == z.shape
 
 
+# ------------------------------------------------------------------ where values may lie
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(5, 40), (700, 3000), (600, 9000), (3, 50257), (300, 70001)])
+def test_values_in_the_place_of_arguments(rows, cols, dtype):
+    """A forward pass may write a value of 32 bits per row over an argument of 32 bits per row, entry upon entry."""
+    say("in an argument's place", rows, cols, dtype)
+    z, t, y = logits(1, rows, cols, dtype), ids_of(some_tokens(2, rows, cols), I32), floats(3, rows, 5)
+    ids, lse_t = ids_of(lists(4, rows, cols, 5), I32), floats(5, rows, spread=0.3) + 4.0
+    for k in (0, min(cols, 20)):
+        ref = mb.mgrit_token_logprobs_forward(z, t, k)
+        for name in ("logprob", "entropy", "lse"):
+            own = t.clone()
+            r = mb.mgrit_token_logprobs_forward(z, own, k, **{name: own.view(F32)})
+            for a, b in zip(r[:5 if k else 3], ref):
+                assert torch.equal(a, b)
+    for kept in (5, 1):
+        ids_, y_ = ids[:, :kept].contiguous(), y[:, :kept].contiguous()
+        ref = mb.mgrit_distill_forward(z, ids_, y_, teacher_lse=lse_t)
+        for name in ("loss", "lse"):
+            for place in ("lse",) + (("ids", "values") if kept == 1 else ()):
+                own = dict(ids=ids_.clone(), values=y_.clone(), lse=lse_t.clone())
+                out = own[place].view(F32).view(rows)
+                r = mb.mgrit_distill_forward(z, own["ids"], own["values"], teacher_lse=own["lse"], **{name: out})
+                assert r[0 if name == "loss" else 1] is out and torch.equal(r[0], ref[0]) and torch.equal(r[1], ref[1])
+
+
+def test_values_between_rows():
+    """Values and cotangents in what a matrix of wider rows has to spare, and one array directly behind another."""
+    say("between rows")
+    rows, cols = 3, 1000
+    z, t, g = logits(1, rows, cols), ids_of([5, -1, 7]), floats(2, rows)
+    ids, y = ids_of(lists(3, rows, cols, 4)), floats(4, rows, 4)
+    big = torch.zeros(rows, cols + 12, device="cuda")
+    view, room = big[:, :cols], [big[i, cols + 3 * j:cols + 3 * j + 3] for i in range(2) for j in range(4)]
+    view.copy_(z)
+    ref, d = mb.mgrit_token_logprobs_step(z, t, g)
+    r = mb.mgrit_token_logprobs_forward(view, t, logprob=room[0], entropy=room[1], lse=room[2])
+    for a, b in zip(r[:3], mb.mgrit_token_logprobs_forward(view, t)):
+        assert torch.equal(a, b)
+    room[3].copy_(g)
+    r, e = mb.mgrit_token_logprobs_step(view, t, room[3], logprob=room[4], entropy=room[5], lse=room[6], dlogits=view)
+    assert r.lse is room[6] and torch.equal(view, d) and torch.equal(room[3], g)
+    for a, b in zip(r[:3], ref):
+        assert torch.equal(a, b)
+    loss, lse, d = mb.mgrit_distill_step(z, ids, y, g)
+    view.copy_(z)
+    mb.mgrit_distill_step(view, ids, y, room[3], loss=room[0], lse=room[1], dlogits=view)
+    assert torch.equal(view, d) and torch.equal(room[0], loss) and torch.equal(room[1], lse) and torch.equal(room[3], g)
+    view.copy_(z)
+    mb.mgrit_distill_backward(view, ids, y, room[1], room[3], dlogits=view)
+    assert torch.equal(view, mb.mgrit_distill_backward(z, ids, y, lse, g))
+    for refused in (lambda: mb.mgrit_distill_backward(z, ids, y, lse, room[3], dlogits=big[:, 12:]),
+                    lambda: mb.mgrit_token_logprobs_step(view, t, g, lse=big[0, cols - 1:cols + 2]),
+                    lambda: mb.mgrit_token_logprobs_forward(view, t, entropy=room[0], lse=big[0, cols + 2:cols + 5])):
+        with pytest.raises(mb.MgritError):
+            refused()
+
+
 # ------------------------------------------------------------------ statistics far from zero
 def given_bound(z, tau, lse, ref, dtype, slope, mass, weights, h=None, entropy=None):
     """The gradient from a given log-sum-exp in 32 bits, an argument that is exact here.  ln p = z / tau - lse: a difference to lse tau,
