@@ -10,7 +10,7 @@
 // instructions of a lane (counted at 2048 x 131072 fp32, loop and sums included), and in bf16 twice as many elements come
 // with the same bytes.  Hence the exponents of one instruction (Reader) and sums of which nothing is rescaled as a rule.
 // Values, fp32, 2048 x 131072: 158 us, 6.8 TB/s; bf16, 4096 x 50257: 70 us, 5.9 TB/s, 81 with 5 alternatives.  Backward,
-// 4096 x 50257 bf16 with entropies: 140 us, 5.9 TB/s (a large copy reaches 5.7).  Both in one call, 8192 x 50304 bf16: 312 us, 5.3
+// 4096 x 50257 bf16 with entropies: 143 us, 5.8 TB/s (a large copy reaches 5.7).  Both in one call, 8192 x 50304 bf16: 312 us, 5.3
 // TB/s over one reading and one writing; the two calls one after the other take 133 and 275.  One row of 50257 with 20
 // alternatives: 12 us in two launches.
 #include <math.h>
@@ -790,7 +790,7 @@ template <typename T> __device__ __forceinline__ void write_left_out(const Run<T
 }
 
 // Bound by its bytes: 4096 x 50257 bf16 with one token a row 141 us, 5.8 TB/s.  A teacher's list costs what every run's
-// wavefronts spend on looking through it: 146 us with 1 id a row, 151 with 16, 156 with 64, 192 with 200.
+// wavefronts spend on looking through it: 147 us with 1 id a row, 151 with 16, 157 with 64, 190 with 200, 200 with 256.
 // FROM: where a row's sums come from.  GIVEN: its log-sum-exp (and entropy) are arguments; PARTS: they lie in the workspace, and the
 // rows' values are written as well.  A block (W = 4) writes a run of a row, a wavefront (W = 1) a whole short one, STEP
 // vectors per lane.  dz may be z
@@ -881,6 +881,8 @@ __global__ void __launch_bounds__(THREADS) logits_gradient_kernel(const LogitsAr
 // RV vectors per lane.  A row is read once; the next row's loads are issued as its registers are written.  With the row's
 // sums in the workspace and the row read again, 8192 x 50304 bf16 takes 394 us, here 319; that is the way of larger rows
 // (1024 x 200000 bf16: 215 us), and of few long ones (fits()).
+// A teacher's list is one wavefront's, while the others wait: 4096 x 50304 bf16 160 us with 1 id a row, 170 with 32, 173 with 64,
+// 189 with 128, 223 with 200, 238 with 256.
 // GRAD false: the values alone, of short rows (NW = 1), TOP with alternatives.
 template <typename T, int NW, int RV, bool ENTROPY, int MODE, int OCC, bool GRAD, bool TOP>
 __global__ void __launch_bounds__(NW == 1 ? THREADS : NW * WAVE, OCC) logits_step_kernel(const LogitsArgs a) {
@@ -1123,7 +1125,8 @@ bool short_rows(int cols, bool is_bf16) { return cols <= (is_bf16 ? 4096 : 2048)
 // Few rows: a row's elements are shared out over several blocks, with a join behind them, from 64 KB on, into no less than
 // 8 KB, at most two blocks per CU; 128 KB a part in any case.  In parts and whole: 1 x 50257 bf16 5.7 and 7.7 us, with 20
 // alternatives 11.7 and 11.8; 16 x 131072 fp32 7.3 and 27.5, with 20 17.4 and 35.7; 300 x 200000 bf16 with 20 39.5 and 50.4; the join costs
-// where a part is short and there are alternatives: 16 x 32003 fp32 with 20 14.6 and 12.4, 256 x 50257 bf16 with 20 19.0 and 16.9.
+// where a part is short and there are alternatives: 16 x 32003 fp32 with 20 14.6 and 12.4, 256 x 50257 bf16 with 20 19.0 and 16.9 (the
+// rule does not look at top_k).
 int parts_of(long rows, int cols, bool is_bf16) {
   const long bytes = (long)cols * (is_bf16 ? 2 : 4);
   if (bytes < 65536 || rows >= 512 || rows < 1) return 1;
@@ -1134,9 +1137,12 @@ int parts_of(long rows, int cols, bool is_bf16) {
   return (int)(parts < MOST_PARTS ? parts : MOST_PARTS);
 }
 // Rows that a step keeps in registers.  Few long ones keep too few CUs at work so and go through the workspace, in parts (in
-// registers and in parts: 1 x 131072 bf16 19.3 and 7.7 us, 32 rows 21.4 and 10.4, 77 rows 24.9 and 19.2, 200 rows 30.4 and 37.2; 32 x
-// 65536 fp32 14.7 and 9.4).  Up to 128 KB a row the two are about even for few rows (32 x 50304 bf16 10.8 and 9.5, distillation 10.5 and
-// 12.0) and one launch is less than two.
+// registers and in parts: 1 x 131072 bf16 19.3 and 7.7 us, 32 rows 21.4 and 10.4, 77 rows 24.4 and 19.2, 128 rows 27.0 and 24.3, 200 rows
+// 30.1 and 36.9, 300 rows 56.2 and 46.4, 400 rows 55.9 and 58.9; 32 x 65536 fp32 14.7 and 9.4, 77 rows 18.2 and 16.2, 128 rows 20.5
+// and 22.3, 257 rows 45.5 and 38.9, 300 rows 46.0 and 43.0).  The bound lies below the break-even at 100 to 150 rows, and does not know of
+// the second one: from 257 to about 350 rows a second round of blocks, one per CU, has hardly begun, and parts would take 7 to 25 per cent
+// less.  Up to 128 KB a row the two are about even for few rows (32 x 50304 bf16 10.8 and 9.5, distillation 10.5 and 12.0) and one
+// launch is less than two.
 bool fits(long rows, int cols, bool is_bf16) {
   const long bytes = (long)cols * (is_bf16 ? 2 : 4);
   return bytes <= 262144 && (bytes <= 131072 || rows > 64);
@@ -1180,9 +1186,11 @@ template <typename T, int MODE, int NW, int RV, int OCC> hipError_t step_of(cons
   });
 }
 // The fewer wavefronts hold a row, the more rows a CU works on, whose loads, sums and stores overlap; few rows are done
-// soonest by many (step, bf16, with few as the rule has it and the other way: 1 x 50304 9.7 and 13.6 us, 200 rows 14.8 and 18.0, 500 rows
-// 26.4 and 26.6, 600 rows 31.4 and 36.8, 1000 rows 38 and 49; 500 x 3000 5.4 and 6.6).  Wavefronts per SIMD, by a sweep: what
-// the registers of RV vectors leave room for (16384 x 3000, distillation, 4 and 5: 54 and 71 us).
+// soonest by many (step, bf16, with few as the rule has it and the other way: 1 x 50304 9.7 and 13.6 us, 64 rows 11.3 and 14.5, 256 rows
+// 15.6 and 19.1, 500 rows 26.5 and 25.9, 600 rows 31.4 and 36.8, 1000 rows 38 and 49; 256 x 20000 9.6 and 10.3; 500 x 3000 5.4 and 6.6).  Not so
+// everywhere: blocks of 16 wavefronts run one per CU, and from 257 rows on a second round keeps few of them at work (257 x 50304 25.7 and
+// 22.9, 300 rows 24.8 and 23.7, 300 x 20000 15.0 and 12.8), and a row of up to 32 KB is too short for 16 (64 x 9000 7.1 and 6.4, 300 rows 11.9
+// and 7.7).  Wavefronts per SIMD, by a sweep: what the registers of RV vectors leave room for (16384 x 3000, distillation, 4 and 5: 54 and 71 us).
 template <typename T, int MODE> hipError_t step(const LogitsArgs& a, hipStream_t st) {
   const int vecs = a.cols / vec<T>();                    // (an odd element less may make one vector less)
   const bool few = a.rows <= 2 * compute_units();
