@@ -280,3 +280,78 @@ def test_steps_of_sharp_and_shifted_rows(cols, dtype):
                 close(d[at:at + rows], ref, bound, "gradient")
                 close(e[at:at + rows], d_ref, d_bound, "distillation's gradient")
                 close(loss[at:at + rows], loss_ref, e_loss, "loss")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_the_longest_rows(dtype):
+    """2^24 logits a row, whole and in slices at odd addresses: values, alternatives and both steps."""
+    cols, rows, kept = 2 ** 24, 2, 100
+    say("longest rows", dtype)
+    z, o = many_logits(1, rows, cols, dtype), operands(2, rows, cols, kept)
+    o["tokens"][:] = cols - 1, 5
+    o["ids"][1] = np.random.default_rng(3).integers(0, cols, kept)
+    o["ids"][:, 0] = cols - 1
+    t, ids, at = ids_of(o["tokens"]), ids_of(o["ids"]), np.arange(rows)
+    b, best = Bounds(n64(z), 1.0), ol.largest(n64(z), 64)
+    r = mb.mgrit_token_logprobs_forward(z, t, 64)
+    close(r.lse, b.lse, b.lse_bound(), "lse")
+    close(r.entropy, b.entropy, b.entropy_bound(), "entropy")
+    assert np.array_equal(r.top_ids.cpu().numpy(), best)
+    close(r.top_logprobs, np.take_along_axis(b.lp, best, 1), b.lp_bound(best), "alternatives")
+    s, d = mb.mgrit_token_logprobs_step(z, t, o["g"], o["h"])
+    check_tokens(z, at, o, s, d, True, dtype)
+    loss, lse, d = mb.mgrit_distill_step(z, ids, o["y"], o["g"])
+    check_teacher(z, at, o, loss, lse, d, False, 1.0, dtype)
+    big = many_logits(1, rows, cols, dtype, 3, 8)
+    view = big[:, 3:3 + cols]
+    loss, lse, d = mb.mgrit_distill_step(view, ids, o["y"], o["g"], dlogits=view)
+    check_teacher(z, at, o, loss, lse, d, False, 1.0, dtype)
+    assert untouched(big, cols, 3)
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(2 ** 24 + 40, 3, F32), (2 ** 24 + 40, 5, BF16), (2 ** 22 + 8, 4104, BF16)])
+def test_more_rows_than_blocks_along_x(rows, cols, dtype):
+    """8 rows over and over, more often than a launch has blocks in one direction: all have the results of the first 8."""
+    say("many rows", rows, cols, dtype)
+    z, o = many_logits(1, 8, cols, dtype), operands(2, 8, cols, 3)
+    times = rows // 8
+    assert rows % 8 == 0
+    t, ids = ids_of(o["tokens"], I32), ids_of(o["ids"], I32)
+    many = [x.repeat(times, *[1] * (x.dim() - 1)) for x in (z, t, o["g"], o["h"], ids, o["y"])]
+
+    def same(x, first):
+        """In pieces: the comparison's own memory stays small."""
+        for part in x.view(times, *first.shape).split(2 ** 16):
+            assert torch.equal(part, first.expand_as(part))
+    r = mb.mgrit_token_logprobs_forward(many[0], many[1], 3)
+    for x in r:
+        same(x, x[:8].clone())
+    at = np.arange(8)
+    b, best = Bounds(n64(z), 1.0), ol.largest(n64(z), 3)
+    close(r.lse[:8], b.lse, b.lse_bound(), "lse")
+    assert np.array_equal(r.top_ids[:8].cpu().numpy(), best)
+    loss, lse = mb.mgrit_distill_forward(many[0], many[4], many[5])
+    check_teacher(z, at, o, loss[:8], lse[:8], None, False, 1.0, dtype)
+    same(loss, loss[:8].clone())
+    H, lse, entropy = many[3], r.lse, r.entropy
+    zz, g, h = n64(z), n64(o["g"]) * (o["tokens"] >= 0), n64(o["h"])
+    weights, live = np.zeros(zz.shape), (o["tokens"] >= 0).astype(float)
+    weights[at, np.clip(o["tokens"], 0, None)] = live
+    ref = ol.logprobs_gradient(zz, o["tokens"], g, h, 1.0, n64(lse[:8]), n64(entropy[:8]))
+    # (in place: the gradient replaces the logits, which come back behind it)
+    d = mb.mgrit_token_logprobs_backward(many[0], many[1], lse, many[2], entropy=entropy, g_entropy=H, dlogits=many[0])
+    close(d[:8], ref, b.gradient(ref, dtype, True, np.abs(g), live, weights, h, b.entropy), "backward")
+    same(d, d[:8].clone())
+    many[0].view(times, 8, cols).copy_(z.expand(times, 8, cols))
+    s, d = mb.mgrit_token_logprobs_step(many[0], many[1], many[2], H, dlogits=many[0])
+    check_tokens(z, at, o, s, d, True, dtype)
+    same(d, d[:8].clone())
+    many[0].view(times, 8, cols).copy_(z.expand(times, 8, cols))
+    d = mb.mgrit_distill_backward(many[0], many[4], many[5], lse, many[2], dlogits=many[0])
+    same(d, d[:8].clone())
+    many[0].view(times, 8, cols).copy_(z.expand(times, 8, cols))
+    loss, lse, d = mb.mgrit_distill_step(many[0], many[4], many[5], many[2], dlogits=many[0])
+    check_teacher(z, at, o, loss[:8], lse[:8], d[:8], False, 1.0, dtype)
+    same(d, d[:8].clone())
+    del many, d
+    torch.cuda.empty_cache()
